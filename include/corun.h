@@ -54,6 +54,7 @@ typedef enum {
 } corun_status;
 
 enum { CORUN_KV_CONTIGUOUS = 0, CORUN_KV_PAGED = 1 };
+enum { CORUN_KV_BF16 = 0, CORUN_KV_E4M3 = 1 };   /* corun_kv.dtype */
 
 /* Model shape.  n_experts = top_k = expert_ffn = 0 selects a dense SwiGLU
  * MLP of width `ffn`; otherwise every layer routes each token to top_k of
@@ -106,6 +107,24 @@ typedef struct {
     void *const *k;
     void *const *v;
     const int32_t *page_table;
+    /* The element type (0 = bf16).  CORUN_KV_E4M3: codes of one byte each in
+     * the same element order, and for every block of scale_block tokens (16,
+     * 32 or 64; it divides max_seq_len or page_size) of one kv head a
+     * power-of-two scale: an element is code 2^(byte - 127), codes OCP e4m3
+     * (no infinities).  k_scale, v_scale: HOST arrays of n_layers DEVICE
+     * pointers to the bytes, [n_slots, n_kv_heads, max_seq_len / scale_block]
+     * or [num_pages, n_kv_heads, page_size / scale_block].  Appending chooses
+     * a block's scale as the smallest power of two with amax <= 448 scale over
+     * the finite values of the tokens appended by the call (at least 2^-100),
+     * or the scale of the block's earlier tokens if that is larger; where it
+     * grows, the earlier codes are rounded to it.  Codes are the nearest ones
+     * (ties to even); what is not finite is stored as NaN.  Bytes 27 .. 247
+     * are scales that appending writes; a caller that fills a cache keeps to
+     * them.  The buffers of an e4m3 cache start on 16-byte boundaries. */
+    int32_t dtype;
+    int32_t scale_block;
+    uint8_t *const *k_scale;
+    uint8_t *const *v_scale;
 } corun_kv;
 
 /* Creation options; pass NULL for defaults (all fields 0). */
@@ -257,6 +276,114 @@ corun_status corun_prefill_chunk(corun_engine *e, const int32_t *tokens, int32_t
  * beyond its slot's cache), CORUN_E_INVAL (bad sizes, slots, tokens). */
 corun_status corun_prefill_batch(corun_engine *e, const int32_t *tokens, const int32_t *lens, const int32_t *slots,
                                  int32_t n, int32_t *tokens_out, float *last_logits);
+
+/* ---------------------------------------------------------------------------
+ * Operators of a decoder layer on a cache, without an engine: rotary positions
+ * with the KV append, and attention over an 8-bit cache.  An engine whose
+ * corun_kv is of dtype CORUN_KV_E4M3, or that is given corun_options.rope, runs
+ * the same kernels.
+ *
+ * They run on `stream` (a hipStream_t; NULL = the null stream) on the current
+ * device, return without waiting for it, allocate nothing, and can be captured
+ * into a graph.  Tensors are DEVICE buffers of that device unless marked host;
+ * `kv` and its arrays of layers are host, read during the call.  bf16 rows
+ * (qkv, q, out) have strides ld_* in elements, multiples of 8; they and the
+ * cache's buffers start on 16-byte boundaries.  n_heads / n_kv_heads is a whole number from 1 to 16;
+ * head_dim 64 or 128.  A slot's pages are its own where a call appends.
+ * What a kernel alone can see it checks itself: no lengths, positions or
+ * page-table entries, whatever they hold, make it read or write outside the
+ * cache.
+ * ------------------------------------------------------------------------- */
+
+/* Which elements of a head a rotation pairs, over its first rot_dim elements:
+ * (i, i + rot_dim / 2) or (2 i, 2 i + 1), i < rot_dim / 2; the others stay. */
+enum { CORUN_ROPE_HALF = 0, CORUN_ROPE_INTERLEAVED = 1 };
+/* Frequencies: f_i = theta^(-2 i / rot_dim) radians per position;
+ *  LINEAR  f_i / factor (positions interpolated);
+ *  BANDS   by the turns n = trained_len f_i / (2 pi) that a pair makes over the
+ *          trained length: f_i / factor where n <= low, f_i where n >= high,
+ *          and g f_i + (1 - g) f_i / factor, g = (n - low) / (high - low),
+ *          between (interpolation "by parts", Peng et al., 2023). */
+enum { CORUN_ROPE_UNSCALED = 0, CORUN_ROPE_LINEAR = 1, CORUN_ROPE_BANDS = 2 };
+typedef struct {
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t rot_dim;       /* even, 2 .. head_dim; 0 = head_dim */
+    int32_t layout;        /* CORUN_ROPE_HALF | CORUN_ROPE_INTERLEAVED */
+    int32_t scaling;       /* CORUN_ROPE_UNSCALED | _LINEAR | _BANDS */
+    int32_t trained_len;   /* BANDS: >= 1 */
+    float magnitude;       /* rotated elements are multiplied by it; 0 = 1 */
+    double theta;          /* > 1 */
+    double factor;         /* LINEAR, BANDS: >= 1 */
+    double low, high;      /* BANDS: 0 <= low < high */
+} corun_rope_cfg;
+#define CORUN_ROPE_MAX_PAIRS 64
+/* A rotation as the kernels take it: made by corun_rope_init, or filled in by
+ * a caller with frequencies of its own (radians per position of each pair). */
+typedef struct {
+    int32_t head_dim, rot_dim, layout;
+    float magnitude;       /* > 0 */
+    double freq[CORUN_ROPE_MAX_PAIRS];
+} corun_rope;
+/* Host only.  CORUN_E_SHAPE for head_dim or rot_dim, CORUN_E_INVAL otherwise. */
+corun_status corun_rope_init(const corun_rope_cfg *cfg, corun_rope *out);
+
+/* The QKV epilogue of one padded decode step, bf16 or e4m3 cache: row r of
+ * qkv [rows, (n_heads + 2 n_kv_heads) head_dim] holds slot r's new token (q
+ * heads, then k, then v).  Live rows get their q and k heads rotated by their
+ * position, q [rows, n_heads head_dim] written, and k and v appended at
+ * that position of layer `layer` of slot r, whose earlier positions the
+ * caller has filled.  Nothing of a padding row is read or written.
+ *  valid      uint8 [rows], or NULL: all rows are live
+ *  positions  int32 [rows]
+ * A live row whose position is outside [0, capacity), or whose page is outside
+ * [0, num_pages), appends nothing and its q row is NaN.  rows <= n_slots. */
+corun_status corun_decode_append(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
+                                 const corun_rope *rope, int32_t rows, const void *qkv, int64_t ld_qkv,
+                                 const uint8_t *valid, const int32_t *positions, void *q, int64_t ld_q, void *stream);
+
+/* The same for whole prompts or chunks of them: rows of qkv and q are the n
+ * sequences' tokens back to back, lens[i] of them at positions starts[i] ..
+ * of slot slots[i].
+ *  n          1 .. CORUN_MAX_PREFILL_BATCH
+ *  lens       host int32 [n], each >= 1
+ *  starts     host int32 [n], or NULL: all 0
+ *  slots      host int32 [n], distinct
+ * CORUN_E_CAPACITY where starts[i] + lens[i] exceeds a slot's capacity.  Tokens
+ * on a page outside [0, num_pages) are not appended and their q rows are NaN. */
+corun_status corun_prefill_append(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
+                                  const corun_rope *rope, int32_t n, const int32_t *lens, const int32_t *starts,
+                                  const int32_t *slots, const void *qkv, int64_t ld_qkv, void *q, int64_t ld_q,
+                                  void *stream);
+
+/* Attention of a decode step over an e4m3 cache: row r of q [rows, n_heads
+ * head_dim] sees tokens 0 .. lens[r] - 1 of slot r (softmax(q k / sqrt(head_dim)) v,
+ * sums in fp32).  out [rows, n_heads head_dim]: zeros for padding rows and for
+ * lengths of 0, NaN where lens[r] is outside [0, max_len] or one of the row's
+ * pages outside [0, num_pages).  The launch follows from the sizes given
+ * here, not from the lengths.
+ *  valid      uint8 [rows], or NULL: all rows are live
+ *  lens       int32 [rows]
+ *  max_len    longest length that the launch covers; 0 = the slots' capacity
+ *  ws         workspace on a 16-byte boundary, its contents free between calls;
+ *             calls that may overlap need one each.  ws_bytes at least what
+ *             corun_decode_attention_workspace returns for the same sizes. */
+corun_status corun_decode_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t rows, const void *q, int64_t ld_q, const uint8_t *valid,
+                                    const int32_t *lens, int32_t max_len, void *out, int64_t ld_out, void *ws,
+                                    int64_t ws_bytes, void *stream);
+/* Bytes (>= 0), or a negative corun_status.  Host only. */
+int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                         int32_t rows, int32_t max_len);
+
+/* Causal attention of whole prompts, or chunks of them, over an e4m3 cache:
+ * rows of q and out as for corun_prefill_append; the query at position
+ * starts[i] + t sees tokens 0 .. starts[i] + t of slot slots[i], which earlier
+ * calls have appended.  A query that sees a page outside [0, num_pages) gets
+ * NaN.  A sequence's results do not depend on the others of the call. */
+corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t n, const int32_t *lens, const int32_t *starts,
+                                     const int32_t *slots, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                     void *stream);
 
 /* The engine's fixed batch size, model configuration and KV description
  * (copies; the k/v/page-table pointers are the caller's borrowed ones).

@@ -17,6 +17,9 @@ LIB_PATH = os.path.join(_HERE, "libcorun.so")
 
 OK, E_INVAL, E_SHAPE, E_CAPACITY, E_HIP, E_STATE = 0, -1, -2, -3, -4, -5
 KV_CONTIGUOUS, KV_PAGED = 0, 1
+KV_BF16, KV_E4M3 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_UNSCALED, ROPE_LINEAR, ROPE_BANDS = 0, 1, 2
 
 EXPORTS = ("corun_engine_create", "corun_engine_destroy", "corun_decode_step", "corun_decode_run",
            "corun_prefill", "corun_prefill_chunk", "corun_prefill_batch", "corun_check_config", "corun_check_batch",
@@ -25,7 +28,9 @@ EXPORTS = ("corun_engine_create", "corun_engine_destroy", "corun_decode_step", "
            "corun_engine_set_page_table_host",
            "corun_routing_trace",
            "corun_sched_create", "corun_sched_destroy", "corun_sched_add_request", "corun_sched_step",
-           "corun_sched_output", "corun_sched_state", "corun_sched_last_error")
+           "corun_sched_output", "corun_sched_state", "corun_sched_last_error",
+           "corun_rope_init", "corun_decode_append", "corun_prefill_append", "corun_decode_attention",
+           "corun_decode_attention_workspace", "corun_prefill_attention")
 
 # kernel ids of corun_time_kernel
 K_QKV_GEMM, K_O_GEMM, K_GATE_UP_GEMM, K_DOWN_GEMM, K_LM_HEAD, K_ATTN_SPLIT, K_ATTN_MERGE, K_RMSNORM, \
@@ -52,7 +57,19 @@ class Weights(C.Structure):
 class KV(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "layout", "n_slots", "max_seq_len", "page_size", "num_pages", "max_pages_per_seq")] + [
-        ("k", _PP), ("v", _PP), ("page_table", C.c_void_p)]
+        ("k", _PP), ("v", _PP), ("page_table", C.c_void_p), ("dtype", C.c_int32), ("scale_block", C.c_int32),
+        ("k_scale", _PP), ("v_scale", _PP)]
+
+
+class RopeCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "rot_dim", "layout", "scaling", "trained_len")] + [
+        ("magnitude", C.c_float)] + [(n, C.c_double) for n in ("theta", "factor", "low", "high")]
+
+
+class Rope(C.Structure):
+    """A rotation (corun_rope): made by :func:`rope`."""
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float),
+                ("freq", C.c_double * 64)]
 
 
 class Options(C.Structure):
@@ -141,6 +158,19 @@ def load():
                                     C.POINTER(C.c_int32), C.c_void_p]
     L.corun_sched_last_error.restype = C.c_char_p
     L.corun_sched_last_error.argtypes = []
+    L.corun_rope_init.restype = st
+    L.corun_rope_init.argtypes = [C.POINTER(RopeCfg), C.POINTER(Rope)]
+    i32, i64, ptr = C.c_int32, C.c_int64, C.c_void_p
+    L.corun_decode_append.restype = st
+    L.corun_decode_append.argtypes = [ptr, i32, i32, i32, ptr, i32, ptr, i64, ptr, ptr, ptr, i64, ptr]
+    L.corun_prefill_append.restype = st
+    L.corun_prefill_append.argtypes = [ptr, i32, i32, i32, ptr, i32, ptr, ptr, ptr, ptr, i64, ptr, i64, ptr]
+    L.corun_decode_attention.restype = st
+    L.corun_decode_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, i64, ptr, ptr, i32, ptr, i64, ptr, i64, ptr]
+    L.corun_decode_attention_workspace.restype = i64
+    L.corun_decode_attention_workspace.argtypes = [ptr, i32, i32, i32, i32, i32]
+    L.corun_prefill_attention.restype = st
+    L.corun_prefill_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr, i64, ptr]
     L.corun_last_error.restype = C.c_char_p
     L.corun_last_error.argtypes = []
     _lib = L
@@ -258,6 +288,180 @@ def sample_noalloc(logits, valid, positions, seeds, temperature, vocab=None, str
                                        sd.ctypes.data, tp.ctypes.data, tok.ctypes.data, lp.ctypes.data,
                                        C.c_void_p(stream.cuda_stream)))
     return tok, lp
+
+
+def rope(head_dim, theta=10000.0, rot_dim=0, layout=ROPE_HALF, scaling=ROPE_UNSCALED, factor=1.0, low=0.0, high=0.0,
+         trained_len=0, magnitude=1.0) -> Rope:
+    """corun_rope_init: the rotation of a model's q and k heads."""
+    c = RopeCfg(head_dim, rot_dim, layout, scaling, trained_len, magnitude, theta, factor, low, high)
+    r = Rope()
+    _check(load().corun_rope_init(C.byref(c), C.byref(r)))
+    return r
+
+
+class KvCache:
+    """A cache for the operators below: per-layer lists of device tensors, K
+    and V [n_slots, n_kv_heads, max_seq_len, head_dim] or, with page_table
+    (device int32 [n_slots, max_pages_per_seq]), [num_pages, n_kv_heads,
+    page_size, head_dim]; bf16, or e4m3 codes (float8_e4m3fn or uint8) with
+    scale bytes (float8_e8m0fnu or uint8) k_scale and v_scale [.., n_kv_heads,
+    tokens / scale_block].  The tensors are borrowed and kept alive."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, scale_block=0, page_table=None):
+        import torch
+        k, v = list(k), list(v)
+        e4m3 = k_scale is not None
+        codes = (torch.float8_e4m3fn, torch.uint8) if e4m3 else (torch.bfloat16,)
+        n, self.n_kv_heads, tokens, self.head_dim = k[0].shape
+        self.device = k[0].device
+        groups = [(k + v, codes, tuple(k[0].shape))]
+        if e4m3:
+            k_scale, v_scale = list(k_scale), list(v_scale)
+            if scale_block < 1 or len(k_scale) != len(k) or len(v_scale) != len(k):
+                raise ValueError("an e4m3 cache has scale bytes for every layer and a scale_block")
+            groups.append((k_scale + v_scale, (torch.float8_e8m0fnu, torch.uint8),
+                           (n, self.n_kv_heads, tokens // scale_block)))
+        if len(k) != len(v):
+            raise ValueError("as many layers of K as of V")
+        for tensors, types, shape in groups:
+            for t in tensors:
+                if t.dtype not in types or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError(f"cache tensors: {types} {shape}, contiguous, on {self.device}")
+        if page_table is not None and (page_table.dtype != torch.int32 or page_table.dim() != 2 or
+                                       not page_table.is_contiguous() or page_table.device != self.device):
+            raise ValueError("page_table: contiguous int32 [n_slots, max_pages_per_seq] on the cache's device")
+        self.layers = len(k)
+        self._keep = keep = [k, v, k_scale, v_scale, page_table]
+        if page_table is None:
+            self.kv = kv_struct(KV_CONTIGUOUS, n, k, v, keep, max_seq_len=tokens)
+        else:
+            self.kv = kv_struct(KV_PAGED, page_table.shape[0], k, v, keep, page_size=tokens, num_pages=n,
+                                max_pages_per_seq=page_table.shape[1], page_table=page_table)
+        if e4m3:
+            self.kv.dtype, self.kv.scale_block = KV_E4M3, scale_block
+            self.kv.k_scale, self.kv.v_scale = _ptr_array(k_scale, keep), _ptr_array(v_scale, keep)
+        self._at = C.addressof(self.kv)
+
+
+def _layer(cache, layer):
+    if not 0 <= layer < cache.layers:
+        raise ValueError(f"layer {layer} of {cache.layers}")
+    return layer
+
+
+def _rows(cache, t, name):
+    """(rows, row width, row stride) of a 2-D or 3-D bf16 tensor of head rows."""
+    import torch
+    if t.dtype != torch.bfloat16 or t.device != cache.device or t.dim() not in (2, 3) or t.stride(-1) != 1 or \
+            (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: bf16 rows of heads on {cache.device}, the elements of a row contiguous")
+    width = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
+    return t.shape[0], width, (t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0)))
+
+
+def _heads(cache, width, name):
+    if width % cache.head_dim:
+        raise ValueError(f"{name}: rows of {width} elements are not heads of {cache.head_dim}")
+    return width // cache.head_dim
+
+
+def _vec(cache, t, dtype, n, name):
+    if t.dtype not in dtype or t.device != cache.device or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtype[0]} [{n}] on {cache.device}")
+    return t.data_ptr()
+
+
+def _stream(cache, stream):
+    import torch
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _append_rows(cache, qkv, q, rope):
+    if rope.head_dim != cache.head_dim:
+        raise ValueError(f"rope of head_dim {rope.head_dim}, cache of {cache.head_dim}")
+    n, wq, ldq = _rows(cache, q, "q")
+    m, w, ld = _rows(cache, qkv, "qkv")
+    nq = _heads(cache, wq, "q")
+    if n != m or w != (nq + 2 * cache.n_kv_heads) * cache.head_dim:
+        raise ValueError("qkv: a row of q, k and v heads for every row of q")
+    return n, nq, ld, ldq
+
+
+def decode_append(cache, layer, qkv, positions, rope, q, valid=None, stream=None) -> None:
+    """corun_decode_append: rotate the q and k heads of one decode step's packed
+    QKV rows (bf16 [rows, (n_heads + 2 n_kv_heads) head_dim], row r = slot r) at
+    positions (device int32 [rows]), write q (bf16 [rows, n_heads head_dim]),
+    append k and v.  valid: device uint8 [rows].  Does not wait."""
+    import torch
+    rows, nq, ld, ldq = _append_rows(cache, qkv, q, rope)
+    pos = _vec(cache, positions, (torch.int32,), rows, "positions")
+    vm = None if valid is None else _vec(cache, valid, (torch.uint8, torch.bool), rows, "valid")
+    _check(load().corun_decode_append(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, C.addressof(rope), rows,
+                                      qkv.data_ptr(), ld, vm, pos, q.data_ptr(), ldq, _stream(cache, stream)))
+
+
+def _sequences(lens, starts, slots, rows):
+    ln, sl = _np(lens, np.int32), _np(slots, np.int32)
+    sr = None if starts is None else _np(starts, np.int32)
+    if ln.ndim != 1 or sl.shape != ln.shape or (sr is not None and sr.shape != ln.shape):
+        raise ValueError("lens, starts and slots: one entry for each sequence")
+    if int(ln.sum(dtype=np.int64)) != rows:
+        raise ValueError(f"the sequences have {int(ln.sum(dtype=np.int64))} tokens, the tensors {rows} rows")
+    return ln, sr, sl
+
+
+def prefill_append(cache, layer, qkv, lens, starts, slots, rope, q, stream=None) -> None:
+    """corun_prefill_append: the same for n sequences' tokens back to back;
+    lens, starts (None: all 0) and slots are host sequences of n."""
+    rows, nq, ld, ldq = _append_rows(cache, qkv, q, rope)
+    ln, sr, sl = _sequences(lens, starts, slots, rows)
+    _check(load().corun_prefill_append(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, C.addressof(rope), ln.size,
+                                       ln.ctypes.data, None if sr is None else sr.ctypes.data, sl.ctypes.data,
+                                       qkv.data_ptr(), ld, q.data_ptr(), ldq, _stream(cache, stream)))
+
+
+def decode_attention_workspace(cache, rows, n_heads, max_len=0) -> int:
+    """Bytes of workspace that decode_attention needs for these sizes."""
+    n = load().corun_decode_attention_workspace(cache._at, n_heads, cache.n_kv_heads, cache.head_dim, rows, max_len)
+    if n < 0:
+        raise CorunError(n, last_error())
+    return n
+
+
+def _attention_rows(cache, q, out):
+    n, w, ldq = _rows(cache, q, "q")
+    m, wo, ldo = _rows(cache, out, "out")
+    if n != m or w != wo:
+        raise ValueError("out: as many rows and heads as q")
+    return n, _heads(cache, w, "q"), ldq, ldo
+
+
+def decode_attention(cache, layer, q, lens, out, ws, valid=None, max_len=0, stream=None) -> None:
+    """corun_decode_attention: attention of one query token per row (bf16
+    [rows, n_heads head_dim]) over the first lens[r] (device int32 [rows])
+    tokens of slot r of an e4m3 cache.  ws: a device uint8 tensor of
+    decode_attention_workspace bytes, not shared by calls that may overlap."""
+    import torch
+    rows, nq, ldq, ldo = _attention_rows(cache, q, out)
+    ln = _vec(cache, lens, (torch.int32,), rows, "lens")
+    vm = None if valid is None else _vec(cache, valid, (torch.uint8, torch.bool), rows, "valid")
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != cache.device:
+        raise ValueError(f"ws: contiguous uint8 on {cache.device}")
+    _check(load().corun_decode_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, rows,
+                                         q.data_ptr(), ldq, vm, ln, max_len, out.data_ptr(), ldo, ws.data_ptr(),
+                                         ws.numel(), _stream(cache, stream)))
+
+
+def prefill_attention(cache, layer, q, lens, starts, slots, out, stream=None) -> None:
+    """corun_prefill_attention: causal attention of n sequences' queries (rows
+    as for prefill_append) over an e4m3 cache that holds their tokens."""
+    rows, nq, ldq, ldo = _attention_rows(cache, q, out)
+    ln, sr, sl = _sequences(lens, starts, slots, rows)
+    _check(load().corun_prefill_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, ln.size,
+                                          ln.ctypes.data, None if sr is None else sr.ctypes.data, sl.ctypes.data,
+                                          q.data_ptr(), ldq, out.data_ptr(), ldo, _stream(cache, stream)))
 
 
 class SchedCfg(C.Structure):

@@ -1,0 +1,18 @@
+// cache_ops.h -- a corun_kv's checks and its kernels' view of it, shared by
+// the engine and the cache operators.
+#pragma once
+#include "corun.h"
+#include "kernels.h"
+
+namespace corun {
+
+corun_status set_error(corun_status s, const char *msg);
+corun_status set_errorf(corun_status s, const char *fmt, ...);
+
+// Layout, type and sizes of a cache (the pointers are not looked at).
+corun_status check_cache(const corun_kv *kv);
+corun_status check_rope(const corun_rope *rope);
+CacheView cache_view(const corun_kv *kv);
+RopeArgs rope_args(const corun_rope &rope);
+
+}  // namespace corun

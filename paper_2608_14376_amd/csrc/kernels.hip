@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "device.h"
 #include "kernels.h"
 
 namespace corun {
@@ -31,6 +32,7 @@ namespace corun {
 // own execution (hipExtLaunchKernel) and lists them in the recorder.
 namespace {
 thread_local LaunchRecorder *t_rec = nullptr;
+}  // namespace
 
 void launch_events(hipEvent_t *start, hipEvent_t *stop)
 {
@@ -47,36 +49,8 @@ void launch_events(hipEvent_t *start, hipEvent_t *stop)
     r->used += 2;
     r->launches.push_back({*start, *stop});
 }
-}  // namespace
 
 void set_launch_recorder(LaunchRecorder *r) { t_rec = r; }
-
-#define KLAUNCH(kernel, grid, block, shmem, stream, ...)                                                   \
-    do {                                                                                                    \
-        hipEvent_t ks_, ke_;                                                                                \
-        launch_events(&ks_, &ke_);                                                                          \
-        if (ks_ != nullptr)                                                                                 \
-            hipExtLaunchKernelGGL(kernel, grid, block, shmem, stream, ks_, ke_, 0, __VA_ARGS__);            \
-        else                                                                                                \
-            hipLaunchKernelGGL(kernel, grid, block, shmem, stream, __VA_ARGS__);                            \
-    } while (0)
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float bf2f(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-
-// fp32 -> bf16, round to nearest even, NaN quieted: gfx950's v_cvt_pk_bf16_f32
-// (bit-identical, over all 2^32 inputs, to adding 0x7fff + lsb and truncating,
-// with (u >> 16) | 0x40 for NaN)
-__device__ __forceinline__ uint16_t f2bf(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-// two values in one instruction: a in the low half, b in the high half
-__device__ __forceinline__ uint32_t f2bf2(float a, float b)
-{
-    typedef float f32x2_t __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
-}
 
 // where a projection's outputs go: the address it was launched with, or the
 // one that stands in device memory now (a captured launch whose caller's
@@ -710,13 +684,6 @@ __global__ __launch_bounds__(256) void k_gemm_tiled(const uint16_t *__restrict__
 // streams weights, this is 5-20% faster.
 //
 // ---------------------------------------------------------------------------
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-__device__ __forceinline__ constexpr int vmcnt_imm(int n)
-{
-    return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8);   // vmcnt(n), expcnt and lgkmcnt not waited
-}
-
 // wait until at most `stages` stages of OPS loads each are outstanding
 // (s_waitcnt takes an immediate: dispatch the uniform stage count)
 template <int OPS, int S_>
@@ -726,13 +693,6 @@ __device__ __forceinline__ void wait_stages(int stages)
         if (stages == S_) __builtin_amdgcn_s_waitcnt(vmcnt_imm(S_ * OPS));
         else wait_stages<OPS, S_ - 1>(stages);
     }
-}
-
-__device__ __forceinline__ void lds_barrier()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 }
 
 template <int C>
