@@ -483,6 +483,358 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
 }
 
 // ---------------------------------------------------------------------------
+// Decode attention, split over the tokens.  A row of n tokens has ceil(n /
+// chunk) splits, a function of its own length, and merges them in order.
+//
+// Workgroup (kv head, split, row), four wavefronts.  The chunk is walked in
+// steps of 128 tokens whose key and value rows go global -> LDS by direct
+// 16-byte loads that cover whole rows; a wavefront takes 32 tokens of a step,
+// reads its operands into registers, and the next step's loads go out before
+// it computes.  Codes become bf16 in registers, with their scale, exactly
+// (v_cvt_scalef32_pk_bf16_fp8).
+//  * S^T = K q^T on 16x16x32 MFMA, two tiles of 16 tokens, the group's query
+//    heads in the columns; tile T's row m is token 8 (m / 4) + 4 T + m % 4,
+//    so lane l ends with head l % 16's scores of tokens 8 (l / 16) .. + 7;
+//  * the running maximum and sum of a softmax, per lane over its own tokens;
+//  * O += P V: those eight weights are the lane's A operand, in two bf16 halves
+//    hi + lo (about 16 bits), and one transposed 8-bit read gives the B operand,
+//    eight tokens of a dimension.
+// Tokens past the length: loads repeat the last token, scores are masked by
+// selection, value codes are cleared.
+// ---------------------------------------------------------------------------
+
+// Transposed LDS read of bytes (ds_read_b64_tr_b8): in each group of 16 lanes,
+// lane a + 2 q points at eight bytes (row q, columns 8 a .. 8 a + 7) and lane i
+// receives column i of rows 0 .. 7.
+__device__ __forceinline__ uint2 lds_read_tr8(const void *lds_ptr)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (lds_i32x2 *)(const __attribute__((address_space(3))) void *)lds_ptr);
+    return __builtin_bit_cast(uint2, v);
+}
+
+// Eight codes times a power of two, in bf16: exact.
+__device__ __forceinline__ bf16x8 codes_bf16(uint2 w, float scale)
+{
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    bf16x2_t h[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, false),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, false),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, true)};
+    return __builtin_bit_cast(bf16x8, h);
+}
+
+// LDS: 16-byte unit c of token t's row (KB units) at t KB + (c ^ swizzle(t)).
+// A key read's half wavefront takes one unit of the 16 tokens 8 a + 4 T + b (a,
+// b < 4), a value read's one unit of 16 consecutive tokens: each lands on the
+// 16 groups of four banks once.
+template <int KB>
+__device__ __forceinline__ int key_swz(int t)
+{
+    if constexpr (KB == 8) return (((t >> 3) & 3) << 1) | ((t >> 1) & 1);
+    else return (t >> 3) & 3;
+}
+template <int KB>
+__device__ __forceinline__ int val_swz(int t)
+{
+    if constexpr (KB == 8) return (t >> 1) & 7;
+    else return (t >> 2) & 3;
+}
+
+// Tokens that row r attends to; -1 for a length outside the launch.
+__device__ __forceinline__ int row_len(const uint8_t *valid, const int32_t *lens, int plus_one, int max_len, int r)
+{
+    if (valid != nullptr && !valid[r]) return 0;
+    const int n = lens[r];
+    return n < 0 || n > max_len - plus_one ? -1 : n + plus_one;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void k_attn8_split(const uint16_t *__restrict__ q, long long ldq,
+                                                     const uint8_t *__restrict__ valid, const int32_t *__restrict__ lens,
+                                                     int plus_one, int G, int nkv, CacheView cv, CacheLayer cl, int chunk,
+                                                     int max_splits, int max_len, float *__restrict__ ws,
+                                                     const int32_t *__restrict__ row_order)
+{
+    constexpr int ET = D / 16, KB = D / 16, STEP = 128, KU = STEP * KB, OPS = KU / 256;
+    static_assert(4 * 16 * D * 4 <= 2 * KU * 16, "wavefront partials fit the tile");
+    __shared__ __attribute__((aligned(16))) uint4 tile[2 * KU];       // keys, then values
+    __shared__ float cm[4][16], cl_[4][16];
+    __shared__ int32_t pgs[2][64];                    // paged: a step's pages, fetched one step ahead
+    __shared__ int lost;
+    typedef __attribute__((address_space(3))) void lds_void;
+
+    const int kvh = blockIdx.x, split = blockIdx.y, r = row_order != nullptr ? row_order[blockIdx.z] : blockIdx.z;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, hl = lane & 15, kg = lane >> 4;
+    const int n = row_len(valid, lens, plus_one, max_len, r);
+    const int t0 = split * chunk;
+    if (t0 >= n) return;
+    const int t1 = min(n, t0 + chunk), kmax = t1 - 1;
+    if (tid == 0) lost = 0;
+
+    // q^T (B operand of the scores): lane l supplies head l % 16, dims 32 kk + 8 (l / 16) .. + 7
+    bf16x8 qf[D / 32];
+    {
+        const uint16_t *qr = q + (size_t)r * ldq + ((size_t)kvh * G + hl) * D + kg * 8;
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk) {
+            uint4 v = {0u, 0u, 0u, 0u};
+            if (hl < G) v = *(const uint4 *)(qr + 32 * kk);
+            qf[kk] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    const float scale = 1.0f / sqrtf((float)D);
+    f32x4 oacc[ET];
+#pragma unroll
+    for (int et = 0; et < ET; ++et) oacc[et] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float mrun = -INFINITY, lrun = 0.f;
+
+    const bool paged = cv.kv.layout == 1;
+    const int ps = paged ? cv.kv.page_size : 1, last_page = kmax / ps;
+    const uint8_t *kc = (const uint8_t *)cl.k, *vc = (const uint8_t *)cl.v;
+    const size_t head0 = ((size_t)r * nkv + kvh) * cv.kv.max_seq_len;                 // contiguous: the head's first row
+    const size_t blk0 = ((size_t)r * nkv + kvh) * (cv.kv.max_seq_len >> cv.blk_shift);
+    bool bad = false;
+    auto fetch_pages = [&](int tb0, int buf) {        // wavefront 0, lane l: page tb0 / ps + l (clamped)
+        if (paged && wave == 0) {
+            const int pi = min(tb0 / ps + lane, last_page);
+            __builtin_amdgcn_global_load_lds((const void *)(cv.kv.page_table + (size_t)r * cv.kv.max_pages_per_seq + pi),
+                                             (lds_void *)&pgs[buf][0], 4, 0, 0);
+        }
+    };
+    // row of token t (real: t <= kmax) of the step at tb0, and its scale block
+    auto at = [&](int t, int first, int p0, int buf) -> Place {
+        if (!paged) return {head0 + t, blk0 + (t >> cv.blk_shift)};
+        const int i = (int)(((float)(t - first) + 0.5f) * cv.page_inv);   // (t - first) / ps: exact below 2^21
+        int page = pgs[buf][i];
+        if ((unsigned)page >= (unsigned)cv.num_pages) {
+            bad = true;
+            page = 0;
+        }
+        const int in = t - first - i * ps;
+        const size_t head = (size_t)page * nkv + kvh;
+        return {head * ps + in, head * (ps >> cv.blk_shift) + (in >> cv.blk_shift)};
+    };
+    uint32_t kb_next = 0, vb_next = 0;                // scale bytes of the lane's key rows and of its value tokens
+    auto issue = [&](int tb0, int buf) {
+        uint4 *base = tile + wave * 64;
+        const int p0 = tb0 / ps, first = paged ? p0 * ps : 0;
+#pragma unroll
+        for (int j = 0; j < OPS; ++j) {
+            const int u = j * 256 + tid, tk = u / KB, c = u % KB;
+            const size_t off = at(min(tb0 + tk, kmax), first, p0, buf).row * D;
+            __builtin_amdgcn_global_load_lds((const void *)(kc + off + 16 * (c ^ key_swz<KB>(tk))),
+                                             (lds_void *)(base + j * 256), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const void *)(vc + off + 16 * (c ^ val_swz<KB>(tk))),
+                                             (lds_void *)(base + KU + j * 256), 16, 0, 0);
+        }
+        const int tb = tb0 + 32 * wave;
+        kb_next = cl.ks[at(min(tb + 8 * (hl >> 2), kmax), first, p0, buf).blk];
+        vb_next = cl.vs[at(min(tb + 8 * kg, kmax), first, p0, buf).blk];
+    };
+
+    const int nsteps = (t1 - t0 + STEP - 1) / STEP;
+    fetch_pages(t0, 0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    lds_barrier();
+    issue(t0, 0);
+    if (nsteps > 1) fetch_pages(t0 + STEP, 1);
+    for (int i = 0; i < nsteps; ++i) {
+        const int tb0 = t0 + STEP * i, tb = tb0 + 32 * wave;
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        lds_barrier();                                // the step (and the next step's pages) are in LDS
+        const bool active = tb < t1;                  // wave-uniform: some token of the wavefront's 32 is real
+        const float ksc = __uint_as_float(kb_next << 23), vsc = __uint_as_float(vb_next << 23);
+        uint2 kr[2][D / 32], vr[ET];
+        if (active) {
+#pragma unroll
+            for (int T = 0; T < 2; ++T) {
+                const int tl = 32 * wave + 8 * (hl >> 2) + 4 * T + (hl & 3);
+#pragma unroll
+                for (int kk = 0; kk < D / 32; ++kk)
+                    kr[T][kk] = *(const uint2 *)((const char *)(tile + tl * KB + ((2 * kk + (kg >> 1)) ^ key_swz<KB>(tl))) +
+                                                 8 * (kg & 1));
+            }
+            const int tv = 32 * wave + 8 * kg + (hl >> 1);
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+                vr[et] = lds_read_tr8((const char *)(tile + KU + tv * KB + (et ^ val_swz<KB>(tv))) + 8 * (hl & 1));
+            const int nv = t1 - (tb + 8 * kg);        // the lane's real tokens, of eight
+            if (nv < 8) {
+                const unsigned long long keep = nv <= 0 ? 0ull : (1ull << (8 * nv)) - 1;
+#pragma unroll
+                for (int et = 0; et < ET; ++et) {
+                    vr[et].x &= (uint32_t)keep;
+                    vr[et].y &= (uint32_t)(keep >> 32);
+                }
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0): this wavefront's LDS reads are done
+        lds_barrier();                                // the tile is free: the next step's loads go out
+        if (i + 1 < nsteps) {
+            issue(tb0 + STEP, (i + 1) & 1);
+            if (i + 2 < nsteps) fetch_pages(tb0 + 2 * STEP, i & 1);
+        }
+        if (!active) continue;
+        f32x4 st[2];
+#pragma unroll
+        for (int T = 0; T < 2; ++T) {
+            st[T] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+                st[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16(kr[T][kk], ksc), qf[kk], st[T], 0, 0, 0);
+        }
+        float mt = -INFINITY;
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float sv = (tb + 8 * kg + 4 * T + e < t1) ? st[T][e] * scale : -INFINITY;
+                st[T][e] = sv;
+                mt = fmaxf(mt, sv);
+            }
+        mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float mnew = fmaxf(mrun, mt);           // every 32-token block has a real token (NaN scores aside)
+        const float alpha = mnew == mrun ? 1.f : __expf(mrun - mnew);   // also where both are -inf (NaN scores only)
+        const float moff = mnew == -INFINITY ? 0.f : mnew;
+        uint32_t hi[4], lo[4];
+        float ls = 0.f;
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const float a = __expf(st[T][e] - moff), b = __expf(st[T][e + 1] - moff);
+                ls += a;
+                ls += b;
+                const uint32_t w = f2bf2(a, b);
+                hi[2 * T + e / 2] = w;
+                lo[2 * T + e / 2] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+            }
+        lrun = lrun * alpha + ls;
+        mrun = mnew;
+        if (__ballot(alpha != 1.f)) {                 // lane l's accumulators belong to heads 4 (l / 16) + e
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float ae = __shfl(alpha, 4 * kg + e, 64);
+#pragma unroll
+                for (int et = 0; et < ET; ++et) oacc[et][e] *= ae;
+            }
+        }
+        const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+        for (int et = 0; et < ET; ++et) {
+            const bf16x8 vf = codes_bf16(vr[et], vsc);
+            oacc[et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vf, oacc[et], 0, 0, 0);
+            oacc[et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vf, oacc[et], 0, 0, 0);
+        }
+    }
+    lrun += __shfl_xor(lrun, 16, 64);
+    lrun += __shfl_xor(lrun, 32, 64);
+
+    // the four wavefronts in order, through the idle tile
+    lds_barrier();
+    if (bad) lost = 1;
+    float *ca = reinterpret_cast<float *>(tile);      // [4][G D]
+    if (lane < 16) {
+        cm[wave][lane] = mrun;
+        cl_[wave][lane] = lrun;
+    }
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int g = 4 * kg + e;
+            if (g < G) ca[(wave * G + g) * D + 16 * et + hl] = oacc[et][e];
+        }
+    __syncthreads();
+    float *o = ws + (((size_t)r * nkv + kvh) * max_splits + split) * (G * (D + 2));
+    for (int idx = tid; idx < G * D; idx += 256) {
+        const int g = idx / D;
+        float M = cm[0][g];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) M = fmaxf(M, cm[w][g]);
+        const float off = M == -INFINITY ? 0.f : M;   // NaN scores only
+        float L = 0.f, A = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __expf(cm[w][g] - off);   // a wavefront without tokens: exp(-inf) = 0
+            L += cl_[w][g] * f;
+            A += ca[w * G * D + idx] * f;
+        }
+        o[2 * G + idx] = A;
+        if (idx % D == 0) {
+            o[g] = lost ? QNAN : M;
+            o[G + g] = L;
+        }
+    }
+}
+
+// Merge: 256 / D query heads of one row to a workgroup, one thread to a
+// dimension; a head's first wavefront turns its splits' maxima into weights and
+// sums, every thread folds its dimension over the splits in order.
+template <int D>
+__global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ ws, const uint8_t *__restrict__ valid,
+                                                     const int32_t *__restrict__ lens, int plus_one, int nq, int nkv,
+                                                     int chunk, int max_splits, int max_len, uint16_t *__restrict__ out,
+                                                     long long ldo)
+{
+    constexpr int HB = 256 / D, PF = 16;
+    extern __shared__ float fs[];                     // [HB][max_splits] weights
+    __shared__ float total[HB];
+    const int hb = threadIdx.x / D, dd = threadIdx.x % D, lane = threadIdx.x & 63;
+    const int h = blockIdx.x * HB + hb, r = blockIdx.y, G = nq / nkv;
+    const int n = row_len(valid, lens, plus_one, max_len, r);
+    uint16_t *o = out + (size_t)r * ldo + (size_t)h * D + dd;
+    if (n <= 0) {
+        if (h < nq) *o = n < 0 ? (uint16_t)0x7fc0 : (uint16_t)0;
+        return;
+    }
+    const int ns = (n + chunk - 1) / chunk, kvh = min(h, nq - 1) / G, g = min(h, nq - 1) % G;
+    const size_t stride = (size_t)G * (D + 2);
+    const float *base = ws + ((size_t)r * nkv + kvh) * max_splits * stride;
+    const float *a = base + 2 * G + g * D + dd;
+    float v[PF];
+#pragma unroll
+    for (int u = 0; u < PF; ++u) v[u] = u < ns ? a[u * stride] : 0.f;
+    float *f = fs + hb * max_splits;
+    if (dd < 64) {
+        float M = -INFINITY, L = 0.f;
+        bool nan = false;
+        for (int sp = lane; sp < ns; sp += 64) {
+            const float m = base[sp * stride + g];
+            nan |= m != m;
+            f[sp] = m;
+            M = fmaxf(M, m);
+        }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+        const float off_ = M == -INFINITY ? 0.f : M;
+        for (int sp = lane; sp < ns; sp += 64) {
+            const float w = __expf(f[sp] - off_);
+            f[sp] = w;
+            L += base[sp * stride + G + g] * w;
+        }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
+        if (lane == 0) total[hb] = L;
+    }
+    __syncthreads();
+    float acc = 0.f;
+    for (int sp = 0; sp < ns; sp += PF) {
+        if (sp > 0)
+#pragma unroll
+            for (int u = 0; u < PF; ++u) v[u] = sp + u < ns ? a[(size_t)(sp + u) * stride] : 0.f;
+#pragma unroll
+        for (int u = 0; u < PF; ++u)
+            if (sp + u < ns) acc += v[u] * f[sp + u];
+    }
+    if (h < nq) *o = f2bf(acc / total[hb]);
+}
+
+// ---------------------------------------------------------------------------
 // Attention, one wavefront per (query, query head): 64 keys at a time, a key
 // to a lane for the scores, then two dimensions to a lane for the values.
 // ---------------------------------------------------------------------------
@@ -540,24 +892,6 @@ __device__ __forceinline__ void attend(const uint16_t *q, int n, int kvh, int nk
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void k_attend_rows(const uint16_t *q, long long ldq, int rows, const uint8_t *valid,
-                                                     const int32_t *lens, int plus_one, int nq, int nkv, CacheView cv,
-                                                     CacheLayer cl, int max_len, uint16_t *out, long long ldo)
-{
-    const int u = blockIdx.x * 4 + (threadIdx.x >> 6), r = u / nq, h = u % nq;
-    if (r >= rows) return;
-    uint16_t *o = out + (size_t)r * ldo + (size_t)h * D;
-    const bool live = valid == nullptr || valid[r];
-    int n = live ? lens[r] : 0;
-    bool bad = n < 0;
-    if (live && !bad) {
-        bad = n > max_len - plus_one;
-        n += plus_one;
-    }
-    attend<D>(q + (size_t)r * ldq + (size_t)h * D, live ? n : 0, h / (nq / nkv), nkv, r, cv, cl, o, bad);
-}
-
-template <int D>
 __global__ __launch_bounds__(256) void k_attend_seqs(const uint16_t *q, long long ldq, SeqTable seq, int nq, int nkv,
                                                      CacheView cv, CacheLayer cl, uint16_t *out, long long ldo)
 {
@@ -607,16 +941,60 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
     return hipGetLastError();
 }
 
+// The smallest chunk from 128 tokens up to 1024 for which rows of max_len have
+// at most 2048 workgroups, four rounds of two to a CU; more where a row would
+// have over 512 splits to merge.
+int attn8_chunk(int rows, int nkv, int max_len)
+{
+    long long chunk = 128;
+    while (chunk < 1024 && (long long)rows * nkv * ((max_len + chunk - 1) / chunk) > 2048) chunk *= 2;
+    while ((max_len + chunk - 1) / chunk > 512) chunk *= 2;
+    return (int)std::min<long long>(chunk, 1 << 30);
+}
+
+size_t attn8_workspace(int rows, int nq, int nkv, int d, int max_len)
+{
+    const int chunk = attn8_chunk(rows, nkv, max_len);
+    return (size_t)rows * nq * ((max_len + (long long)chunk - 1) / chunk) * (d + 2);
+}
+
 hipError_t launch_attn8_rows(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
                              int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                             uint16_t *out, long long ldo, hipStream_t st)
+                             float *ws, uint16_t *out, long long ldo, hipStream_t st, const int32_t *row_order)
 {
-    const dim3 grid((unsigned)(((long long)rows * nq + 3) / 4));
+    hipError_t e = launch_attn8_split(q, ldq, rows, valid, lens, plus_one, nq, nkv, d, cv, cl, max_len, ws, st, row_order);
+    return e != hipSuccess ? e : launch_attn8_merge(ws, rows, valid, lens, plus_one, nq, nkv, d, max_len, out, ldo, st);
+}
+
+hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
+                              int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
+                              float *ws, hipStream_t st, const int32_t *row_order)
+{
+    const int chunk = attn8_chunk(rows, nkv, max_len), splits = (int)((max_len + (long long)chunk - 1) / chunk), G = nq / nkv;
+    const dim3 grid(nkv, splits, rows);
     if (d == 128)
-        KLAUNCH((k_attend_rows<128>), grid, dim3(256), 0, st, q, ldq, rows, valid, lens, plus_one, nq, nkv, cv, cl, max_len,
+        KLAUNCH((k_attn8_split<128>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits,
+                max_len, ws, row_order);
+    else if (d == 64)
+        KLAUNCH((k_attn8_split<64>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits,
+                max_len, ws, row_order);
+    else
+        return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, const int32_t *lens, int plus_one, int nq,
+                              int nkv, int d, int max_len, uint16_t *out, long long ldo, hipStream_t st)
+{
+    const int chunk = attn8_chunk(rows, nkv, max_len), splits = (int)((max_len + (long long)chunk - 1) / chunk);
+    const int hb = 256 / d;
+    const dim3 grid((nq + hb - 1) / hb, rows);
+    const size_t shm = sizeof(float) * hb * splits;
+    if (d == 128)
+        KLAUNCH((k_attn8_merge<128>), grid, dim3(256), shm, st, ws, valid, lens, plus_one, nq, nkv, chunk, splits, max_len,
                 out, ldo);
     else if (d == 64)
-        KLAUNCH((k_attend_rows<64>), grid, dim3(256), 0, st, q, ldq, rows, valid, lens, plus_one, nq, nkv, cv, cl, max_len,
+        KLAUNCH((k_attn8_merge<64>), grid, dim3(256), shm, st, ws, valid, lens, plus_one, nq, nkv, chunk, splits, max_len,
                 out, ldo);
     else
         return hipErrorInvalidValue;

@@ -280,7 +280,7 @@ extern "C" int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t 
     TRY(check_step_rows(kv, rows));
     if (max_len < 0 || max_len > cache_view(kv).cap)
         return set_errorf(CORUN_E_CAPACITY, "max_len %d outside [0, %d]", max_len, cache_view(kv).cap);
-    return 0;
+    return (int64_t)(sizeof(float) * attn8_workspace(rows, n_heads, n_kv_heads, head_dim, longest(kv, max_len)));
 }
 
 extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
@@ -299,7 +299,7 @@ extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer
     if (ws_bytes < need)
         return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
     return launched(launch_attn8_rows((const uint16_t *)q, ld_q, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim,
-                                      cache_view(kv), cl, longest(kv, max_len), (uint16_t *)out, ld_out,
+                                      cache_view(kv), cl, longest(kv, max_len), (float *)ws, (uint16_t *)out, ld_out,
                                       (hipStream_t)stream));
 }
 
