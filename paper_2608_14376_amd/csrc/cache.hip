@@ -835,73 +835,356 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 }
 
 // ---------------------------------------------------------------------------
-// Attention, one wavefront per (query, query head): 64 keys at a time, a key
-// to a lane for the scores, then two dimensions to a lane for the values.
+// Prefill attention, causal, no split: keys in tiles of 64 in order, online
+// softmax in base 2.
+//
+// A unit is 32 queries of one query head; a workgroup of eight wavefronts takes
+// eight units of one kv head in [query block][head] order, latest first, one to
+// a wavefront, on shared key and value tiles.  A tile's codes are read into
+// registers one tile ahead, and become 16-bit LDS rows once for all eight
+// wavefronts: keys in bf16 with their scale (exact), values in fp16 under a
+// common exponent `top`, the largest scale of the values so far (exact down to
+// 2^-15 of it; what is smaller yet keeps an absolute error of 2^-25 of that
+// scale).  fp16 weights keep 11 bits where bf16 would keep 8.
+//  * S^T = K Q^T on v_mfma_f32_32x32x16_bf16, two 32 x 32 tiles, key rows
+//    permuted (pf_key_of_row) so that lane l ends with eight consecutive keys
+//    16 s + 8 (l / 32) .. + 7 of each step s of query l % 32: the P^T operand of
+//  * O^T += V^T P^T on v_mfma_f32_32x32x16_f16, V^T by transposed LDS reads.
+// Weights are 2^(s - max + P_UP) and values code 2^(e - top + V_UP): both stay
+// normal fp16 numbers where it matters; the row sum carries P_UP too, and the
+// output takes 2^(top - V_UP) back.  Keys past the sequence, future ones and
+// those of a bad page are masked by selection (bad pages: NaN keys, so that a
+// query that sees one becomes NaN).  A NaN among the value codes would reach
+// queries that do not see it (0 NaN): value tiles hold zeros in their place and a
+// bit for each, and from the first one on the queries' sums are set to NaN by
+// the bits of the keys that they see.
 // ---------------------------------------------------------------------------
-template <int D>
-__device__ __forceinline__ void attend(const uint16_t *q, int n, int kvh, int nkv, int slot, const CacheView &cv,
-                                       const CacheLayer &cl, uint16_t *out, bool bad)
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr int P_UP = 14, V_UP = 6;
+
+// Sixteen codes times a power of two, as 32 bytes of bf16 or fp16.
+template <bool F16>
+__device__ __forceinline__ void codes_16(uint4 w, float scale, uint4 &lo, uint4 &hi)
 {
-    const int lane = threadIdx.x & 63;
-    constexpr int E = D / 64;
-    float qv[D];
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    uint32_t o[8];
+    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < D; ++i) qv[i] = bf2f(q[i]);
-    const float scale = 1.0f / sqrtf((float)D);
-    float m = -INFINITY, l = 0.f, acc[E];
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int b = 0; b < n && !bad; b += 64) {
-        const int t = min(b + lane, n - 1);
-        int page = 0;
-        if (cv.kv.layout == 1) page = page_of(cv, slot, t);
-        const bool lost = page < 0;
-        const Place pl = place(cv, nkv, kvh, slot, max(page, 0), t);
-        const uint8_t *k = (const uint8_t *)cl.k + pl.row * D;
-        float sc = 0.f;
-#pragma unroll
-        for (int i = 0; i < D; i += 4) {
-            const uint32_t w = *(const uint32_t *)(k + i);
-            sc += qv[i] * __builtin_amdgcn_cvt_f32_fp8(w, 0);
-            sc += qv[i + 1] * __builtin_amdgcn_cvt_f32_fp8(w, 1);
-            sc += qv[i + 2] * __builtin_amdgcn_cvt_f32_fp8(w, 2);
-            sc += qv[i + 3] * __builtin_amdgcn_cvt_f32_fp8(w, 3);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F16) {
+            o[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], scale, false));
+            o[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], scale, true));
+        } else {
+            o[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], scale, false));
+            o[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], scale, true));
         }
-        sc *= exp2_int((int)cl.ks[pl.blk] - 127) * scale;
-        if (b + lane >= n) sc = -INFINITY;
-        float mt = sc;
-        for (int o = 32; o; o >>= 1) mt = fmaxf(mt, __shfl_xor(mt, o, 64));
-        const float mn = fmaxf(m, mt);
-        const float al = __expf(m - mn), pe = b + lane < n ? __expf(sc - mn) : 0.f;
-        float ps = pe;
-        for (int o = 32; o; o >>= 1) ps += __shfl_xor(ps, o, 64);
-        l = l * al + ps;
-        m = mn;
-        for (int e = 0; e < E; ++e) acc[e] *= al;
-        const float vsc = exp2_int((int)cl.vs[pl.blk] - 127);
-        for (int i = 0; i < min(64, n - b); ++i) {
-            const float pi = __shfl(pe, i, 64) * __shfl(vsc, i, 64);
-            const size_t row = __shfl((unsigned long long)pl.row, i, 64);
-            for (int e = 0; e < E; ++e) {
-                const uint32_t c = ((const uint8_t *)cl.v)[row * D + E * lane + e];
-                acc[e] += pi * __builtin_amdgcn_cvt_f32_fp8(c, 0);
-            }
-        }
-        bad = __ballot(lost) != 0ull;
     }
-    for (int e = 0; e < E; ++e) out[E * lane + e] = f2bf(bad ? QNAN : n > 0 ? acc[e] / l : 0.f);
+    lo = (uint4){o[0], o[1], o[2], o[3]};
+    hi = (uint4){o[4], o[5], o[6], o[7]};
 }
 
+// Bit 7 of a byte of the result: that code is NaN (0x7f or 0xff).
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 template <int D>
-__global__ __launch_bounds__(256) void k_attend_seqs(const uint16_t *q, long long ldq, SeqTable seq, int nq, int nkv,
-                                                     CacheView cv, CacheLayer cl, uint16_t *out, long long ldo)
+__global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq, int G,
+                                                       int nkv, CacheView cv, CacheLayer cl, uint16_t *__restrict__ out,
+                                                       long long ldo)
 {
-    int i = 0;
-    while (i + 1 < seq.n && seq.unit0[i + 1] <= (int)blockIdx.x) ++i;
-    const int u = ((int)blockIdx.x - seq.unit0[i]) * 4 + (threadIdx.x >> 6), t = u / nq, h = u % nq;
-    if (t >= seq.len[i]) return;
-    const size_t r = (size_t)seq.row0[i] + t;
-    attend<D>(q + r * ldq + (size_t)h * D, seq.start[i] + t + 1, h / (nq / nkv), nkv, seq.slot[i], cv, cl,
-              out + r * ldo + (size_t)h * D, false);
+    constexpr int NW = 8, QB = 32, BKT = 64;          // wavefronts; queries of a unit; keys of a tile
+    constexpr int DT = D / 32, KS = D / 16, KCH = D / 8, KB = D / 16;
+    constexpr int HALF = BKT * KCH, STAGE = 2 * HALF; // 16-byte units of a tile's 16-bit keys (then values)
+    constexpr int OPITCH = D + 8;
+    static_assert(NW * QB * OPITCH * 2 <= 2 * STAGE * 16 + NW * QB * 16, "output staging fits");
+    __shared__ __attribute__((aligned(16))) uint4 ring[2 * STAGE + NW * QB];
+    __shared__ __attribute__((aligned(16))) uint16_t nan_bits[2][BKT][KB];         // one bit for each value code of a tile's rows
+    __shared__ int has_nan;
+
+    const int kvh = blockIdx.x % nkv;
+    int si = 0;
+    while (si + 1 < seq.n && seq.unit0[si + 1] <= (int)(blockIdx.x / nkv)) ++si;
+    const int grp = (int)(blockIdx.x / nkv) - seq.unit0[si];
+    const int n = seq.len[si], p0 = seq.start[si], slot = seq.slot[si], Lk = p0 + n;
+    q += (size_t)seq.row0[si] * ldq;
+    out += (size_t)seq.row0[si] * ldo;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r32 = lane & 31, h = lane >> 5;
+    const int units = (n + QB - 1) / QB * G;
+    const int u = units - 1 - (grp * NW + wave);
+    const bool active = u >= 0;
+    const int qb = active ? u / G : 0, g = active ? u % G : 0, hq = kvh * G + g, q0 = qb * QB;
+    const int wg_last_q = p0 + min(n, ((units - 1 - grp * NW) / G + 1) * QB) - 1;
+    const int my_last_q = active ? p0 + min(n, q0 + QB) - 1 : -1;
+    const int ntiles = __builtin_amdgcn_readfirstlane(wg_last_q / BKT + 1);
+
+    // Loads: thread t takes 16-byte unit c of key row `row` and, for heads of
+    // 128, of the value row; for heads of 64 wavefronts 4 .. 7 take the values.
+    // A wavefront's rows are in one 16-token group of the tile, `sub`.
+    constexpr bool BOTH = D == 128;
+    const int row = BOTH ? tid >> 3 : (tid & 255) >> 2, c = BOTH ? tid & 7 : tid & 3;
+    const bool has_k = BOTH || wave < 4, has_v = BOTH || wave >= 4;
+    const int sub = BOTH ? wave >> 1 : wave & 3;
+    const bool paged = cv.kv.layout == 1;
+    const int ps = cv.kv.page_size;
+    const int32_t *pt = paged ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
+    const size_t head0 = ((size_t)slot * nkv + kvh) * cv.kv.max_seq_len;
+    const size_t blk0 = ((size_t)slot * nkv + kvh) * (cv.kv.max_seq_len >> cv.blk_shift);
+    const uint8_t *kc = (const uint8_t *)cl.k, *vc = (const uint8_t *)cl.v;
+    // this thread's key of a tile, and the first key of the 16-token group whose
+    // scale bytes this lane loads (lanes 0 .. 3 values', 4 .. 7 keys')
+    auto key_at = [&](int k0) { return min(k0 + row, Lk - 1); };
+    auto grp_at = [&](int k0) { return min(k0 + 16 * (lane & 3), Lk - 1); };
+    int pg_row = 0, pg_grp = 0;                       // pages of the next tile to be loaded
+    auto fetch_pages = [&](int k0) {
+        if (!paged) return;
+        pg_row = pt[key_at(k0) / ps];
+        pg_grp = pt[grp_at(k0) / ps];
+    };
+    uint4 kraw, vraw;
+    uint32_t sc = 0;
+    bool kbad = false;                                // the loaded row's page is none
+    kraw = vraw = (uint4){0u, 0u, 0u, 0u};
+    auto load = [&](int k0) {
+        size_t off, blk;
+        const int t = key_at(k0), tg = grp_at(k0);
+        if (paged) {
+            kbad = (unsigned)pg_row >= (unsigned)cv.num_pages;
+            const size_t hr = (size_t)(kbad ? 0 : pg_row) * nkv + kvh;
+            const size_t hg = (size_t)((unsigned)pg_grp >= (unsigned)cv.num_pages ? 0 : pg_grp) * nkv + kvh;
+            off = hr * ps + t % ps;
+            blk = hg * (ps >> cv.blk_shift) + ((tg % ps) >> cv.blk_shift);
+        } else {
+            off = head0 + t;
+            blk = blk0 + (tg >> cv.blk_shift);
+        }
+        if (has_k) kraw = *(const uint4 *)(kc + off * D + 16 * c);
+        if (has_v) vraw = *(const uint4 *)(vc + off * D + 16 * c);
+        sc = (lane & 4 ? cl.ks : cl.vs)[blk];
+    };
+    // The loaded tile (keys from k0) to LDS buffer b; `top` becomes the common
+    // exponent byte of its values.
+    auto store = [&](int k0, int b, int &top) {
+        const int v0 = __builtin_amdgcn_readlane(sc, 0), v1 = __builtin_amdgcn_readlane(sc, 1);
+        const int v2 = __builtin_amdgcn_readlane(sc, 2), v3 = __builtin_amdgcn_readlane(sc, 3);
+        top = max(top, max(max(v0, v1), max(v2, v3)));
+        const int kb = __builtin_amdgcn_readlane(sc, 4 + sub), vb = __builtin_amdgcn_readlane(sc, sub);
+        uint4 *K = ring + b * STAGE, *V = K + HALF;
+        uint4 lo, hi;
+        if (has_k) {
+            codes_16<false>(kraw, __uint_as_float((uint32_t)kb << 23), lo, hi);
+            if (kbad) lo = hi = (uint4){0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+            K[pf_swz<KCH>(row, 2 * c)] = lo;
+            K[pf_swz<KCH>(row, 2 * c + 1)] = hi;
+        }
+        if (has_v) {
+            const bool drop = k0 + row >= Lk || kbad;
+            if (drop) vraw = (uint4){0u, 0u, 0u, 0u};
+            const uint32_t nx = nan_codes(vraw.x), ny = nan_codes(vraw.y), nz = nan_codes(vraw.z), nw = nan_codes(vraw.w);
+            uint32_t bits = 0u;
+            if (nx | ny | nz | nw) {
+                has_nan = 1;
+                const uint32_t n4[4] = {nx, ny, nz, nw};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits |= ((((n4[i] >> 7) * 0x10204080u) >> 28) & 15u) << (4 * i);
+                vraw.x &= ~((nx >> 7) * 255u);
+                vraw.y &= ~((ny >> 7) * 255u);
+                vraw.z &= ~((nz >> 7) * 255u);
+                vraw.w &= ~((nw >> 7) * 255u);
+            }
+            nan_bits[b][row][c] = (uint16_t)bits;
+            const int e = max(vb - top + V_UP, -60);
+            codes_16<true>(vraw, exp2_int(e), lo, hi);
+            // odd rows write their second unit first: neighbouring rows' units lie in the same banks
+            const int odd = row & 1, s = vtile_swz<KCH>(row);
+            V[row * KCH + ((2 * c + odd) ^ s)] = odd ? hi : lo;
+            V[row * KCH + ((2 * c + 1 - odd) ^ s)] = odd ? lo : hi;
+        }
+    };
+
+    // Q^T operand: lane l supplies query q0 + l % 32, dims 16 s + 8 (l / 32) .. + 7
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        uint4 v = {0u, 0u, 0u, 0u};
+        if (active && q0 + r32 < n) v = *(const uint4 *)(q + (size_t)(q0 + r32) * ldq + (size_t)hq * D + 16 * ks + 8 * h);
+        qf[ks] = __builtin_bit_cast(bf16x8, v);
+    }
+    f32x16 acc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
+    float mrow = -INFINITY, lpart = 0.f;
+    const float scale2 = 1.4426950408889634f / sqrtf((float)D);   // log2(e) / sqrt(d)
+    const int qq = p0 + q0 + r32;
+
+    if (tid == 0) has_nan = 0;
+    int top_next = 0, top_acc = 0;
+    fetch_pages(0);
+    load(0);
+    fetch_pages(BKT);
+    __syncthreads();
+    store(0, 0, top_next);
+    int top = top_next;
+    top_acc = top;
+    load(min(BKT, (ntiles - 1) * BKT));
+    fetch_pages(2 * BKT);
+    for (int i = 0; i < ntiles; ++i) {
+        const int k0 = i * BKT, b = i & 1;
+        __syncthreads();                              // tile i is in LDS, and tile i - 1's buffer is free
+        top = top_next;
+        if (i + 1 < ntiles) {
+            store(k0 + BKT, b ^ 1, top_next);
+            if (i + 2 < ntiles) {
+                load(k0 + 2 * BKT);
+                fetch_pages(k0 + 3 * BKT);
+            }
+        }
+        if (k0 > my_last_q) continue;                 // wave-uniform: the whole tile is in this unit's future
+
+        const uint4 *Kt = ring + b * STAGE, *Vt = Kt + HALF;
+        f32x16 st[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) st[kt][j] = 0.f;
+        // key operands two steps ahead of their products, in a fixed order
+        constexpr int KD = 2;
+        bf16x8 kf[KD + 1][2];
+        auto kread = [&](int ks) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+                kf[ks % (KD + 1)][kt] =
+                    __builtin_bit_cast(bf16x8, Kt[pf_swz<KCH>(32 * kt + pf_key_of_row(r32), 2 * ks + h)]);
+        };
+#pragma unroll
+        for (int ks = 0; ks < KD; ++ks) kread(ks);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + KD < KS) kread(ks + KD);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+                st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks % (KD + 1)][kt], qf[ks], st[kt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // lane: keys k0 + 32 kt + 16 (j / 8) + 8 h + j % 8 of query qq
+        const bool masked = k0 + BKT - 1 > p0 + q0 || k0 + BKT > Lk;
+        float mt = -INFINITY;
+        if (masked) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = k0 + 32 * kt + 16 * (j >> 3) + 8 * h + (j & 7);
+                    const float sv = (key <= qq && key < Lk) ? st[kt][j] : -INFINITY;
+                    st[kt][j] = sv;
+                    mt = fmaxf(mt, sv);
+                }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
+        }
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float mnew = fmaxf(mrow, mt * scale2);
+        const float moff = (mnew == -INFINITY ? 0.f : mnew) - P_UP;
+        float ls = 0.f;
+        f16x8 pf[4];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f16x2 w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e], scale2, -moff));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e + 1], scale2, -moff));
+                    ls += x + y;
+                    w[e] = __builtin_convertvector((f32x2_t){x, y}, f16x2);
+                }
+                pf[2 * kt + half] = __builtin_bit_cast(f16x8, w);
+            }
+        if (__ballot(mnew != mrow) || top != top_acc) {
+            const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
+            const float fall = exp2_int(max(top_acc - top, -126));
+            lpart *= alpha;
+            const float a = alpha * fall;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[dt][j] *= a;
+            top_acc = top;
+        }
+        lpart += ls;
+        mrow = mnew;
+        // operand f: 16-key step f / DT, output tile f % DT; lane l takes
+        // dimension 32 dt + l % 32 of keys 16 s + 8 h .. + 7 by two transposed reads
+        const int a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
+        constexpr int VD = 3;                         // read three ahead of their products
+        f16x8 vf[VD + 1];
+        auto vread = [&](int f) {
+            uint2 part[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int key = 16 * (f / DT) + 8 * h + 4 * r + qv;
+                const int cc = 4 * (f % DT) + 2 * half16 + (a4 >> 1);
+                part[r] = lds_read_tr16(reinterpret_cast<const char *>(Vt + key * KCH + (cc ^ vtile_swz<KCH>(key))) + 8 * (a4 & 1));
+            }
+            vf[f % (VD + 1)] = __builtin_bit_cast(f16x8, (uint4){part[0].x, part[0].y, part[1].x, part[1].y});
+        };
+#pragma unroll
+        for (int f = 0; f < VD; ++f) vread(f);
+#pragma unroll
+        for (int f = 0; f < 4 * DT; ++f) {
+            if (f + VD < 4 * DT) vread(f + VD);
+            __builtin_amdgcn_sched_barrier(0);
+            acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[f % (VD + 1)], pf[f / DT], acc[f % DT], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (has_nan) {   // once a tile of this workgroup had one; a tile without changes nothing here
+            uint32_t hit[DT];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) hit[dt] = 0u;
+#pragma unroll 1
+            for (int key = 0; key < BKT; ++key) {
+                if (k0 + key > qq) break;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) hit[dt] |= ((const uint32_t *)nan_bits[b][key])[dt];
+            }
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (hit[dt] >> (8 * (j >> 2) + 4 * h + (j & 3)) & 1u) acc[dt][j] = QNAN;
+        }
+    }
+    __syncthreads();                                  // every wavefront is done with the tiles
+
+    // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]; through LDS for whole rows
+    uint16_t *ost = (uint16_t *)ring + (size_t)wave * QB * OPITCH;
+    {
+        float L = lpart;
+        L += __shfl_xor(L, 32, 64);
+        const float inv = 1.0f / L;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                ost[r32 * OPITCH + 32 * dt + 8 * (j >> 2) + 4 * h + (j & 3)] =
+                    f2bf(__builtin_amdgcn_ldexpf(acc[dt][j] * inv, top_acc - 127 - V_UP));
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wavefront's staging writes are done
+    if (!active) return;
+#pragma unroll 4
+    for (int it = lane; it < QB * (D / 8); it += 64) {
+        const int qr = it / (D / 8), c8 = it % (D / 8), qo = q0 + qr;
+        if (qo < n) *(uint4 *)(out + (size_t)qo * ldo + (size_t)hq * D + 8 * c8) = *(const uint4 *)(ost + qr * OPITCH + 8 * c8);
+    }
 }
 
 }  // namespace
@@ -1004,14 +1287,15 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
 hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
                              const CacheLayer &cl, uint16_t *out, long long ldo, hipStream_t st)
 {
-    int units = 0;
+    const int G = nq / nkv;
+    int groups = 0;
     for (int i = 0; i < seq.n; ++i) {
-        seq.unit0[i] = units;
-        units += (seq.len[i] * nq + 3) / 4;
+        seq.unit0[i] = groups;
+        groups += ((seq.len[i] + 31) / 32 * G + 7) / 8;
     }
-    const dim3 grid(units);
-    if (d == 128) KLAUNCH((k_attend_seqs<128>), grid, dim3(256), 0, st, q, ldq, seq, nq, nkv, cv, cl, out, ldo);
-    else if (d == 64) KLAUNCH((k_attend_seqs<64>), grid, dim3(256), 0, st, q, ldq, seq, nq, nkv, cv, cl, out, ldo);
+    const dim3 grid((unsigned)groups * nkv);
+    if (d == 128) KLAUNCH((k_attn8_prefill<128>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo);
+    else if (d == 64) KLAUNCH((k_attn8_prefill<64>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }

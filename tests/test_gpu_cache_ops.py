@@ -454,6 +454,32 @@ def test_prefill_attention_sequences_do_not_touch_each_other():
         assert same(alone, out[row:row + n])
 
 
+@pytest.mark.parametrize("d,page", [(128, 0), (64, 16)])
+def test_prefill_attention_nan_reaches_only_those_who_see_it(d, page):
+    """NaN keys make the queries from there on NaN; NaN values do so in their own dimension."""
+    nkv, G, blk, cap = 2, 2, 16, 256
+    hc = HostCache(nkv, d, 2, cap, blk, page, seed=55)
+    for slot, h, t, e, what in [(0, 0, 40, 3, "v"), (0, 0, 63, 17, "v"), (0, 0, 64, d - 1, "v"), (0, 1, 129, 0, "v"),
+                                (0, 1, 170, 5, "k"), (1, 0, 99, 31, "v"), (1, 1, 0, d // 2, "v")]:
+        a, b = hc.at(slot, t)
+        (hc.v if what == "v" else hc.k)[a, h, b, e] = 0xFF if t % 2 else 0x7F
+    cache = hc.device_cache(corun)
+    lens, starts, slots = [200, 61], [0, 40], [0, 1]
+    x, q = rows_of(261, nkv * G, d, 56)
+    out = run_prefill(cache, q, lens, starts, slots)
+    for row, n, p0, slot in seqs_of(lens, starts, slots):
+        k, v = hc.values(slot, p0 + n)
+        for t in range(n):
+            o, pv, size = ref.attention(x[row + t].double().view(-1, d), torch.nan_to_num(k), torch.nan_to_num(v), p0 + t + 1)
+            o = o.view(nkv, G, d)
+            seen = torch.isnan(v[:, : p0 + t + 1]).any(1)[:, None, :] | torch.isnan(k[:, : p0 + t + 1]).any(-1).any(-1)[:, None, None]
+            got = out[row + t].double().view(nkv, G, d)
+            assert torch.equal(torch.isnan(got), seen.expand_as(got)), (slot, t)
+            tol = ref.attention_bound(o, pv.view(nkv, G, d), size, d, p0 + t + 1, 2.0**-8)
+            fine = ~seen.expand_as(got)
+            assert ((got - o).abs() <= tol)[fine].all(), (slot, t)
+
+
 def test_prefill_attention_bad_pages():
     d, nkv, G, blk, page, cap = 128, 1, 2, 16, 16, 256
     hc = HostCache(nkv, d, 2, cap, blk, page, seed=60)
