@@ -974,13 +974,16 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         uint4 lo, hi;
         if (has_k) {
             codes_16<false>(kraw, __uint_as_float((uint32_t)kb << 23), lo, hi);
-            if (kbad) lo = hi = (uint4){0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+            const uint32_t nan = kbad ? 0x7fc07fc0u : 0u;    // or'ed in: still NaN
+            lo = (uint4){lo.x | nan, lo.y | nan, lo.z | nan, lo.w | nan};
+            hi = (uint4){hi.x | nan, hi.y | nan, hi.z | nan, hi.w | nan};
             K[pf_swz<KCH>(row, 2 * c)] = lo;
             K[pf_swz<KCH>(row, 2 * c + 1)] = hi;
         }
         if (has_v) {
             const bool drop = k0 + row >= Lk || kbad;
-            if (drop) vraw = (uint4){0u, 0u, 0u, 0u};
+            const uint32_t use = drop ? 0u : 0xffffffffu;
+            vraw = (uint4){vraw.x & use, vraw.y & use, vraw.z & use, vraw.w & use};
             const uint32_t nx = nan_codes(vraw.x), ny = nan_codes(vraw.y), nz = nan_codes(vraw.z), nw = nan_codes(vraw.w);
             uint32_t bits = 0u;
             if (nx | ny | nz | nw) {
@@ -998,8 +1001,10 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
             codes_16<true>(vraw, exp2_int(e), lo, hi);
             // odd rows write their second unit first: neighbouring rows' units lie in the same banks
             const int odd = row & 1, s = vtile_swz<KCH>(row);
-            V[row * KCH + ((2 * c + odd) ^ s)] = odd ? hi : lo;
-            V[row * KCH + ((2 * c + 1 - odd) ^ s)] = odd ? lo : hi;
+            V[row * KCH + ((2 * c + odd) ^ s)] =
+                (uint4){odd ? hi.x : lo.x, odd ? hi.y : lo.y, odd ? hi.z : lo.z, odd ? hi.w : lo.w};
+            V[row * KCH + ((2 * c + 1 - odd) ^ s)] =
+                (uint4){odd ? lo.x : hi.x, odd ? lo.y : hi.y, odd ? lo.z : hi.z, odd ? lo.w : hi.w};
         }
     };
 
