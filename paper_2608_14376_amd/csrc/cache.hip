@@ -850,9 +850,11 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 //    permuted (pf_key_of_row) so that lane l ends with eight consecutive keys
 //    16 s + 8 (l / 32) .. + 7 of each step s of query l % 32: the P^T operand of
 //  * O^T += V^T P^T on v_mfma_f32_32x32x16_f16, V^T by transposed LDS reads.
-// Weights are 2^(s - max + P_UP) and values code 2^(e - top + V_UP): both stay
-// normal fp16 numbers where it matters; the row sum carries P_UP too, and the
-// output takes 2^(top - V_UP) back.  Keys past the sequence, future ones and
+// Weights are 2^(s - ref + P_UP), where ref follows the running maximum once that
+// is more than P_LAG above it (at most 2^15, and what is 2^-22 of the largest is
+// still a normal number), and values code 2^(e - top + V_UP); the row sum, a
+// product with ones, carries 2^P_UP too, and the output takes 2^(top - V_UP)
+// back.  Keys past the sequence, future ones and
 // those of a bad page are masked by selection (bad pages: NaN keys, so that a
 // query that sees one becomes NaN).  A NaN among the value codes would reach
 // queries that do not see it (0 NaN): value tiles hold zeros in their place and a
@@ -861,7 +863,7 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-constexpr int P_UP = 14, V_UP = 6;
+constexpr int P_UP = 8, P_LAG = 7, V_UP = 6;
 
 // Sixteen codes times a power of two, as 32 bytes of bf16 or fp16.
 template <bool F16>
@@ -932,40 +934,49 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     const size_t head0 = ((size_t)slot * nkv + kvh) * cv.kv.max_seq_len;
     const size_t blk0 = ((size_t)slot * nkv + kvh) * (cv.kv.max_seq_len >> cv.blk_shift);
     const uint8_t *kc = (const uint8_t *)cl.k, *vc = (const uint8_t *)cl.v;
-    // this thread's key of a tile, and the first key of the 16-token group whose
-    // scale bytes this lane loads (lanes 0 .. 3 values', 4 .. 7 keys')
-    auto key_at = [&](int k0) { return min(k0 + row, Lk - 1); };
-    auto grp_at = [&](int k0) { return min(k0 + 16 * (lane & 3), Lk - 1); };
-    int pg_row = 0, pg_grp = 0;                       // pages of the next tile to be loaded
-    auto fetch_pages = [&](int k0) {
+    // The thread's key row and the 16-token group whose scale bytes its lane
+    // loads (lanes 0 .. 3 values', 4 .. 7 keys'): rows of the slot, or a page's
+    // index in the slot's table and a row in it, moved on by a tile at a time.
+    // Rows past the sequence are not loaded (scales: the group's first token).
+    int t_row = row, t_grp = 16 * (lane & 3), i_row = 0, i_grp = 0, in_row = t_row, in_grp = t_grp;
+    auto advance = [&](int &idx, int &in) {           // in < page_size + 64 <= 2^20 + 64: the quotient is exact
+        const int step = (int)(((float)in + 0.5f) * cv.page_inv);
+        idx += step;
+        in -= step * ps;
+    };
+    int pg_row = 0, pg_grp = 0;                       // pages of the tile to be loaded next
+    auto fetch_pages = [&]() {                        // of the tile that t_row and t_grp stand at
         if (!paged) return;
-        pg_row = pt[key_at(k0) / ps];
-        pg_grp = pt[grp_at(k0) / ps];
+        advance(i_row, in_row);
+        advance(i_grp, in_grp);
+        if (t_row < Lk) pg_row = pt[i_row];
+        if (t_grp < Lk) pg_grp = pt[i_grp];
     };
     uint4 kraw, vraw;
     uint32_t sc = 0;
     bool kbad = false;                                // the loaded row's page is none
-    kraw = vraw = (uint4){0u, 0u, 0u, 0u};
-    auto load = [&](int k0) {
-        size_t off, blk;
-        const int t = key_at(k0), tg = grp_at(k0);
+    auto load = [&]() {                               // that tile; then on to the next
+        size_t off = head0 + t_row, blk = blk0 + (t_grp >> cv.blk_shift);
+        const bool ok = t_row < Lk;
         if (paged) {
             kbad = (unsigned)pg_row >= (unsigned)cv.num_pages;
             const size_t hr = (size_t)(kbad ? 0 : pg_row) * nkv + kvh;
             const size_t hg = (size_t)((unsigned)pg_grp >= (unsigned)cv.num_pages ? 0 : pg_grp) * nkv + kvh;
-            off = hr * ps + t % ps;
-            blk = hg * (ps >> cv.blk_shift) + ((tg % ps) >> cv.blk_shift);
-        } else {
-            off = head0 + t;
-            blk = blk0 + (tg >> cv.blk_shift);
+            off = hr * ps + in_row;
+            blk = hg * (ps >> cv.blk_shift) + (in_grp >> cv.blk_shift);
+            in_row += BKT;
+            in_grp += BKT;
         }
-        if (has_k) kraw = *(const uint4 *)(kc + off * D + 16 * c);
-        if (has_v) vraw = *(const uint4 *)(vc + off * D + 16 * c);
-        sc = (lane & 4 ? cl.ks : cl.vs)[blk];
+        kraw = vraw = (uint4){0u, 0u, 0u, 0u};
+        if (has_k && ok) kraw = *(const uint4 *)(kc + off * D + 16 * c);
+        if (has_v && ok) vraw = *(const uint4 *)(vc + off * D + 16 * c);
+        if (t_grp < Lk) sc = (lane & 4 ? cl.ks : cl.vs)[blk];
+        t_row += BKT;
+        t_grp += BKT;
     };
     // The loaded tile (keys from k0) to LDS buffer b; `top` becomes the common
     // exponent byte of its values.
-    auto store = [&](int k0, int b, int &top) {
+    auto store = [&](int b, int &top) {
         const int v0 = __builtin_amdgcn_readlane(sc, 0), v1 = __builtin_amdgcn_readlane(sc, 1);
         const int v2 = __builtin_amdgcn_readlane(sc, 2), v3 = __builtin_amdgcn_readlane(sc, 3);
         top = max(top, max(max(v0, v1), max(v2, v3)));
@@ -981,8 +992,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
             K[pf_swz<KCH>(row, 2 * c + 1)] = hi;
         }
         if (has_v) {
-            const bool drop = k0 + row >= Lk || kbad;
-            const uint32_t use = drop ? 0u : 0xffffffffu;
+            const uint32_t use = kbad ? 0u : 0xffffffffu;
             vraw = (uint4){vraw.x & use, vraw.y & use, vraw.z & use, vraw.w & use};
             const uint32_t nx = nan_codes(vraw.x), ny = nan_codes(vraw.y), nz = nan_codes(vraw.z), nw = nan_codes(vraw.w);
             uint32_t bits = 0u;
@@ -1021,31 +1031,35 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
-    float mrow = -INFINITY, lpart = 0.f;
+    float mrow = -INFINITY;
+    f32x16 lsum;                                      // ones P^T: every row the sums of the rounded weights
+#pragma unroll
+    for (int j = 0; j < 16; ++j) lsum[j] = 0.f;
+    f16x8 ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = (_Float16)1.0f;
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);   // log2(e) / sqrt(d)
     const int qq = p0 + q0 + r32;
 
     if (tid == 0) has_nan = 0;
     int top_next = 0, top_acc = 0;
-    fetch_pages(0);
-    load(0);
-    fetch_pages(BKT);
+    fetch_pages();
+    load();
+    fetch_pages();
     __syncthreads();
-    store(0, 0, top_next);
+    store(0, top_next);
     int top = top_next;
     top_acc = top;
-    load(min(BKT, (ntiles - 1) * BKT));
-    fetch_pages(2 * BKT);
+    load();
+    fetch_pages();
     for (int i = 0; i < ntiles; ++i) {
         const int k0 = i * BKT, b = i & 1;
         __syncthreads();                              // tile i is in LDS, and tile i - 1's buffer is free
         top = top_next;
         if (i + 1 < ntiles) {
-            store(k0 + BKT, b ^ 1, top_next);
-            if (i + 2 < ntiles) {
-                load(k0 + 2 * BKT);
-                fetch_pages(k0 + 3 * BKT);
-            }
+            store(b ^ 1, top_next);
+            load();                                   // a tile past the last: rows past the sequence, or one never stored
+            fetch_pages();
         }
         if (k0 > my_last_q) continue;                 // wave-uniform: the whole tile is in this unit's future
 
@@ -1094,10 +1108,14 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
 #pragma unroll
                 for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
         }
-        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-        const float mnew = fmaxf(mrow, mt * scale2);
+        {
+            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+            mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * scale2;   // both halves of the query's keys
+        }
+        // the reference stays where the maximum is at most 2^P_LAG above it, so
+        // most tiles rescale nothing
+        const float mnew = mt > mrow + P_LAG ? mt : mrow;
         const float moff = (mnew == -INFINITY ? 0.f : mnew) - P_UP;
-        float ls = 0.f;
         f16x8 pf[4];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -1109,7 +1127,6 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
                     typedef float f32x2_t __attribute__((ext_vector_type(2)));
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e], scale2, -moff));
                     const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e + 1], scale2, -moff));
-                    ls += x + y;
                     w[e] = __builtin_convertvector((f32x2_t){x, y}, f16x2);
                 }
                 pf[2 * kt + half] = __builtin_bit_cast(f16x8, w);
@@ -1117,7 +1134,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         if (__ballot(mnew != mrow) || top != top_acc) {
             const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
             const float fall = exp2_int(max(top_acc - top, -126));
-            lpart *= alpha;
+            lsum[0] *= alpha;                         // the only one read
             const float a = alpha * fall;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -1125,7 +1142,6 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
                 for (int j = 0; j < 16; ++j) acc[dt][j] *= a;
             top_acc = top;
         }
-        lpart += ls;
         mrow = mnew;
         // operand f: 16-key step f / DT, output tile f % DT; lane l takes
         // dimension 32 dt + l % 32 of keys 16 s + 8 h .. + 7 by two transposed reads
@@ -1148,6 +1164,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         for (int f = 0; f < 4 * DT; ++f) {
             if (f + VD < 4 * DT) vread(f + VD);
             __builtin_amdgcn_sched_barrier(0);
+            if (f % DT == 0) lsum = __builtin_amdgcn_mfma_f32_32x32x16_f16(ones, pf[f / DT], lsum, 0, 0, 0);
             acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[f % (VD + 1)], pf[f / DT], acc[f % DT], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -1173,9 +1190,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]; through LDS for whole rows
     uint16_t *ost = (uint16_t *)ring + (size_t)wave * QB * OPITCH;
     {
-        float L = lpart;
-        L += __shfl_xor(L, 32, 64);
-        const float inv = 1.0f / L;
+        const float inv = 1.0f / lsum[0];
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
