@@ -852,14 +852,17 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 //  * O^T += V^T P^T on v_mfma_f32_32x32x16_f16, V^T by transposed LDS reads.
 // Weights are 2^(s - ref + P_UP), where ref follows the running maximum once that
 // is more than P_LAG above it (at most 2^15, and what is 2^-22 of the largest is
-// still a normal number), and values code 2^(e - top + V_UP); the row sum, a
-// product with ones, carries 2^P_UP too, and the output takes 2^(top - V_UP)
-// back.  Keys past the sequence, future ones and
-// those of a bad page are masked by selection (bad pages: NaN keys, so that a
-// query that sees one becomes NaN).  A NaN among the value codes would reach
-// queries that do not see it (0 NaN): value tiles hold zeros in their place and a
-// bit for each, and from the first one on the queries' sums are set to NaN by
-// the bits of the keys that they see.
+// still a normal number), and values code 2^(e - top + V_UP); the row sum (fp32,
+// of the weights before they are rounded) carries 2^P_UP too, and the output
+// takes 2^(top - V_UP) back.
+//
+// A wavefront loads rows of one 16-token group of a tile, so its page and row
+// base are scalars and the loop has no vector address arithmetic.  Future keys
+// and those past the sequence are masked by selection, value codes past it are
+// cleared.  A NaN among the values would reach queries that do not see it
+// (0 NaN), and a page that is none is read as page 0: a wavefront whose sums
+// hold a NaN, or whose workgroup met such a page, does its rows again one by
+// one (attend_row).
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -869,7 +872,6 @@ constexpr int P_UP = 8, P_LAG = 7, V_UP = 6;
 template <bool F16>
 __device__ __forceinline__ void codes_16(uint4 w, float scale, uint4 &lo, uint4 &hi)
 {
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     uint32_t o[8];
     const uint32_t in[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -886,22 +888,75 @@ __device__ __forceinline__ void codes_16(uint4 w, float scale, uint4 &lo, uint4 
     hi = (uint4){o[4], o[5], o[6], o[7]};
 }
 
-// Bit 7 of a byte of the result: that code is NaN (0x7f or 0xff).
-__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-
+// One query row over its first n keys, by one wavefront in fp32: 64 keys at a
+// time, a key to a lane for the scores, then D / 64 dimensions to a lane.  For
+// rows that see a NaN or a page that is none (the whole row becomes NaN).
 template <int D>
+__device__ __forceinline__ void attend_row(const uint16_t *q, int n, int kvh, int nkv, int slot, const CacheView &cv,
+                                        const CacheLayer &cl, uint16_t *out)
+{
+    constexpr int E = D / 64;
+    const int lane = threadIdx.x & 63;
+    const float scale = 1.0f / sqrtf((float)D);
+    float m = -INFINITY, l = 0.f, acc[E] = {};
+    bool lost = false;
+    for (int b = 0; b < n; b += 64) {
+        const int t = min(b + lane, n - 1);
+        int page = 0;
+        if (cv.kv.layout == 1) page = page_of(cv, slot, t);
+        lost |= page < 0;
+        const Place pl = place(cv, nkv, kvh, slot, max(page, 0), t);
+        const uint8_t *k = (const uint8_t *)cl.k + pl.row * D;
+        float sc = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < D; i += 4) {
+            const uint32_t w = *(const uint32_t *)(k + i);
+            sc += bf2f(q[i]) * __builtin_amdgcn_cvt_f32_fp8(w, 0);
+            sc += bf2f(q[i + 1]) * __builtin_amdgcn_cvt_f32_fp8(w, 1);
+            sc += bf2f(q[i + 2]) * __builtin_amdgcn_cvt_f32_fp8(w, 2);
+            sc += bf2f(q[i + 3]) * __builtin_amdgcn_cvt_f32_fp8(w, 3);
+        }
+        sc *= __uint_as_float((uint32_t)cl.ks[pl.blk] << 23) * scale;
+        const bool on = b + lane < n;
+        float mt = on ? sc : -INFINITY;
+        for (int o = 32; o; o >>= 1) mt = fmaxf(mt, __shfl_xor(mt, o, 64));
+        const float mn = fmaxf(m, mt), off = mn == -INFINITY ? 0.f : mn;
+        const float al = __expf(m - off), pe = on ? __expf(sc - off) : 0.f;
+        float sum = pe;
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        l = l * al + sum;
+        m = mn;
+        for (int e = 0; e < E; ++e) acc[e] *= al;
+        const float vsc = __uint_as_float((uint32_t)cl.vs[pl.blk] << 23);
+        for (int i = 0; i < min(64, n - b); ++i) {
+            const float w = __shfl(pe, i, 64), vs = __shfl(vsc, i, 64);
+            const size_t row = __shfl((unsigned long long)pl.row, i, 64);
+            for (int e = 0; e < E; ++e)
+                acc[e] += w * (__builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)cl.v)[row * D + E * lane + e], 0) * vs);
+        }
+    }
+    lost = __ballot(lost) != 0ull;
+    for (int e = 0; e < E; ++e) out[E * lane + e] = f2bf(lost ? QNAN : acc[e] / l);
+}
+
+// LDS units of a value tile: vtile_swz, and odd rows' units in the other of two
+// neighbours, so that the 16 lanes of a store phase (every second unit of two
+// rows) land on different banks; a transposed read takes both neighbours.
+template <int KCH>
+__device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
+
+template <int D, bool PAGED>
 __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq, int G,
                                                        int nkv, CacheView cv, CacheLayer cl, uint16_t *__restrict__ out,
                                                        long long ldo)
 {
     constexpr int NW = 8, QB = 32, BKT = 64;          // wavefronts; queries of a unit; keys of a tile
-    constexpr int DT = D / 32, KS = D / 16, KCH = D / 8, KB = D / 16;
-    constexpr int HALF = BKT * KCH, STAGE = 2 * HALF; // 16-byte units of a tile's 16-bit keys (then values)
+    constexpr int DT = D / 32, KS = D / 16, KCH = D / 8;
+    constexpr int UNITS = BKT * KCH;                  // 16-byte units of a tile's 16-bit keys, or values
     constexpr int OPITCH = D + 8;
-    static_assert(NW * QB * OPITCH * 2 <= 2 * STAGE * 16 + NW * QB * 16, "output staging fits");
-    __shared__ __attribute__((aligned(16))) uint4 ring[2 * STAGE + NW * QB];
-    __shared__ __attribute__((aligned(16))) uint16_t nan_bits[2][BKT][KB];         // one bit for each value code of a tile's rows
-    __shared__ int has_nan;
+    constexpr int LDS_UNITS = 4 * UNITS > NW * QB * OPITCH / 8 ? 4 * UNITS : NW * QB * OPITCH / 8;
+    __shared__ __attribute__((aligned(16))) uint4 ring[LDS_UNITS];    // two key tiles, two value tiles; the output
+    __shared__ int lost;
 
     const int kvh = blockIdx.x % nkv;
     int si = 0;
@@ -921,100 +976,95 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     const int my_last_q = active ? p0 + min(n, q0 + QB) - 1 : -1;
     const int ntiles = __builtin_amdgcn_readfirstlane(wg_last_q / BKT + 1);
 
-    // Loads: thread t takes 16-byte unit c of key row `row` and, for heads of
-    // 128, of the value row; for heads of 64 wavefronts 4 .. 7 take the values.
-    // A wavefront's rows are in one 16-token group of the tile, `sub`.
+    // Loads: for heads of 128 a wavefront takes eight rows of a tile's keys and
+    // values, for heads of 64 sixteen rows of keys (wavefronts 0 .. 3) or values:
+    // 16-byte unit c of row `row`, in 16-token group `sub` of the tile.
     constexpr bool BOTH = D == 128;
     const int row = BOTH ? tid >> 3 : (tid & 255) >> 2, c = BOTH ? tid & 7 : tid & 3;
     const bool has_k = BOTH || wave < 4, has_v = BOTH || wave >= 4;
     const int sub = BOTH ? wave >> 1 : wave & 3;
-    const bool paged = cv.kv.layout == 1;
-    const int ps = cv.kv.page_size;
-    const int32_t *pt = paged ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
+    const int ps = PAGED ? cv.kv.page_size : 0, bs = cv.blk_shift;
+    const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
     const size_t head0 = ((size_t)slot * nkv + kvh) * cv.kv.max_seq_len;
-    const size_t blk0 = ((size_t)slot * nkv + kvh) * (cv.kv.max_seq_len >> cv.blk_shift);
-    const uint8_t *kc = (const uint8_t *)cl.k, *vc = (const uint8_t *)cl.v;
-    // The thread's key row and the 16-token group whose scale bytes its lane
-    // loads (lanes 0 .. 3 values', 4 .. 7 keys'): rows of the slot, or a page's
-    // index in the slot's table and a row in it, moved on by a tile at a time.
-    // Rows past the sequence are not loaded (scales: the group's first token).
-    int t_row = row, t_grp = 16 * (lane & 3), i_row = 0, i_grp = 0, in_row = t_row, in_grp = t_grp;
-    auto advance = [&](int &idx, int &in) {           // in < page_size + 64 <= 2^20 + 64: the quotient is exact
-        const int step = (int)(((float)in + 0.5f) * cv.page_inv);
-        idx += step;
-        in -= step * ps;
-    };
-    int pg_row = 0, pg_grp = 0;                       // pages of the tile to be loaded next
-    auto fetch_pages = [&]() {                        // of the tile that t_row and t_grp stand at
-        if (!paged) return;
-        advance(i_row, in_row);
-        advance(i_grp, in_grp);
-        if (t_row < Lk) pg_row = pt[i_row];
-        if (t_grp < Lk) pg_grp = pt[i_grp];
+    const size_t blk0 = ((size_t)slot * nkv + kvh) * (cv.kv.max_seq_len >> bs);
+    const uint32_t off = (uint32_t)((row & 15) * D + 16 * c);      // in the group's rows
+    // The next tile to load: its groups start at tokens t + 16 j; paged, page
+    // idx and row `in` of the wavefront's group, and of the group whose value
+    // scale this lane loads (lane & 3).
+    int t = 0, idx = 0, in = 16 * sub, l_idx = 0, l_in = 16 * (lane & 3);
+    int page = 0, l_page = 0;
+    bool bad = false;
+    auto fetch_pages = [&]() {
+        if constexpr (PAGED) {
+            while (in >= ps) {
+                in -= ps;
+                ++idx;
+            }
+            const int step = (int)(((float)l_in + 0.5f) * cv.page_inv);   // l_in < page_size + 64: exact
+            l_idx += step;
+            l_in -= step * ps;
+            page = l_page = 0;
+            if (t + 16 * sub < Lk) page = pt[idx];
+            if (t + 16 * (lane & 3) < Lk) l_page = pt[l_idx];
+        }
     };
     uint4 kraw, vraw;
-    uint32_t sc = 0;
-    bool kbad = false;                                // the loaded row's page is none
-    auto load = [&]() {                               // that tile; then on to the next
-        size_t off = head0 + t_row, blk = blk0 + (t_grp >> cv.blk_shift);
-        const bool ok = t_row < Lk;
-        if (paged) {
-            kbad = (unsigned)pg_row >= (unsigned)cv.num_pages;
-            const size_t hr = (size_t)(kbad ? 0 : pg_row) * nkv + kvh;
-            const size_t hg = (size_t)((unsigned)pg_grp >= (unsigned)cv.num_pages ? 0 : pg_grp) * nkv + kvh;
-            off = hr * ps + in_row;
-            blk = hg * (ps >> cv.blk_shift) + (in_grp >> cv.blk_shift);
-            in_row += BKT;
-            in_grp += BKT;
-        }
+    uint32_t kb = 0, vb = 0;                          // scale bytes: of the wavefront's group's keys, of group lane & 3's values
+    auto load = [&]() {
         kraw = vraw = (uint4){0u, 0u, 0u, 0u};
-        if (has_k && ok) kraw = *(const uint4 *)(kc + off * D + 16 * c);
-        if (has_v && ok) vraw = *(const uint4 *)(vc + off * D + 16 * c);
-        if (t_grp < Lk) sc = (lane & 4 ? cl.ks : cl.vs)[blk];
-        t_row += BKT;
-        t_grp += BKT;
+        size_t base, kblk, vblk;
+        if constexpr (PAGED) {
+            page = __builtin_amdgcn_readfirstlane(page);
+            if ((unsigned)page >= (unsigned)cv.num_pages) {
+                bad = true;
+                page = 0;
+            }
+            if ((unsigned)l_page >= (unsigned)cv.num_pages) l_page = 0;
+            const size_t head = (size_t)page * nkv + kvh;
+            base = head * ps + in;
+            kblk = head * (ps >> bs) + (in >> bs);
+            vblk = ((size_t)l_page * nkv + kvh) * (ps >> bs) + (l_in >> bs);
+            in += BKT;
+            l_in += BKT;
+        } else {
+            base = head0 + t + 16 * sub;
+            kblk = blk0 + ((t + 16 * sub) >> bs);
+            vblk = blk0 + ((t + 16 * (lane & 3)) >> bs);
+        }
+        if (t + 16 * sub < Lk) {                      // the whole group stands in the slot
+            if (has_k) {
+                kraw = *(const uint4 *)((const uint8_t *)cl.k + base * D + off);
+                kb = cl.ks[kblk];
+            }
+            if (has_v) vraw = *(const uint4 *)((const uint8_t *)cl.v + base * D + off);
+        }
+        if (t + 16 * (lane & 3) < Lk) vb = cl.vs[vblk];
+        t += BKT;
     };
-    // The loaded tile (keys from k0) to LDS buffer b; `top` becomes the common
+    // The loaded tile, from key k0, to LDS buffer b; `top` becomes the common
     // exponent byte of its values.
-    auto store = [&](int b, int &top) {
-        const int v0 = __builtin_amdgcn_readlane(sc, 0), v1 = __builtin_amdgcn_readlane(sc, 1);
-        const int v2 = __builtin_amdgcn_readlane(sc, 2), v3 = __builtin_amdgcn_readlane(sc, 3);
+    const int kw0 = pf_swz<KCH>(row, 2 * c), kw1 = pf_swz<KCH>(row, 2 * c + 1);
+    const int vw0 = row * KCH + ((2 * c) ^ val16_swz<KCH>(row)), vw1 = row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row));
+    auto store = [&](int k0, int b, int &top) {
+        const int v0 = __builtin_amdgcn_readlane(vb, 0), v1 = __builtin_amdgcn_readlane(vb, 1);
+        const int v2 = __builtin_amdgcn_readlane(vb, 2), v3 = __builtin_amdgcn_readlane(vb, 3);
         top = max(top, max(max(v0, v1), max(v2, v3)));
-        const int kb = __builtin_amdgcn_readlane(sc, 4 + sub), vb = __builtin_amdgcn_readlane(sc, sub);
-        uint4 *K = ring + b * STAGE, *V = K + HALF;
+        uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
         uint4 lo, hi;
         if (has_k) {
-            codes_16<false>(kraw, __uint_as_float((uint32_t)kb << 23), lo, hi);
-            const uint32_t nan = kbad ? 0x7fc07fc0u : 0u;    // or'ed in: still NaN
-            lo = (uint4){lo.x | nan, lo.y | nan, lo.z | nan, lo.w | nan};
-            hi = (uint4){hi.x | nan, hi.y | nan, hi.z | nan, hi.w | nan};
-            K[pf_swz<KCH>(row, 2 * c)] = lo;
-            K[pf_swz<KCH>(row, 2 * c + 1)] = hi;
+            codes_16<false>(kraw, __uint_as_float(__builtin_amdgcn_readfirstlane(kb) << 23), lo, hi);
+            K[kw0] = lo;
+            K[kw1] = hi;
         }
         if (has_v) {
-            const uint32_t use = kbad ? 0u : 0xffffffffu;
-            vraw = (uint4){vraw.x & use, vraw.y & use, vraw.z & use, vraw.w & use};
-            const uint32_t nx = nan_codes(vraw.x), ny = nan_codes(vraw.y), nz = nan_codes(vraw.z), nw = nan_codes(vraw.w);
-            uint32_t bits = 0u;
-            if (nx | ny | nz | nw) {
-                has_nan = 1;
-                const uint32_t n4[4] = {nx, ny, nz, nw};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bits |= ((((n4[i] >> 7) * 0x10204080u) >> 28) & 15u) << (4 * i);
-                vraw.x &= ~((nx >> 7) * 255u);
-                vraw.y &= ~((ny >> 7) * 255u);
-                vraw.z &= ~((nz >> 7) * 255u);
-                vraw.w &= ~((nw >> 7) * 255u);
+            if (k0 + BKT > Lk) {
+                const uint32_t use = k0 + row < Lk ? 0xffffffffu : 0u;
+                vraw = (uint4){vraw.x & use, vraw.y & use, vraw.z & use, vraw.w & use};
             }
-            nan_bits[b][row][c] = (uint16_t)bits;
-            const int e = max(vb - top + V_UP, -60);
+            const int e = max((sub == 0 ? v0 : sub == 1 ? v1 : sub == 2 ? v2 : v3) - top + V_UP, -60);
             codes_16<true>(vraw, exp2_int(e), lo, hi);
-            // odd rows write their second unit first: neighbouring rows' units lie in the same banks
-            const int odd = row & 1, s = vtile_swz<KCH>(row);
-            V[row * KCH + ((2 * c + odd) ^ s)] =
-                (uint4){odd ? hi.x : lo.x, odd ? hi.y : lo.y, odd ? hi.z : lo.z, odd ? hi.w : lo.w};
-            V[row * KCH + ((2 * c + 1 - odd) ^ s)] =
-                (uint4){odd ? lo.x : hi.x, odd ? lo.y : hi.y, odd ? lo.z : hi.z, odd ? lo.w : hi.w};
+            V[vw0] = lo;
+            V[vw1] = hi;
         }
     };
 
@@ -1031,39 +1081,34 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
-    float mrow = -INFINITY;
-    f32x16 lsum;                                      // ones P^T: every row the sums of the rounded weights
-#pragma unroll
-    for (int j = 0; j < 16; ++j) lsum[j] = 0.f;
-    f16x8 ones;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ones[j] = (_Float16)1.0f;
+    float mrow = -INFINITY, lpart = 0.f;              // reference and sum of the lane's own keys
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);   // log2(e) / sqrt(d)
     const int qq = p0 + q0 + r32;
+    // operand addresses in a tile: key unit 2 s + h of the row that this lane's
+    // MFMA row stands for; transposed value reads (see vread)
+    const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
 
-    if (tid == 0) has_nan = 0;
-    int top_next = 0, top_acc = 0;
+    if (tid == 0) lost = 0;
+    int top_next = 0;
     fetch_pages();
     load();
     fetch_pages();
-    __syncthreads();
-    store(0, top_next);
-    int top = top_next;
-    top_acc = top;
+    store(0, 0, top_next);
+    int top_acc = top_next;
     load();
     fetch_pages();
     for (int i = 0; i < ntiles; ++i) {
         const int k0 = i * BKT, b = i & 1;
-        __syncthreads();                              // tile i is in LDS, and tile i - 1's buffer is free
-        top = top_next;
+        __syncthreads();                              // tile i is in LDS, and tile i - 1's buffers are free
+        const int top = top_next;
         if (i + 1 < ntiles) {
-            store(b ^ 1, top_next);
-            load();                                   // a tile past the last: rows past the sequence, or one never stored
+            store(k0 + BKT, b ^ 1, top_next);
+            load();                                   // past the last tile: groups past the sequence, or a tile not stored
             fetch_pages();
         }
         if (k0 > my_last_q) continue;                 // wave-uniform: the whole tile is in this unit's future
 
-        const uint4 *Kt = ring + b * STAGE, *Vt = Kt + HALF;
+        const uint4 *Kt = ring + b * UNITS, *Vt = ring + (2 + b) * UNITS;
         f32x16 st[2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -1072,11 +1117,12 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         // key operands two steps ahead of their products, in a fixed order
         constexpr int KD = 2;
         bf16x8 kf[KD + 1][2];
+        int kr = krow;
+        asm volatile("" : "+v"(kr));                  // the steps' addresses are made anew: kept, they cost registers
         auto kread = [&](int ks) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
-                kf[ks % (KD + 1)][kt] =
-                    __builtin_bit_cast(bf16x8, Kt[pf_swz<KCH>(32 * kt + pf_key_of_row(r32), 2 * ks + h)]);
+                kf[ks % (KD + 1)][kt] = __builtin_bit_cast(bf16x8, Kt[pf_swz<KCH>(32 * kt + kr, 2 * ks + h)]);
         };
 #pragma unroll
         for (int ks = 0; ks < KD; ++ks) kread(ks);
@@ -1090,24 +1136,20 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
             __builtin_amdgcn_sched_barrier(0);
         }
         // lane: keys k0 + 32 kt + 16 (j / 8) + 8 h + j % 8 of query qq
-        const bool masked = k0 + BKT - 1 > p0 + q0 || k0 + BKT > Lk;
         float mt = -INFINITY;
-        if (masked) {
+        if (k0 + BKT - 1 > p0 + q0 || k0 + BKT > Lk) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int key = k0 + 32 * kt + 16 * (j >> 3) + 8 * h + (j & 7);
-                    const float sv = (key <= qq && key < Lk) ? st[kt][j] : -INFINITY;
-                    st[kt][j] = sv;
-                    mt = fmaxf(mt, sv);
+                    st[kt][j] = (key <= qq && key < Lk) ? st[kt][j] : -INFINITY;
                 }
-        } else {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
         }
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
         {
             const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
             mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * scale2;   // both halves of the query's keys
@@ -1117,6 +1159,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         const float mnew = mt > mrow + P_LAG ? mt : mrow;
         const float moff = (mnew == -INFINITY ? 0.f : mnew) - P_UP;
         f16x8 pf[4];
+        float ls = 0.f;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -1127,25 +1170,25 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
                     typedef float f32x2_t __attribute__((ext_vector_type(2)));
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e], scale2, -moff));
                     const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e + 1], scale2, -moff));
+                    ls += x + y;
                     w[e] = __builtin_convertvector((f32x2_t){x, y}, f16x2);
                 }
                 pf[2 * kt + half] = __builtin_bit_cast(f16x8, w);
             }
         if (__ballot(mnew != mrow) || top != top_acc) {
             const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
-            const float fall = exp2_int(max(top_acc - top, -126));
-            lsum[0] *= alpha;                         // the only one read
-            const float a = alpha * fall;
+            const float a = alpha * exp2_int(max(top_acc - top, -126));
+            lpart *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[dt][j] *= a;
             top_acc = top;
         }
+        lpart += ls;
         mrow = mnew;
         // operand f: 16-key step f / DT, output tile f % DT; lane l takes
         // dimension 32 dt + l % 32 of keys 16 s + 8 h .. + 7 by two transposed reads
-        const int a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
         constexpr int VD = 3;                         // read three ahead of their products
         f16x8 vf[VD + 1];
         auto vread = [&](int f) {
@@ -1154,7 +1197,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
             for (int r = 0; r < 2; ++r) {
                 const int key = 16 * (f / DT) + 8 * h + 4 * r + qv;
                 const int cc = 4 * (f % DT) + 2 * half16 + (a4 >> 1);
-                part[r] = lds_read_tr16(reinterpret_cast<const char *>(Vt + key * KCH + (cc ^ vtile_swz<KCH>(key))) + 8 * (a4 & 1));
+                part[r] = lds_read_tr16(reinterpret_cast<const char *>(Vt + key * KCH + (cc ^ val16_swz<KCH>(key))) + 8 * (a4 & 1));
             }
             vf[f % (VD + 1)] = __builtin_bit_cast(f16x8, (uint4){part[0].x, part[0].y, part[1].x, part[1].y});
         };
@@ -1164,42 +1207,38 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
         for (int f = 0; f < 4 * DT; ++f) {
             if (f + VD < 4 * DT) vread(f + VD);
             __builtin_amdgcn_sched_barrier(0);
-            if (f % DT == 0) lsum = __builtin_amdgcn_mfma_f32_32x32x16_f16(ones, pf[f / DT], lsum, 0, 0, 0);
             acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[f % (VD + 1)], pf[f / DT], acc[f % DT], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (has_nan) {   // once a tile of this workgroup had one; a tile without changes nothing here
-            uint32_t hit[DT];
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) hit[dt] = 0u;
-#pragma unroll 1
-            for (int key = 0; key < BKT; ++key) {
-                if (k0 + key > qq) break;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) hit[dt] |= ((const uint32_t *)nan_bits[b][key])[dt];
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (hit[dt] >> (8 * (j >> 2) + 4 * h + (j & 3)) & 1u) acc[dt][j] = QNAN;
-        }
     }
+    if (bad) lost = 1;
     __syncthreads();                                  // every wavefront is done with the tiles
 
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]; through LDS for whole rows
     uint16_t *ost = (uint16_t *)ring + (size_t)wave * QB * OPITCH;
+    bool nan = false;
     {
-        const float inv = 1.0f / lsum[0];
+        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
+        const float inv = 1.0f / (__uint_as_float(two[0]) + __uint_as_float(two[1]));
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (int j = 0; j < 16; ++j) {
+                const float v = acc[dt][j] * inv;
+                nan |= v != v;
                 ost[r32 * OPITCH + 32 * dt + 8 * (j >> 2) + 4 * h + (j & 3)] =
-                    f2bf(__builtin_amdgcn_ldexpf(acc[dt][j] * inv, top_acc - 127 - V_UP));
+                    f2bf(__builtin_amdgcn_ldexpf(v, top_acc - 127 - V_UP));
+            }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wavefront's staging writes are done
     if (!active) return;
+    if (lost || __ballot(nan && q0 + r32 < n)) {
+#pragma unroll 1
+        for (int r = 0; r < QB && q0 + r < n; ++r)
+            attend_row<D>(q + (size_t)(q0 + r) * ldq + (size_t)hq * D, p0 + q0 + r + 1, kvh, nkv, slot, cv, cl,
+                          out + (size_t)(q0 + r) * ldo + (size_t)hq * D);
+        return;
+    }
 #pragma unroll 4
     for (int it = lane; it < QB * (D / 8); it += 64) {
         const int qr = it / (D / 8), c8 = it % (D / 8), qo = q0 + qr;
@@ -1314,9 +1353,15 @@ hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, SeqTable &seq, in
         groups += ((seq.len[i] + 31) / 32 * G + 7) / 8;
     }
     const dim3 grid((unsigned)groups * nkv);
-    if (d == 128) KLAUNCH((k_attn8_prefill<128>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo);
-    else if (d == 64) KLAUNCH((k_attn8_prefill<64>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo);
+    const bool paged = cv.kv.layout == 1;
+#define CORUN_PREFILL8(D_, P_) \
+    KLAUNCH((k_attn8_prefill<D_, P_>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo)
+    if (d == 128 && paged) CORUN_PREFILL8(128, true);
+    else if (d == 128) CORUN_PREFILL8(128, false);
+    else if (d == 64 && paged) CORUN_PREFILL8(64, true);
+    else if (d == 64) CORUN_PREFILL8(64, false);
     else return hipErrorInvalidValue;
+#undef CORUN_PREFILL8
     return hipGetLastError();
 }
 

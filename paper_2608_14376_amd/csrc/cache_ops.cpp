@@ -67,7 +67,7 @@ CacheView cache_view(const corun_kv *kv)
     v.num_pages = kv->num_pages;
     const bool paged = kv->layout == CORUN_KV_PAGED;
     const long long cap = paged ? (long long)kv->max_pages_per_seq * kv->page_size : kv->max_seq_len;
-    v.cap = (int)(cap < 0x7fffffff ? cap : 0x7fffffff);
+    v.cap = (int)(cap < (1 << 30) ? cap : (1 << 30));   // positions stay far from 2^31 in the kernels
     v.e4m3 = kv->dtype == CORUN_KV_E4M3;
     v.blk_shift = !v.e4m3 || kv->scale_block == 16 ? 4 : kv->scale_block == 32 ? 5 : 6;
     v.page_inv = paged ? 1.0f / (float)kv->page_size : 0.f;
