@@ -127,6 +127,35 @@ typedef struct {
     uint8_t *const *v_scale;
 } corun_kv;
 
+/* Which elements of a head a rotation pairs, over its first rot_dim elements:
+ * (i, i + rot_dim / 2) or (2 i, 2 i + 1), i < rot_dim / 2; the others stay. */
+enum { CORUN_ROPE_HALF = 0, CORUN_ROPE_INTERLEAVED = 1 };
+/* Frequencies: f_i = theta^(-2 i / rot_dim) radians per position;
+ *  LINEAR  f_i / factor (positions interpolated);
+ *  BANDS   by the turns n = trained_len f_i / (2 pi) that a pair makes over the
+ *          trained length: f_i / factor where n <= low, f_i where n >= high,
+ *          and g f_i + (1 - g) f_i / factor, g = (n - low) / (high - low),
+ *          between (interpolation "by parts", Peng et al., 2023). */
+enum { CORUN_ROPE_UNSCALED = 0, CORUN_ROPE_LINEAR = 1, CORUN_ROPE_BANDS = 2 };
+typedef struct {
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t rot_dim;       /* even, 2 .. head_dim; 0 = head_dim */
+    int32_t layout;        /* CORUN_ROPE_HALF | CORUN_ROPE_INTERLEAVED */
+    int32_t scaling;       /* CORUN_ROPE_UNSCALED | _LINEAR | _BANDS */
+    int32_t trained_len;   /* BANDS: >= 1 */
+    float magnitude;       /* rotated elements are multiplied by it; 0 = 1 */
+    double theta;          /* > 1 */
+    double factor;         /* LINEAR, BANDS: >= 1 */
+    double low, high;      /* BANDS: 0 <= low < high */
+} corun_rope_cfg;
+#define CORUN_ROPE_MAX_PAIRS 64
+/* A rotation as the kernels take it: made by corun_rope_init, or filled in by
+ * a caller with frequencies of its own (radians per position of each pair). */
+typedef struct {
+    int32_t head_dim, rot_dim, layout;
+    float magnitude;       /* > 0 */
+    double freq[CORUN_ROPE_MAX_PAIRS];
+} corun_rope;
 /* Creation options; pass NULL for defaults (all fields 0). */
 typedef struct {
     int32_t attn_chunk;        /* split-KV chunk in tokens (multiple of 64); 0 = chosen from (model, B, capacity);
@@ -176,6 +205,11 @@ typedef struct {
                                   batch_invariant, qkv_epilogue, split_k_override or gemm_bm is set);
                                   1 = on for a dense model with B_fixed <= 8 (CORUN_E_INVAL otherwise);
                                   2 = off. */
+    const corun_rope *rope;    /* rotary positions, read at creation; NULL = half pairs over the whole of a head,
+                                  f_i = rope_theta^(-2 i / head_dim).  Its head_dim is the model's.  With
+                                  interleaved pairs, a part of the head or a magnitude, and with an e4m3 cache,
+                                  the QKV epilogue is a kernel of its own (corun_decode_append's), in decode and in
+                                  prefill: CORUN_E_INVAL with qkv_epilogue = 2 or small_batch_layer = 1. */
 } corun_options;
 
 /* Create an engine for one fixed padded batch size B_fixed (Sec. IV,
@@ -295,35 +329,6 @@ corun_status corun_prefill_batch(corun_engine *e, const int32_t *tokens, const i
  * cache.
  * ------------------------------------------------------------------------- */
 
-/* Which elements of a head a rotation pairs, over its first rot_dim elements:
- * (i, i + rot_dim / 2) or (2 i, 2 i + 1), i < rot_dim / 2; the others stay. */
-enum { CORUN_ROPE_HALF = 0, CORUN_ROPE_INTERLEAVED = 1 };
-/* Frequencies: f_i = theta^(-2 i / rot_dim) radians per position;
- *  LINEAR  f_i / factor (positions interpolated);
- *  BANDS   by the turns n = trained_len f_i / (2 pi) that a pair makes over the
- *          trained length: f_i / factor where n <= low, f_i where n >= high,
- *          and g f_i + (1 - g) f_i / factor, g = (n - low) / (high - low),
- *          between (interpolation "by parts", Peng et al., 2023). */
-enum { CORUN_ROPE_UNSCALED = 0, CORUN_ROPE_LINEAR = 1, CORUN_ROPE_BANDS = 2 };
-typedef struct {
-    int32_t head_dim;      /* 64 or 128 */
-    int32_t rot_dim;       /* even, 2 .. head_dim; 0 = head_dim */
-    int32_t layout;        /* CORUN_ROPE_HALF | CORUN_ROPE_INTERLEAVED */
-    int32_t scaling;       /* CORUN_ROPE_UNSCALED | _LINEAR | _BANDS */
-    int32_t trained_len;   /* BANDS: >= 1 */
-    float magnitude;       /* rotated elements are multiplied by it; 0 = 1 */
-    double theta;          /* > 1 */
-    double factor;         /* LINEAR, BANDS: >= 1 */
-    double low, high;      /* BANDS: 0 <= low < high */
-} corun_rope_cfg;
-#define CORUN_ROPE_MAX_PAIRS 64
-/* A rotation as the kernels take it: made by corun_rope_init, or filled in by
- * a caller with frequencies of its own (radians per position of each pair). */
-typedef struct {
-    int32_t head_dim, rot_dim, layout;
-    float magnitude;       /* > 0 */
-    double freq[CORUN_ROPE_MAX_PAIRS];
-} corun_rope;
 /* Host only.  CORUN_E_SHAPE for head_dim or rot_dim, CORUN_E_INVAL otherwise. */
 corun_status corun_rope_init(const corun_rope_cfg *cfg, corun_rope *out);
 
@@ -537,7 +542,8 @@ enum {
 
 /* Measurement aid: launch one kernel of the decode step n_iters times back
  * to back on the engine's stream, launch i using layer (layer + i) mod
- * n_layers (so weights and cache stream from HBM as in the step) and the
+ * n_layers (so weights and cache stream from HBM as in the step; the append to
+ * e4m3 caches, or with a rope of its own, the last layer) and the
  * engine's current workspace (as left by the last step), and return the mean
  * duration per launch in microseconds, measured with HIP events around the
  * launches.  The launches run on the inputs of the last decode step (tokens,

@@ -76,7 +76,7 @@ class Options(C.Structure):
     _fields_ = [(n, C.c_int32) for n in (
         "attn_chunk", "max_prefill_len", "no_graph", "poison_workspace", "split_k_override", "gemm_bm",
         "batch_invariant", "bi_prefill", "no_weight_pack", "qkv_epilogue", "record_routing",
-        "small_batch_layer")]
+        "small_batch_layer")] + [("rope", C.c_void_p)]
 
 
 class CorunError(RuntimeError):
@@ -209,10 +209,12 @@ def kv_struct(layout: int, n_slots: int, k, v, keep, max_seq_len=0, page_size=0,
 
 def options(attn_chunk=0, max_prefill_len=0, no_graph=False, poison_workspace=False, split_k_override=0,
             gemm_bm=0, batch_invariant=False, bi_prefill=False, no_weight_pack=False, qkv_epilogue=0,
-            record_routing=False, small_batch_layer=0):
-    return Options(attn_chunk, max_prefill_len, int(no_graph), int(poison_workspace), split_k_override, gemm_bm,
+            record_routing=False, small_batch_layer=0, rope=None):
+    o = Options(attn_chunk, max_prefill_len, int(no_graph), int(poison_workspace), split_k_override, gemm_bm,
                    int(batch_invariant), int(bi_prefill), int(no_weight_pack), int(qkv_epilogue),
-                   int(record_routing), int(small_batch_layer))
+                   int(record_routing), int(small_batch_layer), None if rope is None else C.addressof(rope))
+    o._rope = rope   # kept alive as long as the options
+    return o
 
 
 def _np(a, dt):
@@ -549,10 +551,12 @@ def torch_float32():
 
 class Engine:
     """One fixed-B engine.  `weights` is a workload.Weights of device bf16
-    tensors; `k`, `v` lists of per-layer device bf16 cache tensors."""
+    tensors; `k`, `v` lists of per-layer device bf16 cache tensors, or of e4m3
+    codes (one byte each) with their scale bytes `k_scale`, `v_scale` per
+    block of `scale_block` tokens (see KvCache)."""
 
     def __init__(self, cfg: dict, weights, B: int, k, v, layout=KV_CONTIGUOUS, page_size=0, page_table=None,
-                 opt: Options | None = None, stream=None):
+                 opt: Options | None = None, stream=None, k_scale=None, v_scale=None, scale_block=0):
         import torch
         L = load()
         self.cfg, self.B = cfg, B
@@ -574,6 +578,11 @@ class Engine:
             n_slots, _, S, _ = k[0].shape
             self._kv = kv_struct(layout, n_slots, k, v, keep, max_seq_len=S)
             self.capacity = S
+        if k_scale is not None:
+            cache = KvCache(k, v, k_scale, v_scale, scale_block, page_table if layout == KV_PAGED else None)
+            keep.append(cache)
+            self._kv.dtype, self._kv.scale_block = KV_E4M3, scale_block
+            self._kv.k_scale, self._kv.v_scale = cache.kv.k_scale, cache.kv.v_scale
         self._cfg = model_cfg(cfg)
         self._opt = opt if opt is not None else options()
         if stream is None:

@@ -1246,7 +1246,27 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     }
 }
 
+struct Freqs {
+    double f[64];
+};
+__global__ void k_rope_table_of(float2 *tab, int half, Freqs fr)
+{
+    const int i = threadIdx.x;
+    if (i >= half) return;
+    double s, c;
+    sincos((double)blockIdx.x * fr.f[i], &s, &c);
+    tab[(size_t)blockIdx.x * half + i] = {(float)c, (float)s};
+}
+
 }  // namespace
+
+hipError_t launch_rope_table_of(float2 *tab, int max_pos, int d, const double *freq, hipStream_t st)
+{
+    Freqs fr{};
+    for (int i = 0; i < d / 2; ++i) fr.f[i] = freq[i];
+    KLAUNCH(k_rope_table_of, dim3(max_pos), dim3(64), 0, st, tab, d / 2, fr);
+    return hipGetLastError();
+}
 
 hipError_t launch_append_rows(const QkvRows &in, int rows, const uint8_t *valid, const int32_t *pos, int nq, int nkv,
                               int d, const RopeArgs &rope, uint16_t *q, long long ldq, const CacheView &cv,
@@ -1294,25 +1314,11 @@ int attn8_chunk(int rows, int nkv, int max_len)
     return (int)std::min<long long>(chunk, 1 << 30);
 }
 
-size_t attn8_workspace(int rows, int nq, int nkv, int d, int max_len)
-{
-    const int chunk = attn8_chunk(rows, nkv, max_len);
-    return (size_t)rows * nq * ((max_len + (long long)chunk - 1) / chunk) * (d + 2);
-}
-
-hipError_t launch_attn8_rows(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
-                             int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                             float *ws, uint16_t *out, long long ldo, hipStream_t st, const int32_t *row_order)
-{
-    hipError_t e = launch_attn8_split(q, ldq, rows, valid, lens, plus_one, nq, nkv, d, cv, cl, max_len, ws, st, row_order);
-    return e != hipSuccess ? e : launch_attn8_merge(ws, rows, valid, lens, plus_one, nq, nkv, d, max_len, out, ldo, st);
-}
-
 hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
                               int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                              float *ws, hipStream_t st, const int32_t *row_order)
+                              int chunk, float *ws, hipStream_t st, const int32_t *row_order)
 {
-    const int chunk = attn8_chunk(rows, nkv, max_len), splits = (int)((max_len + (long long)chunk - 1) / chunk), G = nq / nkv;
+    const int splits = (int)((max_len + (long long)chunk - 1) / chunk), G = nq / nkv;
     const dim3 grid(nkv, splits, rows);
     if (d == 128)
         KLAUNCH((k_attn8_split<128>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits,
@@ -1326,9 +1332,9 @@ hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const 
 }
 
 hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, const int32_t *lens, int plus_one, int nq,
-                              int nkv, int d, int max_len, uint16_t *out, long long ldo, hipStream_t st)
+                              int nkv, int d, int max_len, int chunk, uint16_t *out, long long ldo, hipStream_t st)
 {
-    const int chunk = attn8_chunk(rows, nkv, max_len), splits = (int)((max_len + (long long)chunk - 1) / chunk);
+    const int splits = (int)((max_len + (long long)chunk - 1) / chunk);
     const int hb = 256 / d;
     const dim3 grid((nq + hb - 1) / hb, rows);
     const size_t shm = sizeof(float) * hb * splits;

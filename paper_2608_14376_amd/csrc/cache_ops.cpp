@@ -32,12 +32,36 @@ corun_status check_cache(const corun_kv *kv)
     } else {
         return set_errorf(CORUN_E_INVAL, "unknown KV layout %d", kv->layout);
     }
-    if (kv->dtype == CORUN_KV_BF16) return CORUN_OK;
+    if (kv->dtype == CORUN_KV_BF16) return CORUN_OK;   // scale_block and the scales are not looked at
     if (kv->dtype != CORUN_KV_E4M3) return set_errorf(CORUN_E_INVAL, "unknown KV dtype %d", kv->dtype);
     const int b = kv->scale_block, unit = kv->layout == CORUN_KV_PAGED ? kv->page_size : kv->max_seq_len;
     if (b != 16 && b != 32 && b != 64) return set_errorf(CORUN_E_SHAPE, "scale_block %d is not 16, 32 or 64", b);
     if (unit % b != 0)
         return set_errorf(CORUN_E_SHAPE, "scale_block %d does not divide %d tokens of a slot or page", b, unit);
+    return CORUN_OK;
+}
+
+bool plain_rope(const corun_rope &r)
+{
+    return r.layout == CORUN_ROPE_HALF && r.rot_dim == r.head_dim && r.magnitude == 1.f;
+}
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+corun_status layer_of(const corun_kv *kv, int32_t layer, CacheLayer *out)
+{
+    if (layer < 0) return set_errorf(CORUN_E_INVAL, "layer %d", layer);
+    if (!kv->k || !kv->v || !kv->k[layer] || !kv->v[layer]) return set_error(CORUN_E_INVAL, "missing KV pointers");
+    if (kv->layout == CORUN_KV_PAGED && !kv->page_table) return set_error(CORUN_E_INVAL, "paged cache needs page_table");
+    out->k = kv->k[layer];
+    out->v = kv->v[layer];
+    if (!aligned16(out->k) || !aligned16(out->v)) return set_error(CORUN_E_INVAL, "cache buffers must start on 16 bytes");
+    if (kv->dtype == CORUN_KV_E4M3) {
+        if (!kv->k_scale || !kv->v_scale || !kv->k_scale[layer] || !kv->v_scale[layer])
+            return set_error(CORUN_E_INVAL, "an e4m3 cache needs k_scale and v_scale");
+        out->ks = kv->k_scale[layer];
+        out->vs = kv->v_scale[layer];
+    }
     return CORUN_OK;
 }
 
@@ -135,25 +159,6 @@ corun_status check_heads(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || n_heads / n_kv_heads > 16 || n_heads > 4096)
         return set_errorf(CORUN_E_SHAPE, "%d query heads over %d kv heads: groups of 1 to 16 are supported", n_heads,
                           n_kv_heads);
-    return CORUN_OK;
-}
-
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
-corun_status layer_of(const corun_kv *kv, int32_t layer, CacheLayer *out)
-{
-    if (layer < 0) return set_errorf(CORUN_E_INVAL, "layer %d", layer);
-    if (!kv->k || !kv->v || !kv->k[layer] || !kv->v[layer]) return set_error(CORUN_E_INVAL, "missing KV pointers");
-    if (kv->layout == CORUN_KV_PAGED && !kv->page_table) return set_error(CORUN_E_INVAL, "paged cache needs page_table");
-    out->k = kv->k[layer];
-    out->v = kv->v[layer];
-    if (!aligned16(out->k) || !aligned16(out->v)) return set_error(CORUN_E_INVAL, "cache buffers must start on 16 bytes");
-    if (kv->dtype == CORUN_KV_E4M3) {
-        if (!kv->k_scale || !kv->v_scale || !kv->k_scale[layer] || !kv->v_scale[layer])
-            return set_error(CORUN_E_INVAL, "an e4m3 cache needs k_scale and v_scale");
-        out->ks = kv->k_scale[layer];
-        out->vs = kv->v_scale[layer];
-    }
     return CORUN_OK;
 }
 
@@ -280,7 +285,8 @@ extern "C" int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t 
     TRY(check_step_rows(kv, rows));
     if (max_len < 0 || max_len > cache_view(kv).cap)
         return set_errorf(CORUN_E_CAPACITY, "max_len %d outside [0, %d]", max_len, cache_view(kv).cap);
-    return (int64_t)(sizeof(float) * attn8_workspace(rows, n_heads, n_kv_heads, head_dim, longest(kv, max_len)));
+    const int64_t most = longest(kv, max_len), chunk = attn8_chunk(rows, n_kv_heads, (int)most);
+    return (int64_t)sizeof(float) * rows * n_heads * ((most + chunk - 1) / chunk) * (head_dim + 2);
 }
 
 extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
@@ -298,9 +304,12 @@ extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer
     if (need > 0 && (!ws || !aligned16(ws))) return set_error(CORUN_E_INVAL, "the workspace must start on 16 bytes");
     if (ws_bytes < need)
         return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
-    return launched(launch_attn8_rows((const uint16_t *)q, ld_q, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim,
-                                      cache_view(kv), cl, longest(kv, max_len), (float *)ws, (uint16_t *)out, ld_out,
-                                      (hipStream_t)stream));
+    const CacheView cv = cache_view(kv);
+    const int most = longest(kv, max_len), chunk = attn8_chunk(rows, n_kv_heads, most);
+    TRY(launched(launch_attn8_split((const uint16_t *)q, ld_q, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim, cv, cl,
+                                    most, chunk, (float *)ws, (hipStream_t)stream)));
+    return launched(launch_attn8_merge((const float *)ws, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim, most, chunk,
+                                       (uint16_t *)out, ld_out, (hipStream_t)stream));
 }
 
 extern "C" corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,

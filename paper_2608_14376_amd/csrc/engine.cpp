@@ -15,6 +15,7 @@
 #include <string>
 #include <vector>
 
+#include "cache_ops.h"
 #include "corun.h"
 #include "kernels.h"
 
@@ -272,6 +273,13 @@ int choose_chunk(int B, int nkv, int cap, int override_chunk)
     return chunk;
 }
 
+// Whether the QKV epilogue is the one of cache.hip (launch_append_rows /
+// _seqs): an e4m3 cache, or a rotation that the others do not know.
+bool own_epilogue(const corun_kv *kv, const corun_options &opt)
+{
+    return kv->dtype == CORUN_KV_E4M3 || (opt.rope && !plain_rope(*opt.rope));
+}
+
 Plan make_plan(const corun_model_cfg *c, const corun_kv *kv, int B, const corun_options &opt)
 {
     Plan p;
@@ -312,7 +320,7 @@ Plan make_plan(const corun_model_cfg *c, const corun_kv *kv, int B, const corun_
     // 32-row tiles stream faster there) made it 5.3-5.5 against 4.2 ms; it
     // can still be asked for up to B = 8.
     const bool gv_ok = !bi && c->n_experts == 0 && !opt.no_weight_pack && opt.qkv_epilogue == 0 && so == 0 &&
-                       bo == 0 && c->hidden % 256 == 0 && c->head_dim % 16 == 0;
+                       bo == 0 && c->hidden % 256 == 0 && c->head_dim % 16 == 0 && !own_epilogue(kv, opt);
     p.gv = opt.small_batch_layer == 1 ? gv_ok && B <= 8 : (opt.small_batch_layer == 0 && gv_ok && B == 1);
     if (p.gv) {
         for (Proj *pr : {&p.qkv, &p.o, &p.gu, &p.down}) {
@@ -324,7 +332,9 @@ Plan make_plan(const corun_model_cfg *c, const corun_kv *kv, int B, const corun_
     }
     const int cap = kv_capacity(kv);
     // batch-invariant mode turns split-KV off: one split covers the capacity
-    p.chunk = bi ? (cap + 63) / 64 * 64 : choose_chunk(B, c->n_kv_heads, cap, opt.attn_chunk);
+    p.chunk = bi ? (cap + 63) / 64 * 64
+              : kv->dtype == CORUN_KV_E4M3 && opt.attn_chunk == 0 ? attn8_chunk(B, c->n_kv_heads, cap)
+              : choose_chunk(B, c->n_kv_heads, cap, opt.attn_chunk);
     p.max_splits = (cap + p.chunk - 1) / p.chunk;
     return p;
 }
@@ -387,6 +397,12 @@ struct corun_engine {
     LaunchRecorder rec;
     std::vector<uint16_t *> kc, vc;
     KvView view{};
+    // caches and rotations of cache.hip: its epilogue in place of the others'
+    // (own_epilogue), its attention where the cache is e4m3
+    bool own_epi = false, e4m3 = false;
+    CacheView cview{};
+    std::vector<CacheLayer> layers;
+    RopeArgs rope_args{};
     // paged caches: the caller's host copy of the page table
     // (corun_engine_set_page_table_host), read by the host-side checks
     // instead of copying the device table back on every call
@@ -478,16 +494,7 @@ extern "C" corun_status corun_check_config(const corun_model_cfg *c, const corun
     if (!(c->rms_eps > 0.f) || !(c->rope_theta > 0.f)) return fail(CORUN_E_SHAPE, "bad eps or rope theta");
     if (B <= 0 || B > 1024) return fail(CORUN_E_SHAPE, "B_fixed must be in [1, 1024]");
     if (kv->n_slots < B) return fail(CORUN_E_CAPACITY, "KV cache has %d slots < B_fixed %d", kv->n_slots, B);
-    if (kv->layout == CORUN_KV_CONTIGUOUS) {
-        if (kv->max_seq_len <= 0 || kv->max_seq_len % 16 != 0)
-            return fail(CORUN_E_CAPACITY, "max_seq_len must be a positive multiple of 16");
-    } else if (kv->layout == CORUN_KV_PAGED) {
-        if (kv->page_size <= 0 || kv->page_size % 16 != 0 || kv->num_pages <= 0 || kv->max_pages_per_seq <= 0)
-            return fail(CORUN_E_CAPACITY, "bad paged-cache geometry (page_size must be a multiple of 16)");
-    } else {
-        return fail(CORUN_E_INVAL, "unknown KV layout %d", kv->layout);
-    }
-    return CORUN_OK;
+    return check_cache(kv);
 }
 
 extern "C" corun_status corun_check_batch(const corun_model_cfg *c, const corun_kv *kv, const int32_t *pt_host,
@@ -515,6 +522,24 @@ extern "C" corun_status corun_check_batch(const corun_model_cfg *c, const corun_
             }
         }
     }
+    return CORUN_OK;
+}
+
+// The rotation and what it and the cache's type exclude.
+static corun_status check_epilogue(const corun_model_cfg *c, const corun_kv *kv, const corun_options &o)
+{
+    if (o.rope) {
+        ST_TRY(check_rope(o.rope));
+        if (o.rope->head_dim != c->head_dim)
+            return fail(CORUN_E_SHAPE, "rope of head_dim %d, model of %d", o.rope->head_dim, c->head_dim);
+    }
+    if (!own_epilogue(kv, o)) return CORUN_OK;
+    if (o.qkv_epilogue == 2 || o.small_batch_layer == 1)
+        return fail(CORUN_E_INVAL, "an e4m3 cache or this rope has a QKV epilogue kernel of its own: not with "
+                    "qkv_epilogue = 2 or small_batch_layer = 1");
+    const long long cap = kv->layout == CORUN_KV_PAGED ? (long long)kv->max_pages_per_seq * kv->page_size : kv->max_seq_len;
+    if (cap > (1 << 30)) return fail(CORUN_E_CAPACITY, "an e4m3 cache or this rope: at most 2^30 tokens to a slot");
+    if (kv->layout == CORUN_KV_PAGED && kv->page_size > (1 << 20)) return fail(CORUN_E_SHAPE, "page_size above 2^20");
     return CORUN_OK;
 }
 
@@ -546,6 +571,8 @@ extern "C" int32_t corun_describe_plan(const corun_model_cfg *c, const corun_kv 
     corun_options o{};
     if (opt) o = *opt;
     s = check_options(o);
+    if (s != CORUN_OK) return s;
+    s = check_epilogue(c, kv, o);
     if (s != CORUN_OK) return s;
     Plan p = make_plan(c, kv, B, o);
     if (o.small_batch_layer == 1 && !p.gv) return fail(CORUN_E_INVAL, "small_batch_layer = 1 needs a dense model, "
@@ -663,10 +690,16 @@ hipError_t gate_up_swiglu(corun_engine *e, const uint16_t *A, int l, const Proj 
 // The wide tiles without split-K apply the epilogue themselves for heads of
 // 128 (the same bits).
 corun_status prefill_qkv(corun_engine *e, int l, const Proj &pr, int rows, const int32_t *pos,
-                         const int32_t *slot_of_row, int slot_const)
+                         const int32_t *slot_of_row, int slot_const, SeqTable &seq)
 {
     const corun_model_cfg &c = e->c;
     const int H = c.hidden, d = c.head_dim, nq = c.n_heads, nkv = c.n_kv_heads, N = (nq + 2 * nkv) * d;
+    if (e->own_epi) {   // the sequences' rows from the partials, in one kernel
+        HIP_TRY(proj(e, e->pf_h, H, W_QKV, l, pr, rows, e->pf_part, (long long)rows * N, N));
+        HIP_TRY(launch_append_seqs(QkvRows{nullptr, e->pf_part, pr.S, (long long)rows * N, N}, seq, nq, nkv, d,
+                                   e->rope_args, e->pf_q, (long long)nq * d, e->cview, e->layers[l], e->st));
+        return CORUN_OK;
+    }
     if (pr.bm >= 128 && pr.bn > 0 && pr.S == 1 && d == 128) {
         const QkvOut out{e->pf_q, e->kc[l], e->vc[l], e->view, pos, slot_of_row, slot_const, nq, nkv, e->rope};
         HIP_TRY(launch_qkv_wide(e->pf_h, H, e->w_qkv[l], shape_of(pr, rows), out, e->st));
@@ -887,10 +920,21 @@ corun_status launch_one(corun_engine *e, int which, int l)
     }
     case CORUN_K_QKV_POST:   // nothing to launch when attention applies the epilogue
         if (e->qkv_in_attn) break;
+        if (e->own_epi) {
+            HIP_TRY(launch_append_rows(QkvRows{nullptr, e->p_qkv, p.qkv.S, (long long)B * nqkv, nqkv}, B, e->d_valid,
+                                       e->d_seq, nq, nkv, d, e->rope_args, e->q, (long long)nq * d, e->cview, e->layers[l],
+                                       st));
+            break;
+        }
         HIP_TRY(launch_qkv_post(e->p_qkv, p.qkv.S, (long long)B * nqkv, B, e->d_valid, e->d_seq, nullptr, -1, nq,
                                 nkv, d, e->rope, e->q, e->kc[l], e->vc[l], e->view, st));
         break;
     case CORUN_K_ATTN_SPLIT:
+        if (e->e4m3) {
+            HIP_TRY(launch_attn8_split(e->q, (long long)nq * d, B, e->d_valid, e->d_seq, 1, nq, nkv, d, e->cview,
+                                       e->layers[l], kv_capacity(&e->kv), p.chunk, e->attn_ws, st, e->d_order));
+            break;
+        }
         HIP_TRY(launch_attn_split(e->q, B, e->d_valid, e->d_seq, nullptr, -1, nq, nkv, d, e->kc[l], e->vc[l],
                                   e->view, p.chunk, p.max_splits, e->attn_ws, st,
                                   e->qkv_in_attn ? QkvIn{e->p_qkv, p.qkv.S, (long long)B * nqkv, e->rope}
@@ -898,6 +942,11 @@ corun_status launch_one(corun_engine *e, int which, int l)
                                   e->d_order));
         break;
     case CORUN_K_ATTN_MERGE:
+        if (e->e4m3) {
+            HIP_TRY(launch_attn8_merge(e->attn_ws, B, e->d_valid, e->d_seq, 1, nq, nkv, d, kv_capacity(&e->kv), p.chunk,
+                                       e->o, (long long)nq * d, st));
+            break;
+        }
         HIP_TRY(launch_attn_merge(e->attn_ws, B, e->d_valid, e->d_seq, nq, nkv, d, p.chunk, p.max_splits, e->o, st));
         break;
     case CORUN_K_O_GEMM: {
@@ -1331,8 +1380,16 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
     corun_options o{};
     if (opt) o = *opt;
     ST_TRY(check_options(o));
+    ST_TRY(check_epilogue(cfg, kv, o));
+    const bool own_epi = own_epilogue(kv, o);
+    std::vector<CacheLayer> layers(own_epi ? cfg->n_layers : 0);
+    for (int l = 0; own_epi && l < cfg->n_layers; ++l) ST_TRY(layer_of(kv, l, &layers[l]));
 
     corun_engine *e = new corun_engine();
+    e->own_epi = own_epi;
+    e->e4m3 = kv->dtype == CORUN_KV_E4M3;
+    e->cview = cache_view(kv);
+    e->layers = layers;
     e->c = *cfg;
     e->kv = *kv;
     e->opt = o;
@@ -1375,7 +1432,18 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
     // partials: one launch fewer, which pays where launches dominate (B = 1:
     // about 3%) and costs where many blocks repeat the work (B = 256: the
     // attention kernel 187 -> 206 us against 7 us for the epilogue kernel).
-    e->qkv_in_attn = !p.gv && (o.qkv_epilogue == 2 || (o.qkv_epilogue == 0 && B <= 8));
+    e->qkv_in_attn = !p.gv && !own_epi && (o.qkv_epilogue == 2 || (o.qkv_epilogue == 0 && B <= 8));
+    corun_rope rope{};
+    if (o.rope) {
+        rope = *o.rope;
+    } else {
+        rope.head_dim = rope.rot_dim = cfg->head_dim;
+        rope.magnitude = 1.f;
+        for (int i = 0; i < cfg->head_dim / 2; ++i)
+            rope.freq[i] = std::pow((double)cfg->rope_theta, -2.0 * i / cfg->head_dim);
+    }
+    e->rope_args = rope_args(rope);
+    e->opt.rope = nullptr;   // read here; the caller's may go
 
     auto bail = [&](corun_status s) {
         corun_engine_destroy(e);
@@ -1456,7 +1524,8 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
     const size_t rope_off = (size_t)((char *)e->rope - e->ws);
     if (launch_fill_u32((uint32_t *)e->ws, (long long)(rope_off / 4), fillv, e->st) != hipSuccess ||
         launch_fill_u32((uint32_t *)e->d_counter, 1, (uint32_t)e->hist_cap, e->st) != hipSuccess ||
-        launch_rope_table(e->rope, rope_len, d, (double)cfg->rope_theta, e->st) != hipSuccess ||
+        (o.rope ? launch_rope_table_of(e->rope, rope_len, d, rope.freq, e->st)
+                : launch_rope_table(e->rope, rope_len, d, (double)cfg->rope_theta, e->st)) != hipSuccess ||
         launch_iota(e->d_order, B, e->st) != hipSuccess)   // a valid row order before the first upload
         return bail(fail(CORUN_E_HIP, "workspace initialisation failed"));
 
@@ -1650,14 +1719,24 @@ extern "C" corun_status corun_prefill_chunk(corun_engine *e, const int32_t *toke
     const int dense_S = e->moe ? 0 : pd.S;
     const MoeBufs pmb = prefill_moe(e, Lp);
     e->pf_trace_rows = Lp;
+    SeqTable table;
+    table.n = 1;
+    table.row0[0] = 0;
+    table.len[0] = Lp;
+    table.start[0] = start;
+    table.slot[0] = slot;
 
     HIP_TRY(hipMemcpyAsync(e->pf_tok, tokens, sizeof(int32_t) * Lp, hipMemcpyHostToDevice, st));
     HIP_TRY(launch_embed(e->embed, e->pf_tok, nullptr, Lp, H, e->pf_x, st));
     for (int l = 0; l < c.n_layers; ++l) {
         HIP_TRY(launch_rmsnorm(e->pf_x, l ? e->pf_part : nullptr, l ? dense_S : 0, (long long)Lp * H, Lp, H,
                                e->attn_norm[l], c.rms_eps, e->pf_h, st, fold_of(e, pmb, l)));
-        ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_pos + start, nullptr, slot));
-        HIP_TRY(launch_prefill_attn(e->pf_q, Lp, start, nq, nkv, d, slot, e->kc[l], e->vc[l], e->view, e->pf_o, st));
+        ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_pos + start, nullptr, slot, table));
+        if (e->e4m3)
+            HIP_TRY(launch_attn8_seqs(e->pf_q, (long long)nq * d, table, nq, nkv, d, e->cview, e->layers[l], e->pf_o,
+                                      (long long)nq * d, st));
+        else
+            HIP_TRY(launch_prefill_attn(e->pf_q, Lp, start, nq, nkv, d, slot, e->kc[l], e->vc[l], e->view, e->pf_o, st));
         HIP_TRY(proj(e, e->pf_o, nq * d, W_O, l, po, Lp, e->pf_part, (long long)Lp * H, H));
         HIP_TRY(launch_rmsnorm(e->pf_x, e->pf_part, po.S, (long long)Lp * H, Lp, H, e->mlp_norm[l], c.rms_eps,
                                e->pf_h, st));
@@ -1754,6 +1833,8 @@ extern "C" corun_status corun_prefill_batch(corun_engine *e, const int32_t *toke
     // every row's position within its prompt and its cache slot; per prompt
     // (first row, length, slot, first attention unit group)
     std::vector<int32_t> rowpos(Lp), rowslot(Lp), seq(4 * n);
+    SeqTable table;
+    table.n = n;
     int groups = 0;
     for (int i = 0, r0 = 0; i < n; r0 += lens[i], ++i) {
         for (int t = 0; t < lens[i]; ++t) {
@@ -1764,6 +1845,10 @@ extern "C" corun_status corun_prefill_batch(corun_engine *e, const int32_t *toke
         seq[4 * i + 1] = lens[i];
         seq[4 * i + 2] = slots[i];
         seq[4 * i + 3] = groups;
+        table.row0[i] = r0;
+        table.len[i] = lens[i];
+        table.start[i] = 0;
+        table.slot[i] = slots[i];
         groups += (((lens[i] + 31) / 32) * G + 7) / 8;
     }
     const PrefillPlan pp = prefill_plan(c, Lp, true);   // batch-invariant: no split-K for any Lp
@@ -1781,9 +1866,13 @@ extern "C" corun_status corun_prefill_batch(corun_engine *e, const int32_t *toke
     for (int l = 0; l < c.n_layers; ++l) {
         HIP_TRY(launch_rmsnorm(e->pf_x, l ? e->pf_part : nullptr, l ? dense_S : 0, (long long)Lp * H, Lp, H,
                                e->attn_norm[l], c.rms_eps, e->pf_h, st, fold_of(e, pmb, l)));
-        ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_rowpos, e->pf_rowslot, -1));
-        HIP_TRY(launch_prefill_attn_multi(e->pf_q, e->pf_seq, n, groups, nq, nkv, d, e->kc[l], e->vc[l], e->view,
-                                          e->pf_o, st));
+        ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_rowpos, e->pf_rowslot, -1, table));
+        if (e->e4m3)
+            HIP_TRY(launch_attn8_seqs(e->pf_q, (long long)nq * d, table, nq, nkv, d, e->cview, e->layers[l], e->pf_o,
+                                      (long long)nq * d, st));
+        else
+            HIP_TRY(launch_prefill_attn_multi(e->pf_q, e->pf_seq, n, groups, nq, nkv, d, e->kc[l], e->vc[l], e->view,
+                                              e->pf_o, st));
         HIP_TRY(proj(e, e->pf_o, nq * d, W_O, l, po, Lp, e->pf_part, (long long)Lp * H, H));
         HIP_TRY(launch_rmsnorm(e->pf_x, e->pf_part, po.S, (long long)Lp * H, Lp, H, e->mlp_norm[l], c.rms_eps,
                                e->pf_h, st));
@@ -1915,12 +2004,16 @@ extern "C" corun_status corun_time_kernel(corun_engine *e, int32_t kernel, int32
     hipEvent_t t0, t1;
     HIP_TRY(hipEventCreate(&t0));
     HIP_TRY(hipEventCreate(&t1));
-    corun_status s = launch_one(e, kernel, layer);   // warm-up
+    // The partials that the workspace holds are the last layer's: appended to
+    // another layer of an e4m3 cache they could move its blocks' scales.
+    const bool append = kernel == CORUN_K_QKV_POST && e->own_epi;
+    auto layer_at = [&](int i) { return append ? e->c.n_layers - 1 : (layer + i) % e->c.n_layers; };
+    corun_status s = launch_one(e, kernel, layer_at(0));   // warm-up
     if (s == CORUN_OK && hipEventRecord(t0, e->st) != hipSuccess) s = fail(CORUN_E_HIP, "event record failed");
     // cycle through the layers so every launch streams its own weights and
     // cache from HBM, as in the step (one layer's weights fit the 256 MB
     // last-level cache, all of them do not)
-    for (int i = 0; s == CORUN_OK && i < n_iters; ++i) s = launch_one(e, kernel, (layer + i) % e->c.n_layers);
+    for (int i = 0; s == CORUN_OK && i < n_iters; ++i) s = launch_one(e, kernel, layer_at(i));
     float ms = 0.f;
     if (s == CORUN_OK) {
         if (hipEventRecord(t1, e->st) != hipSuccess || hipEventSynchronize(t1) != hipSuccess ||

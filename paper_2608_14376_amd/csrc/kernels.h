@@ -362,6 +362,10 @@ struct SeqTable {
     int row0[64], len[64], start[64], slot[64], unit0[64];
 };
 
+// cos / sin table of frequencies freq[i] (radians per position) of the d / 2 half
+// pairs of a head, as launch_rope_table's.
+hipError_t launch_rope_table_of(float2 *tab, int max_pos, int d, const double *freq, hipStream_t st);
+
 // Row r of a decode step (padding rows, valid[r] == 0, skipped): q heads
 // rotated at position pos[r] to q [rows][ldq], the rotated k and the v heads
 // appended at that position of slot r.  A row whose position or page is
@@ -377,18 +381,15 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
 // Attention of row r's query heads over tokens 0 .. lens[r] - 1 of slot r of
 // an e4m3 cache (lens[r] = pos[r] + 1 where plus_one): out rows of padding
 // rows and of empty ones are zero, of rows whose length or pages are outside
-// the cache or max_len NaN.  Split over the tokens, then merged; ws:
-// attn8_workspace floats; workgroups take the rows in row_order if given.
-size_t attn8_workspace(int rows, int nq, int nkv, int d, int max_len);
+// the cache or max_len NaN.  Split over the tokens in chunks (attn8_chunk, or
+// any multiple of 64), then merged; ws: [rows][nkv][ceil(max_len / chunk)][G (d +
+// 2)] floats; workgroups take the rows in row_order if given.
+int attn8_chunk(int rows, int nkv, int max_len);
 hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
                               int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                              float *ws, hipStream_t st, const int32_t *row_order = nullptr);
+                              int chunk, float *ws, hipStream_t st, const int32_t *row_order = nullptr);
 hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, const int32_t *lens, int plus_one, int nq,
-                              int nkv, int d, int max_len, uint16_t *out, long long ldo, hipStream_t st);
-// Both.
-hipError_t launch_attn8_rows(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
-                             int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                             float *ws, uint16_t *out, long long ldo, hipStream_t st, const int32_t *row_order = nullptr);
+                              int nkv, int d, int max_len, int chunk, uint16_t *out, long long ldo, hipStream_t st);
 // Causal attention of a prefill call's queries: row row0 + t of sequence i
 // sees tokens 0 .. start + t of its slot.
 hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
