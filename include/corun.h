@@ -337,7 +337,7 @@ corun_status corun_rope_init(const corun_rope_cfg *cfg, corun_rope *out);
  * heads, then k, then v).  Live rows get their q and k heads rotated by their
  * position, q [rows, n_heads head_dim] written, and k and v appended at
  * that position of layer `layer` of slot r, whose earlier positions the
- * caller has filled.  Nothing of a padding row is read or written.
+ * caller has filled.  Nothing of a padding row is used or written.
  *  valid      uint8 [rows], or NULL: all rows are live
  *  positions  int32 [rows]
  * A live row whose position is outside [0, capacity), or whose page is outside

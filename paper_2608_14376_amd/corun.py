@@ -332,7 +332,9 @@ class KvCache:
         if page_table is not None and (page_table.dtype != torch.int32 or page_table.dim() != 2 or
                                        not page_table.is_contiguous() or page_table.device != self.device):
             raise ValueError("page_table: contiguous int32 [n_slots, max_pages_per_seq] on the cache's device")
-        self.layers = len(k)
+        self.layers, self.index = len(k), k[0].get_device()
+        global _torch
+        _torch = _torch or _Torch()
         self._keep = keep = [k, v, k_scale, v_scale, page_table]
         if page_table is None:
             self.kv = kv_struct(KV_CONTIGUOUS, n, k, v, keep, max_seq_len=tokens)
@@ -345,6 +347,9 @@ class KvCache:
         self._at = C.addressof(self.kv)
 
 
+# The operators' argument checks.  A call on one token takes a few microseconds
+# on the GPU, so they look at each tensor's attributes once.
+
 def _layer(cache, layer):
     if not 0 <= layer < cache.layers:
         raise ValueError(f"layer {layer} of {cache.layers}")
@@ -353,12 +358,13 @@ def _layer(cache, layer):
 
 def _rows(cache, t, name):
     """(rows, row width, row stride) of a 2-D or 3-D bf16 tensor of head rows."""
-    import torch
-    if t.dtype != torch.bfloat16 or t.device != cache.device or t.dim() not in (2, 3) or t.stride(-1) != 1 or \
-            (t.dim() == 3 and t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+    shape, stride = t.shape, t.stride()
+    n = len(shape)
+    if t.dtype is not _torch.bf16 or t.get_device() != cache.index or n not in (2, 3) or stride[-1] != 1 or \
+            (n == 3 and shape[1] > 1 and stride[1] != shape[2]):
         raise ValueError(f"{name}: bf16 rows of heads on {cache.device}, the elements of a row contiguous")
-    width = t.shape[1] if t.dim() == 2 else t.shape[1] * t.shape[2]
-    return t.shape[0], width, (t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0)))
+    width = shape[1] if n == 2 else shape[1] * shape[2]
+    return shape[0], width, (stride[0] if shape[0] > 1 else max(width, stride[0]))
 
 
 def _heads(cache, width, name):
@@ -367,17 +373,32 @@ def _heads(cache, width, name):
     return width // cache.head_dim
 
 
-def _vec(cache, t, dtype, n, name):
-    if t.dtype not in dtype or t.device != cache.device or tuple(t.shape) != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {dtype[0]} [{n}] on {cache.device}")
+def _vec(cache, t, dtypes, n, name):
+    if t.dtype not in dtypes or t.get_device() != cache.index or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtypes[0]} [{n}] on {cache.device}")
     return t.data_ptr()
 
 
 def _stream(cache, stream):
-    import torch
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if cache.index != _torch.device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{_torch.device()}")
+    return _torch.stream(cache.index) if stream is None else stream.cuda_stream
+
+
+class _Torch:
+    """What the operators' checks take from torch, which this module imports
+    only where it is used.  The current stream's handle comes from torch's own
+    accessor where there is one: building a Stream object costs 3 us."""
+
+    def __init__(self):
+        import torch
+        self.bf16, self.ints, self.flags = torch.bfloat16, (torch.int32,), (torch.uint8, torch.bool)
+        self.device = torch.cuda.current_device
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_torch = None
 
 
 def _append_rows(cache, qkv, q, rope):
@@ -396,10 +417,9 @@ def decode_append(cache, layer, qkv, positions, rope, q, valid=None, stream=None
     QKV rows (bf16 [rows, (n_heads + 2 n_kv_heads) head_dim], row r = slot r) at
     positions (device int32 [rows]), write q (bf16 [rows, n_heads head_dim]),
     append k and v.  valid: device uint8 [rows].  Does not wait."""
-    import torch
     rows, nq, ld, ldq = _append_rows(cache, qkv, q, rope)
-    pos = _vec(cache, positions, (torch.int32,), rows, "positions")
-    vm = None if valid is None else _vec(cache, valid, (torch.uint8, torch.bool), rows, "valid")
+    pos = _vec(cache, positions, _torch.ints, rows, "positions")
+    vm = None if valid is None else _vec(cache, valid, _torch.flags, rows, "valid")
     _check(load().corun_decode_append(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, C.addressof(rope), rows,
                                       qkv.data_ptr(), ld, vm, pos, q.data_ptr(), ldq, _stream(cache, stream)))
 
@@ -409,8 +429,9 @@ def _sequences(lens, starts, slots, rows):
     sr = None if starts is None else _np(starts, np.int32)
     if ln.ndim != 1 or sl.shape != ln.shape or (sr is not None and sr.shape != ln.shape):
         raise ValueError("lens, starts and slots: one entry for each sequence")
-    if int(ln.sum(dtype=np.int64)) != rows:
-        raise ValueError(f"the sequences have {int(ln.sum(dtype=np.int64))} tokens, the tensors {rows} rows")
+    total = int(ln.sum(dtype=np.int64))
+    if total != rows:
+        raise ValueError(f"the sequences have {total} tokens, the tensors {rows} rows")
     return ln, sr, sl
 
 
@@ -445,15 +466,14 @@ def decode_attention(cache, layer, q, lens, out, ws, valid=None, max_len=0, stre
     [rows, n_heads head_dim]) over the first lens[r] (device int32 [rows])
     tokens of slot r of an e4m3 cache.  ws: a device uint8 tensor of
     decode_attention_workspace bytes, not shared by calls that may overlap."""
-    import torch
     rows, nq, ldq, ldo = _attention_rows(cache, q, out)
-    ln = _vec(cache, lens, (torch.int32,), rows, "lens")
-    vm = None if valid is None else _vec(cache, valid, (torch.uint8, torch.bool), rows, "valid")
-    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != cache.device:
-        raise ValueError(f"ws: contiguous uint8 on {cache.device}")
+    ln = _vec(cache, lens, _torch.ints, rows, "lens")
+    vm = None if valid is None else _vec(cache, valid, _torch.flags, rows, "valid")
+    size = ws.numel()
+    wp = _vec(cache, ws, _torch.flags[:1], size, "ws")
     _check(load().corun_decode_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, rows,
-                                         q.data_ptr(), ldq, vm, ln, max_len, out.data_ptr(), ldo, ws.data_ptr(),
-                                         ws.numel(), _stream(cache, stream)))
+                                         q.data_ptr(), ldq, vm, ln, max_len, out.data_ptr(), ldo, wp, size,
+                                         _stream(cache, stream)))
 
 
 def prefill_attention(cache, layer, q, lens, starts, slots, out, stream=None) -> None:

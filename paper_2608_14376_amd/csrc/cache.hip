@@ -18,6 +18,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "kernels.h"
@@ -130,109 +131,79 @@ __device__ __forceinline__ float to_odd(double y)
 // sines while it goes from head to head: two runs of eight elements from a0 and
 // b0 on, (8 j, 8 j + rot / 2) for rotated half pairs, otherwise the 16
 // elements from 16 j on, whose pairs stand side by side.  Half pairs of a rot
-// that is no multiple of 16 are read one element at a time.
+// that is no multiple of 16 are read one element at a time (VEC false).
+//
+// q is rotated in fp32 (its output rounding is 2^-8).  k goes to codes from a
+// 64-bit rotation rounded to odd, so that a code is the nearest one to the exact
+// product however close it is to a tie; the matrix-free fp64 rate is the fp32
+// rate here, and only the kv heads take it.
 // ---------------------------------------------------------------------------
-template <int D>
+template <bool VEC>
 struct Pairs {
-    int a0, b0, first, rot2;       // first pair; rotated pairs of the head
-    bool half, vec;
-    float c[8], s[8];
-    double cd[8], sd[8];
+    int a0, b0, first, rot2;       // runs; first pair; rotated pairs of the head
+    bool half;
 
+    __device__ __forceinline__ Pairs(const RopeArgs &r, int j)
+    {
+        first = 8 * j;
+        rot2 = r.rot / 2;
+        half = !r.interleaved && first < rot2;
+        a0 = half ? 8 * j : 16 * j;
+        b0 = half ? 8 * j + rot2 : 16 * j + 8;
+    }
     __device__ __forceinline__ bool rotated(int t) const { return first + t < rot2; }
-    // element offsets of pair t where vec does not hold
+    // element offsets of pair t where the runs do not hold it
     __device__ __forceinline__ int at(int t, int which) const
     {
         const int i = first + t;
         return i < rot2 ? i + which * rot2 : 2 * i + which;
     }
-    __device__ __forceinline__ void init(const RopeArgs &r, int j, int pos)
-    {
-        first = 8 * j;
-        rot2 = r.rot / 2;
-        half = !r.interleaved && first < rot2;
-        vec = r.interleaved || r.rot % 16 == 0;
-        a0 = half ? 8 * j : 16 * j;
-        b0 = half ? 8 * j + rot2 : 16 * j + 8;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            turn_cos_sin(r.turns[first + t], (double)pos, cd[t], sd[t]);
-            cd[t] *= r.mag;
-            sd[t] *= r.mag;
-            c[t] = (float)cd[t];
-            s[t] = (float)sd[t];
-        }
-    }
-    __device__ __forceinline__ void rotate(const float *x0, const float *x1, float *y0, float *y1) const
+};
+
+// Cosines and sines of a thread's pairs at a position.
+struct Turn64 {
+    double c[8], s[8];
+    __device__ __forceinline__ void init(const RopeArgs &r, int first, int pos)
     {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            y0[t] = rotated(t) ? __builtin_fmaf(x0[t], c[t], -(x1[t] * s[t])) : x0[t];
-            y1[t] = rotated(t) ? __builtin_fmaf(x1[t], c[t], x0[t] * s[t]) : x1[t];
-        }
-    }
-    __device__ __forceinline__ void rotate_exact(const float *x0, const float *x1, float *y0, float *y1) const
-    {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const double u = x0[t], w = x1[t];
-            y0[t] = rotated(t) ? to_odd(__builtin_fma(u, cd[t], -(w * sd[t]))) : x0[t];
-            y1[t] = rotated(t) ? to_odd(__builtin_fma(w, cd[t], u * sd[t])) : x1[t];
-        }
-    }
-    // runs of eight elements <-> pairs: run A holds the pairs' first elements
-    // and run B the second (half), or the two runs hold the pairs in turn
-    __device__ __forceinline__ void to_pairs(const float *e, float *x0, float *x1) const
-    {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            x0[t] = half ? e[t] : e[2 * t];
-            x1[t] = half ? e[8 + t] : e[2 * t + 1];
-        }
-    }
-    __device__ __forceinline__ void from_pairs(const float *x0, const float *x1, float *e) const
-    {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            e[t] = half ? x0[t] : (t & 1 ? x1[t / 2] : x0[t / 2]);
-            e[8 + t] = half ? x1[t] : (t & 1 ? x1[4 + t / 2] : x0[4 + t / 2]);
+            turn_cos_sin(r.turns[first + t], (double)pos, c[t], s[t]);
+            c[t] *= r.mag;
+            s[t] *= r.mag;
         }
     }
 };
 
-template <int D>
-__device__ __forceinline__ void load_pairs(const QkvRows &in, const Pairs<D> &p, long long row, int head, float *x0, float *x1)
+// What a thread loads of a head, as loaded: 16 bf16 values (fp32 partials are
+// summed and rounded).  Pair t of a VEC thread: elements t and 8 + t (half), or
+// 2 t and 2 t + 1.
+struct Raw {
+    uint32_t w[8];
+};
+
+template <int D, bool VEC>
+__device__ __forceinline__ Raw load_raw(const QkvRows &in, const Pairs<VEC> &p, long long row, int head)
 {
     const size_t off = (size_t)row * in.ld + (size_t)head * D;
-    if (!p.vec) {
+    Raw r;
+    if (in.bf16 != nullptr) {
+        const uint16_t *src = in.bf16 + off;
+        if constexpr (VEC) {
+            const uint4 a = *(const uint4 *)(src + p.a0), b = *(const uint4 *)(src + p.b0);
+            r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+            r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+        } else {
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                float x = 0.f;
-                if (in.bf16 != nullptr) x = bf2f(in.bf16[off + p.at(t, w)]);
-                else {
-                    for (int sp = 0; sp < in.S; ++sp) x += in.part[sp * in.stride + off + p.at(t, w)];
-                    x = bf2f(f2bf(x));
-                }
-                (w ? x1 : x0)[t] = x;
-            }
-        return;
+            for (int t = 0; t < 8; ++t) r.w[t] = (uint32_t)src[p.at(t, 0)] | ((uint32_t)src[p.at(t, 1)] << 16);
+        }
+        return r;
     }
     float e[16];
-    if (in.bf16 != nullptr) {
-        const uint4 a = *(const uint4 *)(in.bf16 + off + p.a0), b = *(const uint4 *)(in.bf16 + off + p.b0);
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            e[2 * i] = __uint_as_float(w[i] << 16);
-            e[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = 0.f;
-        for (int sp = 0; sp < in.S; ++sp) {
-            const float *src = in.part + sp * in.stride + off;
+    for (int i = 0; i < 16; ++i) e[i] = 0.f;
+    for (int sp = 0; sp < in.S; ++sp) {
+        const float *src = in.part + sp * in.stride + off;
+        if constexpr (VEC) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float4 f = *(const float4 *)(src + (i < 2 ? p.a0 : p.b0) + 4 * (i & 1));
@@ -241,50 +212,111 @@ __device__ __forceinline__ void load_pairs(const QkvRows &in, const Pairs<D> &p,
                 e[4 * i + 2] += f.z;
                 e[4 * i + 3] += f.w;
             }
-        }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] = bf2f(f2bf(e[i]));
+            for (int t = 0; t < 8; ++t) {
+                e[2 * t] += src[p.at(t, 0)];
+                e[2 * t + 1] += src[p.at(t, 1)];
+            }
+        }
     }
-    p.to_pairs(e, x0, x1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.w[i] = f2bf2(e[2 * i], e[2 * i + 1]);
+    return r;
 }
 
-template <int D>
-__device__ __forceinline__ void store_bf16(uint16_t *dst, const Pairs<D> &p, const float *y0, const float *y1)
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The pairs' first and second elements.
+template <bool VEC>
+__device__ __forceinline__ void to_pairs(const Raw &r, const Pairs<VEC> &p, float (&x0)[8], float (&x1)[8])
 {
-    if (!p.vec) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        if (VEC && p.half) {
+            x0[t] = t & 1 ? hi_f(r.w[t / 2]) : lo_f(r.w[t / 2]);
+            x1[t] = t & 1 ? hi_f(r.w[4 + t / 2]) : lo_f(r.w[4 + t / 2]);
+        } else {
+            x0[t] = lo_f(r.w[t]);
+            x1[t] = hi_f(r.w[t]);
+        }
+    }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void rotate(const Pairs<VEC> &p, const float (&c)[8], const float (&s)[8], float (&x0)[8],
+                                       float (&x1)[8])
+{
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const float y0 = __builtin_fmaf(x0[t], c[t], -(x1[t] * s[t])), y1 = __builtin_fmaf(x1[t], c[t], x0[t] * s[t]);
+        x0[t] = p.rotated(t) ? y0 : x0[t];
+        x1[t] = p.rotated(t) ? y1 : x1[t];
+    }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void rotate_exact(const Pairs<VEC> &p, const Turn64 &tu, float (&x0)[8], float (&x1)[8])
+{
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const double u = x0[t], w = x1[t];
+        const float y0 = to_odd(__builtin_fma(u, tu.c[t], -(w * tu.s[t]))), y1 = to_odd(__builtin_fma(w, tu.c[t], u * tu.s[t]));
+        x0[t] = p.rotated(t) ? y0 : x0[t];
+        x1[t] = p.rotated(t) ? y1 : x1[t];
+    }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void store_bf16(uint16_t *dst, const Pairs<VEC> &p, const float (&y0)[8], const float (&y1)[8])
+{
+    if constexpr (!VEC) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             dst[p.at(t, 0)] = f2bf(y0[t]);
             dst[p.at(t, 1)] = f2bf(y1[t]);
         }
-        return;
+    } else {
+        uint32_t w[8];
+        if (p.half) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                w[t] = f2bf2(y0[2 * t], y0[2 * t + 1]);
+                w[4 + t] = f2bf2(y1[2 * t], y1[2 * t + 1]);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) w[t] = f2bf2(y0[t], y1[t]);
+        }
+        *(uint4 *)(dst + p.a0) = (uint4){w[0], w[1], w[2], w[3]};
+        *(uint4 *)(dst + p.b0) = (uint4){w[4], w[5], w[6], w[7]};
     }
-    float e[16];
-    p.from_pairs(y0, y1, e);
-    *(uint4 *)(dst + p.a0) = (uint4){f2bf2(e[0], e[1]), f2bf2(e[2], e[3]), f2bf2(e[4], e[5]), f2bf2(e[6], e[7])};
-    *(uint4 *)(dst + p.b0) = (uint4){f2bf2(e[8], e[9]), f2bf2(e[10], e[11]), f2bf2(e[12], e[13]), f2bf2(e[14], e[15])};
 }
 
-template <int D>
-__device__ __forceinline__ void store_codes(uint8_t *dst, const Pairs<D> &p, const float *y0, const float *y1, int e_)
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t *dst, const Pairs<VEC> &p, const float (&y0)[8], const float (&y1)[8],
+                                            int e)
 {
-    const float m = exp2_int(-e_);
-    if (!p.vec) {
+    const float m = exp2_int(-e);
+    if constexpr (!VEC) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             const uint32_t w = encode4(y0[t], y1[t], 0.f, 0.f, m);
             dst[p.at(t, 0)] = (uint8_t)w;
             dst[p.at(t, 1)] = (uint8_t)(w >> 8);
         }
-        return;
+    } else if (p.half) {
+        *(uint2 *)(dst + p.a0) = (uint2){encode4(y0[0], y0[1], y0[2], y0[3], m), encode4(y0[4], y0[5], y0[6], y0[7], m)};
+        *(uint2 *)(dst + p.b0) = (uint2){encode4(y1[0], y1[1], y1[2], y1[3], m), encode4(y1[4], y1[5], y1[6], y1[7], m)};
+    } else {
+        *(uint4 *)(dst + p.a0) =
+            (uint4){encode4(y0[0], y1[0], y0[1], y1[1], m), encode4(y0[2], y1[2], y0[3], y1[3], m),
+                    encode4(y0[4], y1[4], y0[5], y1[5], m), encode4(y0[6], y1[6], y0[7], y1[7], m)};
     }
-    float e[16];
-    p.from_pairs(y0, y1, e);
-    *(uint2 *)(dst + p.a0) = (uint2){encode4(e[0], e[1], e[2], e[3], m), encode4(e[4], e[5], e[6], e[7], m)};
-    *(uint2 *)(dst + p.b0) = (uint2){encode4(e[8], e[9], e[10], e[11], m), encode4(e[12], e[13], e[14], e[15], m)};
 }
 
-__device__ __forceinline__ uint32_t top_of(const float *y0, const float *y1)
+__device__ __forceinline__ uint32_t top_of(const float (&y0)[8], const float (&y1)[8])
 {
     uint32_t u = 0u;
 #pragma unroll
@@ -292,10 +324,17 @@ __device__ __forceinline__ uint32_t top_of(const float *y0, const float *y1)
     return u;
 }
 
+__device__ __forceinline__ uint4 rescale16(uint4 v, float m)
+{
+    return (uint4){rescale4(v.x, m), rescale4(v.y, m), rescale4(v.z, m), rescale4(v.w, m)};
+}
+
 constexpr float QNAN = __builtin_nanf("");
 
-// One decode step's rows: D / 16 threads to a (row, head).
-template <int D>
+// One decode step's rows: D / 16 threads to a (row, head).  What does not wait
+// for the position (the values, the row's flags) is loaded first: one short
+// chain of latencies is the whole time of a small batch.
+template <int D, bool VEC, bool E4>
 __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const uint8_t *__restrict__ valid,
                                                      const int32_t *__restrict__ pos, int nq, int nkv, RopeArgs rope,
                                                      uint16_t *__restrict__ q, long long ldq, CacheView cv, CacheLayer cl)
@@ -303,43 +342,47 @@ __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const
     constexpr int LPT = D / 16;
     const int unit = (blockIdx.x * 256 + threadIdx.x) / LPT, j = threadIdx.x % LPT;
     const int nh = nq + 2 * nkv, r = unit / nh, h = unit % nh;
-    if (r >= rows || (valid != nullptr && !valid[r])) return;
+    if (r >= rows) return;
+    const uint8_t live = valid != nullptr ? valid[r] : 1;
     const int t = pos[r];
+    if (!live) return;                                // nothing of a padding row is read
+    const Pairs<VEC> p(rope, j);
+    const Raw raw = load_raw<D, VEC>(in, p, r, h);
     bool bad = t < 0 || t >= cv.cap;
     int page = 0;
     if (!bad && cv.kv.layout == 1) {
         page = page_of(cv, r, t);
         bad = page < 0;
     }
-    Pairs<D> p;
-    float x0[8], x1[8], y0[8], y1[8];
-    p.init(rope, j, t);
-    load_pairs<D>(in, p, r, h, x0, x1);
+    Turn64 tu;
+    const bool key = h >= nq && h < nq + nkv;
+    if (h < nq + nkv) tu.init(rope, p.first, t);
+    float x0[8], x1[8];
+    to_pairs(raw, p, x0, x1);
+    if (h < nq || (key && !E4)) {
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            c[i] = (float)tu.c[i];
+            s[i] = (float)tu.s[i];
+        }
+        rotate(p, c, s, x0, x1);
+    }
     if (h < nq) {
-        p.rotate(x0, x1, y0, y1);
         if (bad)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y0[i] = y1[i] = QNAN;
-        store_bf16<D>(q + (size_t)r * ldq + (size_t)h * D, p, y0, y1);
+            for (int i = 0; i < 8; ++i) x0[i] = x1[i] = QNAN;
+        store_bf16(q + (size_t)r * ldq + (size_t)h * D, p, x0, x1);
         return;
     }
     if (bad) return;
-    const bool key = h < nq + nkv;
     const int kvh = h - nq - (key ? 0 : nkv);
     const Place pl = place(cv, nkv, kvh, r, page, t);
-    if (!cv.e4m3) {
-        if (key) p.rotate(x0, x1, y0, y1);
-        store_bf16<D>((uint16_t *)(key ? cl.k : cl.v) + pl.row * D, p, key ? y0 : x0, key ? y1 : x1);
+    if constexpr (!E4) {
+        store_bf16((uint16_t *)(key ? cl.k : cl.v) + pl.row * D, p, x0, x1);
         return;
     }
-    if (key) {
-        p.rotate_exact(x0, x1, y0, y1);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x0[i] = y0[i];
-            x1[i] = y1[i];
-        }
-    }
+    if (key) rotate_exact(p, tu, x0, x1);
     uint8_t *codes = (uint8_t *)(key ? cl.k : cl.v) + pl.row * D;
     uint8_t *scale = (key ? cl.ks : cl.vs) + pl.blk;
     uint32_t top = top_of(x0, x1);
@@ -347,19 +390,19 @@ __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const
     for (int o = 1; o < LPT; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o, LPT));
     const int kept = t & ((1 << cv.blk_shift) - 1);
     const int need = scale_exp(top), old = kept ? (int)*scale - 127 : need, e = max(old, need);
-    if (old < e) {   // the block's earlier tokens move to the larger scale
+    store_codes(codes, p, x0, x1, e);
+    if (old < e) {   // the block's earlier tokens move to the larger scale, four of them in flight
         const float m = e - old > 120 ? 0.f : exp2_int(old - e);
-        for (int i = 1; i <= kept; ++i) {
-            uint4 *w = (uint4 *)(codes - (size_t)i * D + 16 * j);
-            uint4 v = *w;
-            v.x = rescale4(v.x, m);
-            v.y = rescale4(v.y, m);
-            v.z = rescale4(v.z, m);
-            v.w = rescale4(v.w, m);
-            *w = v;
+        for (int i = 1; i <= kept; i += 4) {
+            uint4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u <= kept) v[u] = *(const uint4 *)(codes - (size_t)(i + u) * D + 16 * j);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u <= kept) *(uint4 *)(codes - (size_t)(i + u) * D + 16 * j) = rescale16(v[u], m);
         }
     }
-    store_codes<D>(codes, p, x0, x1, e);
     if (j == 0 && (kept == 0 || e != old)) *scale = (uint8_t)(e + 127);
 }
 
@@ -367,8 +410,9 @@ __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const
 // sequence (x), a slice of the heads (y); thread (head group, token, j), so
 // that a head group's wavefronts hold every new token of the block and agree
 // on its scale through LDS, once per pair of key and value heads.  Threads of
-// the block's earlier tokens move those to a scale that grew.
-template <int D>
+// the block's earlier tokens move those to a scale that grew.  The query heads
+// follow, four loads in flight to a thread.
+template <int D, bool VEC, bool E4>
 __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, int nq, int nkv, RopeArgs rope,
                                                      uint16_t *__restrict__ q, long long ldq, CacheView cv, CacheLayer cl)
 {
@@ -388,96 +432,110 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
         page = page_of(cv, slot, t0);
         bad = page < 0;
     }
-    Pairs<D> p;
-    p.init(rope, j, t);
-    float x0[8], x1[8], y0[8], y1[8];
-    // query heads of this slice
-    const int ns = gridDim.y, sl = blockIdx.y;
-    const int q_lo = (int)((long long)nq * sl / ns), q_hi = (int)((long long)nq * (sl + 1) / ns);
-    if (fresh)
-        for (int h = q_lo + hg; h < q_hi; h += groups) {
-            load_pairs<D>(in, p, row, h, x0, x1);
-            p.rotate(x0, x1, y0, y1);
-            if (bad)
+    const Pairs<VEC> p(rope, j);
+    Turn64 tu;
+    tu.init(rope, p.first, t);
+    float c[8], s[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) y0[u] = y1[u] = QNAN;
-            store_bf16<D>(q + (size_t)row * ldq + (size_t)h * D, p, y0, y1);
-        }
-    if (bad) return;
+    for (int u = 0; u < 8; ++u) {
+        c[u] = (float)tu.c[u];
+        s[u] = (float)tu.s[u];
+    }
+    const int ns = gridDim.y, sl = blockIdx.y;
     const int k_lo = (int)((long long)nkv * sl / ns), k_hi = (int)((long long)nkv * (sl + 1) / ns);
-    if (!cv.e4m3) {
-        if (fresh)
+    if constexpr (!E4) {
+        if (fresh && !bad)
             for (int h = k_lo + hg; h < k_hi; h += groups) {
                 const Place pl = place(cv, nkv, h, slot, page, t);
-                load_pairs<D>(in, p, row, nq + h, x0, x1);
-                p.rotate(x0, x1, y0, y1);
-                store_bf16<D>((uint16_t *)cl.k + pl.row * D, p, y0, y1);
-                load_pairs<D>(in, p, row, nq + nkv + h, x0, x1);
-                store_bf16<D>((uint16_t *)cl.v + pl.row * D, p, x0, x1);
+                const Raw rk = load_raw<D, VEC>(in, p, row, nq + h), rv = load_raw<D, VEC>(in, p, row, nq + nkv + h);
+                float x0[8], x1[8];
+                to_pairs(rk, p, x0, x1);
+                rotate(p, c, s, x0, x1);
+                store_bf16((uint16_t *)cl.k + pl.row * D, p, x0, x1);
+                to_pairs(rv, p, x0, x1);
+                store_bf16((uint16_t *)cl.v + pl.row * D, p, x0, x1);
             }
-        return;
-    }
-    __shared__ uint32_t tops[2][8][2];
-    const int kept = max(0, start - t0);              // earlier tokens of the block
-    const int wave = tid >> 6, gw = gt / 64;          // wavefronts of a head group
-    const int per = (k_hi - k_lo + groups - 1) / groups;
-    for (int it = 0; it < per; ++it) {
-        const int h = k_lo + hg + it * groups;
-        const bool on = h < k_hi;
-        uint32_t tk = 0u, tv = 0u;
-        if (on && fresh) {
-            load_pairs<D>(in, p, row, nq + h, x0, x1);
-            p.rotate_exact(x0, x1, y0, y1);
-            load_pairs<D>(in, p, row, nq + nkv + h, x0, x1);
-            tk = top_of(y0, y1);
-            tv = top_of(x0, x1);
-        }
+    } else if (!bad) {                                // bad is uniform, as are the barriers
+        __shared__ uint32_t tops[2][8][2];
+        const int kept = max(0, start - t0);          // earlier tokens of the block
+        const int wave = tid >> 6, gw = gt / 64;      // wavefronts of a head group
+        const int per = (k_hi - k_lo + groups - 1) / groups;
+        for (int it = 0; it < per; ++it) {
+            const int h = k_lo + hg + it * groups;
+            const bool on = h < k_hi;
+            uint32_t tk = 0u, tv = 0u;
+            float x0[8], x1[8], y0[8], y1[8];
+            if (on && fresh) {
+                const Raw rk = load_raw<D, VEC>(in, p, row, nq + h), rv = load_raw<D, VEC>(in, p, row, nq + nkv + h);
+                to_pairs(rk, p, y0, y1);
+                rotate_exact(p, tu, y0, y1);
+                to_pairs(rv, p, x0, x1);
+                tk = top_of(y0, y1);
+                tv = top_of(x0, x1);
+            }
 #pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            tk = max(tk, (uint32_t)__shfl_xor((int)tk, o, 64));
-            tv = max(tv, (uint32_t)__shfl_xor((int)tv, o, 64));
-        }
-        if ((tid & 63) == 0) {
-            tops[it & 1][wave][0] = tk;
-            tops[it & 1][wave][1] = tv;
-        }
-        __syncthreads();                              // the other buffer's readers passed the last one
-        for (int w = 0; w < gw; ++w) {
-            tk = max(tk, tops[it & 1][hg * gw + w][0]);
-            tv = max(tv, tops[it & 1][hg * gw + w][1]);
-        }
-        int ok = 0, ov = 0, ek = 0, ev = 0;
-        const Place pl = place(cv, nkv, on ? h : k_lo, slot, page, t);
-        if (on) {
-            ek = scale_exp(tk);
-            ev = scale_exp(tv);
-            ok = kept ? (int)cl.ks[pl.blk] - 127 : ek;
-            ov = kept ? (int)cl.vs[pl.blk] - 127 : ev;
-            ek = max(ok, ek);
-            ev = max(ov, ev);
-            uint8_t *ck = (uint8_t *)cl.k + pl.row * D, *vk = (uint8_t *)cl.v + pl.row * D;
-            if (fresh) {
-                store_codes<D>(ck, p, y0, y1, ek);
-                store_codes<D>(vk, p, x0, x1, ev);
-            } else if (tok < kept) {
-                auto move = [&](uint8_t *c, int old, int e) {
-                    if (old >= e) return;
-                    const float m = e - old > 120 ? 0.f : exp2_int(old - e);
-                    uint4 v = *(uint4 *)(c + 16 * j);
-                    v.x = rescale4(v.x, m);
-                    v.y = rescale4(v.y, m);
-                    v.z = rescale4(v.z, m);
-                    v.w = rescale4(v.w, m);
-                    *(uint4 *)(c + 16 * j) = v;
-                };
-                move(ck, ok, ek);
-                move(vk, ov, ev);
+            for (int o = 1; o < 64; o *= 2) {
+                tk = max(tk, (uint32_t)__shfl_xor((int)tk, o, 64));
+                tv = max(tv, (uint32_t)__shfl_xor((int)tv, o, 64));
+            }
+            if ((tid & 63) == 0) {
+                tops[it & 1][wave][0] = tk;
+                tops[it & 1][wave][1] = tv;
+            }
+            __syncthreads();                          // the other buffer's readers passed the last one
+            for (int w = 0; w < gw; ++w) {
+                tk = max(tk, tops[it & 1][hg * gw + w][0]);
+                tv = max(tv, tops[it & 1][hg * gw + w][1]);
+            }
+            int ok = 0, ov = 0, ek = 0, ev = 0;
+            const Place pl = place(cv, nkv, on ? h : k_lo, slot, page, t);
+            if (on) {
+                ek = scale_exp(tk);
+                ev = scale_exp(tv);
+                ok = kept ? (int)cl.ks[pl.blk] - 127 : ek;
+                ov = kept ? (int)cl.vs[pl.blk] - 127 : ev;
+                ek = max(ok, ek);
+                ev = max(ov, ev);
+                uint8_t *ck = (uint8_t *)cl.k + pl.row * D, *vk = (uint8_t *)cl.v + pl.row * D;
+                if (fresh) {
+                    store_codes(ck, p, y0, y1, ek);
+                    store_codes(vk, p, x0, x1, ev);
+                } else if (tok < kept) {
+                    auto move = [&](uint8_t *at, int old, int e) {
+                        if (old >= e) return;
+                        const float m = e - old > 120 ? 0.f : exp2_int(old - e);
+                        *(uint4 *)(at + 16 * j) = rescale16(*(const uint4 *)(at + 16 * j), m);
+                    };
+                    move(ck, ok, ek);
+                    move(vk, ov, ev);
+                }
+            }
+            if (kept) __syncthreads();                // every thread of a group has read the old scales (kept is uniform)
+            if (on && tid % gt == 0) {
+                cl.ks[pl.blk] = (uint8_t)(ek + 127);
+                cl.vs[pl.blk] = (uint8_t)(ev + 127);
             }
         }
-        if (kept) __syncthreads();                    // every thread of a group has read the old scales (kept is uniform)
-        if (on && tid % gt == 0) {
-            cl.ks[pl.blk] = (uint8_t)(ek + 127);
-            cl.vs[pl.blk] = (uint8_t)(ev + 127);
+    }
+    // query heads of this slice
+    if (!fresh) return;
+    const int q_lo = (int)((long long)nq * sl / ns), q_hi = (int)((long long)nq * (sl + 1) / ns);
+    constexpr int PF = 4;
+    for (int h = q_lo + hg; h < q_hi; h += PF * groups) {
+        Raw raw[PF];
+#pragma unroll
+        for (int u = 0; u < PF; ++u)
+            if (h + u * groups < q_hi) raw[u] = load_raw<D, VEC>(in, p, row, h + u * groups);
+#pragma unroll
+        for (int u = 0; u < PF; ++u) {
+            if (h + u * groups >= q_hi) break;
+            float x0[8], x1[8];
+            to_pairs(raw[u], p, x0, x1);
+            rotate(p, c, s, x0, x1);
+            if (bad)
+#pragma unroll
+                for (int v = 0; v < 8; ++v) x0[v] = x1[v] = QNAN;
+            store_bf16(q + (size_t)row * ldq + (size_t)(h + u * groups) * D, p, x0, x1);
         }
     }
 }
@@ -1268,19 +1326,31 @@ hipError_t launch_rope_table_of(float2 *tab, int max_pos, int d, const double *f
     return hipGetLastError();
 }
 
+// f(head size, whether pairs come in 16-byte runs, whether the cache is e4m3)
+template <class F>
+static hipError_t append_variant(int d, const RopeArgs &rope, const CacheView &cv, F &&f)
+{
+    const bool vec = rope.interleaved || rope.rot % 16 == 0;
+    const auto go = [&](auto dd) {
+        if (vec) return cv.e4m3 ? f(dd, std::true_type{}, std::true_type{}) : f(dd, std::true_type{}, std::false_type{});
+        return cv.e4m3 ? f(dd, std::false_type{}, std::true_type{}) : f(dd, std::false_type{}, std::false_type{});
+    };
+    if (d == 128) go(std::integral_constant<int, 128>{});
+    else if (d == 64) go(std::integral_constant<int, 64>{});
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
 hipError_t launch_append_rows(const QkvRows &in, int rows, const uint8_t *valid, const int32_t *pos, int nq, int nkv,
                               int d, const RopeArgs &rope, uint16_t *q, long long ldq, const CacheView &cv,
                               const CacheLayer &cl, hipStream_t st)
 {
     const long long threads = (long long)rows * (nq + 2 * nkv) * (d / 16);
     const dim3 grid((unsigned)((threads + 255) / 256));
-    if (d == 128)
-        KLAUNCH((k_append_rows<128>), grid, dim3(256), 0, st, in, rows, valid, pos, nq, nkv, rope, q, ldq, cv, cl);
-    else if (d == 64)
-        KLAUNCH((k_append_rows<64>), grid, dim3(256), 0, st, in, rows, valid, pos, nq, nkv, rope, q, ldq, cv, cl);
-    else
-        return hipErrorInvalidValue;
-    return hipGetLastError();
+    return append_variant(d, rope, cv, [&](auto dd, auto vec, auto e4) {
+        KLAUNCH((k_append_rows<decltype(dd)::value, decltype(vec)::value, decltype(e4)::value>), grid, dim3(256), 0, st, in,
+                rows, valid, pos, nq, nkv, rope, q, ldq, cv, cl);
+    });
 }
 
 hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv, int d, const RopeArgs &rope,
@@ -1297,10 +1367,10 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
     while (slices < nkv && (long long)units * slices < 512) slices *= 2;
     slices = std::min(slices, nkv);
     const dim3 grid(units, slices), block(std::max(256, blk * (d / 16)));
-    if (d == 128) KLAUNCH((k_append_seqs<128>), grid, block, 0, st, in, seq, nq, nkv, rope, q, ldq, cv, cl);
-    else if (d == 64) KLAUNCH((k_append_seqs<64>), grid, block, 0, st, in, seq, nq, nkv, rope, q, ldq, cv, cl);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
+    return append_variant(d, rope, cv, [&](auto dd, auto vec, auto e4) {
+        KLAUNCH((k_append_seqs<decltype(dd)::value, decltype(vec)::value, decltype(e4)::value>), grid, block, 0, st, in, seq,
+                nq, nkv, rope, q, ldq, cv, cl);
+    });
 }
 
 // The smallest chunk from 128 tokens up to 1024 for which rows of max_len have
