@@ -609,8 +609,8 @@ __device__ __forceinline__ int row_len(const uint8_t *valid, const int32_t *lens
     return n < 0 || n > max_len - plus_one ? -1 : n + plus_one;
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void k_attn8_split(const uint16_t *__restrict__ q, long long ldq,
+template <int D, bool PAGED>
+__global__ __launch_bounds__(256, 3) void k_attn8_split(const uint16_t *__restrict__ q, long long ldq,
                                                      const uint8_t *__restrict__ valid, const int32_t *__restrict__ lens,
                                                      int plus_one, int G, int nkv, CacheView cv, CacheLayer cl, int chunk,
                                                      int max_splits, int max_len, float *__restrict__ ws,
@@ -649,48 +649,60 @@ __global__ __launch_bounds__(256) void k_attn8_split(const uint16_t *__restrict_
     for (int et = 0; et < ET; ++et) oacc[et] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float mrun = -INFINITY, lrun = 0.f;
 
-    const bool paged = cv.kv.layout == 1;
-    const int ps = paged ? cv.kv.page_size : 1, last_page = kmax / ps;
+    const int ps = PAGED ? cv.kv.page_size : 1, last_page = kmax / ps, bs = cv.blk_shift;
     const uint8_t *kc = (const uint8_t *)cl.k, *vc = (const uint8_t *)cl.v;
     const size_t head0 = ((size_t)r * nkv + kvh) * cv.kv.max_seq_len;                 // contiguous: the head's first row
-    const size_t blk0 = ((size_t)r * nkv + kvh) * (cv.kv.max_seq_len >> cv.blk_shift);
+    const size_t blk0 = ((size_t)r * nkv + kvh) * (cv.kv.max_seq_len >> bs);
     bool bad = false;
     auto fetch_pages = [&](int tb0, int buf) {        // wavefront 0, lane l: page tb0 / ps + l (clamped)
-        if (paged && wave == 0) {
+        if (PAGED && wave == 0) {
             const int pi = min(tb0 / ps + lane, last_page);
             __builtin_amdgcn_global_load_lds((const void *)(cv.kv.page_table + (size_t)r * cv.kv.max_pages_per_seq + pi),
                                              (lds_void *)&pgs[buf][0], 4, 0, 0);
         }
     };
-    // row of token t (real: t <= kmax) of the step at tb0, and its scale block
-    auto at = [&](int t, int first, int p0, int buf) -> Place {
-        if (!paged) return {head0 + t, blk0 + (t >> cv.blk_shift)};
-        const int i = (int)(((float)(t - first) + 0.5f) * cv.page_inv);   // (t - first) / ps: exact below 2^21
+    // paged: row of the real token that stands `in` tokens behind the first of
+    // the step's first page, and its scale block
+    auto at = [&](int in, int buf) -> Place {
+        const int i = (int)(((float)in + 0.5f) * cv.page_inv);            // in / ps: exact below 2^21
         int page = pgs[buf][i];
         if ((unsigned)page >= (unsigned)cv.num_pages) {
             bad = true;
             page = 0;
         }
-        const int in = t - first - i * ps;
+        in -= i * ps;
         const size_t head = (size_t)page * nkv + kvh;
-        return {head * ps + in, head * (ps >> cv.blk_shift) + (in >> cv.blk_shift)};
+        return {head * ps + in, head * (ps >> bs) + (in >> bs)};
     };
     uint32_t kb_next = 0, vb_next = 0;                // scale bytes of the lane's key rows and of its value tokens
     auto issue = [&](int tb0, int buf) {
         uint4 *base = tile + wave * 64;
-        const int p0 = tb0 / ps, first = paged ? p0 * ps : 0;
+        const int top = kmax - tb0, in0 = PAGED ? tb0 % ps : 0;           // last real token of the step; its place in a page
+        const uint8_t *kb = kc + (head0 + tb0) * D, *vb = vc + (head0 + tb0) * D;   // contiguous
 #pragma unroll
         for (int j = 0; j < OPS; ++j) {
-            const int u = j * 256 + tid, tk = u / KB, c = u % KB;
-            const size_t off = at(min(tb0 + tk, kmax), first, p0, buf).row * D;
-            __builtin_amdgcn_global_load_lds((const void *)(kc + off + 16 * (c ^ key_swz<KB>(tk))),
-                                             (lds_void *)(base + j * 256), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const void *)(vc + off + 16 * (c ^ val_swz<KB>(tk))),
-                                             (lds_void *)(base + KU + j * 256), 16, 0, 0);
+            const int u = j * 256 + tid, tk = u / KB, c = u % KB, t = min(tk, top);
+            const uint32_t kc16 = 16 * (c ^ key_swz<KB>(tk)), vc16 = 16 * (c ^ val_swz<KB>(tk));
+            const uint8_t *ksrc, *vsrc;
+            if constexpr (PAGED) {
+                const size_t off = at(in0 + t, buf).row * D;
+                ksrc = kc + off + kc16;
+                vsrc = vc + off + vc16;
+            } else {
+                ksrc = kb + (uint32_t)(t * D + kc16);
+                vsrc = vb + (uint32_t)(t * D + vc16);
+            }
+            __builtin_amdgcn_global_load_lds((const void *)ksrc, (lds_void *)(base + j * 256), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const void *)vsrc, (lds_void *)(base + KU + j * 256), 16, 0, 0);
         }
-        const int tb = tb0 + 32 * wave;
-        kb_next = cl.ks[at(min(tb + 8 * (hl >> 2), kmax), first, p0, buf).blk];
-        vb_next = cl.vs[at(min(tb + 8 * kg, kmax), first, p0, buf).blk];
+        const int tk = min(32 * wave + 8 * (hl >> 2), top), tv = min(32 * wave + 8 * kg, top);
+        if constexpr (PAGED) {
+            kb_next = cl.ks[at(in0 + tk, buf).blk];
+            vb_next = cl.vs[at(in0 + tv, buf).blk];
+        } else {
+            kb_next = cl.ks[blk0 + (uint32_t)((tb0 + tk) >> bs)];
+            vb_next = cl.vs[blk0 + (uint32_t)((tb0 + tv) >> bs)];
+        }
     };
 
     const int nsteps = (t1 - t0 + STEP - 1) / STEP;
@@ -1390,14 +1402,16 @@ hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const 
 {
     const int splits = (int)((max_len + (long long)chunk - 1) / chunk), G = nq / nkv;
     const dim3 grid(nkv, splits, rows);
-    if (d == 128)
-        KLAUNCH((k_attn8_split<128>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits,
-                max_len, ws, row_order);
-    else if (d == 64)
-        KLAUNCH((k_attn8_split<64>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits,
-                max_len, ws, row_order);
-    else
-        return hipErrorInvalidValue;
+    const bool paged = cv.kv.layout == 1;
+#define CORUN_SPLIT8(D_, P_)                                                                                              \
+    KLAUNCH((k_attn8_split<D_, P_>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits, \
+            max_len, ws, row_order)
+    if (d == 128 && paged) CORUN_SPLIT8(128, true);
+    else if (d == 128) CORUN_SPLIT8(128, false);
+    else if (d == 64 && paged) CORUN_SPLIT8(64, true);
+    else if (d == 64) CORUN_SPLIT8(64, false);
+    else return hipErrorInvalidValue;
+#undef CORUN_SPLIT8
     return hipGetLastError();
 }
 
