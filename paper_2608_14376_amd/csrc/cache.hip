@@ -604,9 +604,9 @@ __device__ __forceinline__ int val_swz(int t)
 // Tokens that row r attends to; -1 for a length outside the launch.
 __device__ __forceinline__ int row_len(const uint8_t *valid, const int32_t *lens, int plus_one, int max_len, int r)
 {
-    if (valid != nullptr && !valid[r]) return 0;
-    const int n = lens[r];
-    return n < 0 || n > max_len - plus_one ? -1 : n + plus_one;
+    const int n = lens[r];                            // in flight together with the flag
+    const bool live = valid == nullptr || valid[r] != 0;
+    return !live ? 0 : n < 0 || n > max_len - plus_one ? -1 : n + plus_one;
 }
 
 template <int D, bool PAGED>
@@ -614,7 +614,8 @@ __global__ __launch_bounds__(256, 3) void k_attn8_split(const uint16_t *__restri
                                                      const uint8_t *__restrict__ valid, const int32_t *__restrict__ lens,
                                                      int plus_one, int G, int nkv, CacheView cv, CacheLayer cl, int chunk,
                                                      int max_splits, int max_len, float *__restrict__ ws,
-                                                     const int32_t *__restrict__ row_order)
+                                                     const int32_t *__restrict__ row_order, uint16_t *__restrict__ out,
+                                                     long long ldo)
 {
     constexpr int ET = D / 16, KB = D / 16, STEP = 128, KU = STEP * KB, OPS = KU / 256;
     static_assert(4 * 16 * D * 4 <= 2 * KU * 16, "wavefront partials fit the tile");
@@ -628,7 +629,13 @@ __global__ __launch_bounds__(256, 3) void k_attn8_split(const uint16_t *__restri
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, hl = lane & 15, kg = lane >> 4;
     const int n = row_len(valid, lens, plus_one, max_len, r);
     const int t0 = split * chunk;
-    if (t0 >= n) return;
+    // out: rows have one split, whose result is the row's
+    uint16_t *orow = out == nullptr ? nullptr : out + (size_t)r * ldo + (size_t)kvh * G * D;
+    if (t0 >= n) {
+        if (orow != nullptr)
+            for (int i = tid; i < G * D; i += 256) orow[i] = n < 0 ? (uint16_t)0x7fc0 : (uint16_t)0;
+        return;
+    }
     const int t1 = min(n, t0 + chunk), kmax = t1 - 1;
     if (tid == 0) lost = 0;
 
@@ -834,6 +841,10 @@ __global__ __launch_bounds__(256, 3) void k_attn8_split(const uint16_t *__restri
             L += cl_[w][g] * f;
             A += ca[w * G * D + idx] * f;
         }
+        if (orow != nullptr) {
+            orow[idx] = f2bf(lost ? QNAN : A / L);
+            continue;
+        }
         o[2 * G + idx] = A;
         if (idx % D == 0) {
             o[g] = lost ? QNAN : M;
@@ -851,8 +862,8 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
                                                      int chunk, int max_splits, int max_len, uint16_t *__restrict__ out,
                                                      long long ldo)
 {
-    constexpr int HB = 256 / D, PF = 16;
-    extern __shared__ float fs[];                     // [HB][max_splits] weights
+    constexpr int HB = 256 / D, PF = 16;              // splits whose values are in flight at once
+    extern __shared__ float fs[];                     // [HB][2][max_splits] maxima, then weights; sums
     __shared__ float total[HB];
     const int hb = threadIdx.x / D, dd = threadIdx.x % D, lane = threadIdx.x & 63;
     const int h = blockIdx.x * HB + hb, r = blockIdx.y, G = nq / nkv;
@@ -869,14 +880,13 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
     float v[PF];
 #pragma unroll
     for (int u = 0; u < PF; ++u) v[u] = u < ns ? a[u * stride] : 0.f;
-    float *f = fs + hb * max_splits;
+    float *f = fs + hb * 2 * max_splits, *fl = f + max_splits;
     if (dd < 64) {
         float M = -INFINITY, L = 0.f;
-        bool nan = false;
-        for (int sp = lane; sp < ns; sp += 64) {
-            const float m = base[sp * stride + g];
-            nan |= m != m;
+        for (int sp = lane; sp < ns; sp += 64) {      // both loads at once: the sums wait for no maximum
+            const float m = base[sp * stride + g], l = base[sp * stride + G + g];
             f[sp] = m;
+            fl[sp] = l;
             M = fmaxf(M, m);
         }
 #pragma unroll
@@ -885,7 +895,7 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
         for (int sp = lane; sp < ns; sp += 64) {
             const float w = __expf(f[sp] - off_);
             f[sp] = w;
-            L += base[sp * stride + G + g] * w;
+            L += fl[sp] * w;
         }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
@@ -1385,11 +1395,15 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
     });
 }
 
-// The smallest chunk from 128 tokens up to 1024 for which rows of max_len have
-// at most 2048 workgroups, four rounds of two to a CU; more where a row would
-// have over 512 splits to merge.
+// One split for lengths up to 512, whose four steps cost less than a second
+// launch that merges (four slots of 128 tokens: 6.8 us a call, 10.2 with
+// two).  Else the smallest chunk from 128 tokens up to 1024 for which rows of
+// max_len have at most 2048 workgroups (162 rows of 512 to 4096 tokens: 154 us
+// at 1024, 156 at 512, 157 at 2048; 32 rows of 1K to 32K: 132, 139, 142); more
+// where a row would have over 512 splits to merge.
 int attn8_chunk(int rows, int nkv, int max_len)
 {
+    if (max_len <= 512) return 512;
     long long chunk = 128;
     while (chunk < 1024 && (long long)rows * nkv * ((max_len + chunk - 1) / chunk) > 2048) chunk *= 2;
     while ((max_len + chunk - 1) / chunk > 512) chunk *= 2;
@@ -1398,14 +1412,16 @@ int attn8_chunk(int rows, int nkv, int max_len)
 
 hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
                               int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                              int chunk, float *ws, hipStream_t st, const int32_t *row_order)
+                              int chunk, float *ws, hipStream_t st, const int32_t *row_order, uint16_t *out,
+                              long long ldo)
 {
     const int splits = (int)((max_len + (long long)chunk - 1) / chunk), G = nq / nkv;
+    if (out != nullptr && splits != 1) return hipErrorInvalidValue;
     const dim3 grid(nkv, splits, rows);
     const bool paged = cv.kv.layout == 1;
 #define CORUN_SPLIT8(D_, P_)                                                                                              \
     KLAUNCH((k_attn8_split<D_, P_>), grid, dim3(256), 0, st, q, ldq, valid, lens, plus_one, G, nkv, cv, cl, chunk, splits, \
-            max_len, ws, row_order)
+            max_len, ws, row_order, out, ldo)
     if (d == 128 && paged) CORUN_SPLIT8(128, true);
     else if (d == 128) CORUN_SPLIT8(128, false);
     else if (d == 64 && paged) CORUN_SPLIT8(64, true);
@@ -1421,7 +1437,7 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
     const int splits = (int)((max_len + (long long)chunk - 1) / chunk);
     const int hb = 256 / d;
     const dim3 grid((nq + hb - 1) / hb, rows);
-    const size_t shm = sizeof(float) * hb * splits;
+    const size_t shm = sizeof(float) * hb * 2 * splits;
     if (d == 128)
         KLAUNCH((k_attn8_merge<128>), grid, dim3(256), shm, st, ws, valid, lens, plus_one, nq, nkv, chunk, splits, max_len,
                 out, ldo);

@@ -1,5 +1,5 @@
 // cache_ops.cpp -- the cache operators of include/corun.h: host-side checks,
-// then one launch (two for decode attention).  Nothing here allocates, waits
+// then one launch (two for decode attention of long rows).  Nothing here allocates, waits
 // or keeps anything from one call for the next.
 #include "cache_ops.h"
 
@@ -286,6 +286,7 @@ extern "C" int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t 
     if (max_len < 0 || max_len > cache_view(kv).cap)
         return set_errorf(CORUN_E_CAPACITY, "max_len %d outside [0, %d]", max_len, cache_view(kv).cap);
     const int64_t most = longest(kv, max_len), chunk = attn8_chunk(rows, n_kv_heads, (int)most);
+    if (chunk >= most) return 0;
     return (int64_t)sizeof(float) * rows * n_heads * ((most + chunk - 1) / chunk) * (head_dim + 2);
 }
 
@@ -306,8 +307,11 @@ extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer
         return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
     const CacheView cv = cache_view(kv);
     const int most = longest(kv, max_len), chunk = attn8_chunk(rows, n_kv_heads, most);
+    const bool one = chunk >= most;                    // one split to a row: written straight to out
     TRY(launched(launch_attn8_split((const uint16_t *)q, ld_q, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim, cv, cl,
-                                    most, chunk, (float *)ws, (hipStream_t)stream)));
+                                    most, chunk, (float *)ws, (hipStream_t)stream, nullptr,
+                                    one ? (uint16_t *)out : nullptr, ld_out)));
+    if (one) return CORUN_OK;
     return launched(launch_attn8_merge((const float *)ws, rows, valid, lens, 0, n_heads, n_kv_heads, head_dim, most, chunk,
                                        (uint16_t *)out, ld_out, (hipStream_t)stream));
 }

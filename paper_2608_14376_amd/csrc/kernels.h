@@ -387,7 +387,8 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
 int attn8_chunk(int rows, int nkv, int max_len);
 hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const uint8_t *valid, const int32_t *lens,
                               int plus_one, int nq, int nkv, int d, const CacheView &cv, const CacheLayer &cl, int max_len,
-                              int chunk, float *ws, hipStream_t st, const int32_t *row_order = nullptr);
+                              int chunk, float *ws, hipStream_t st, const int32_t *row_order = nullptr,
+                              uint16_t *out = nullptr, long long ldo = 0);   // out: chunk >= max_len, nothing to merge
 hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, const int32_t *lens, int plus_one, int nq,
                               int nkv, int d, int max_len, int chunk, uint16_t *out, long long ldo, hipStream_t st);
 // Causal attention of a prefill call's queries: row row0 + t of sequence i
