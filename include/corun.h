@@ -322,8 +322,11 @@ corun_status corun_prefill_batch(corun_engine *e, const int32_t *tokens, const i
  * into a graph.  Tensors are DEVICE buffers of that device unless marked host;
  * `kv` and its arrays of layers are host, read during the call.  bf16 rows
  * (qkv, q, out) have strides ld_* in elements, multiples of 8; they and the
- * cache's buffers start on 16-byte boundaries.  n_heads / n_kv_heads is a whole number from 1 to 16;
- * head_dim 64 or 128.  A slot's pages are its own where a call appends.
+ * cache's buffers start on 16-byte boundaries, and no output overlaps another
+ * buffer.  n_heads / n_kv_heads is a whole number from 1 to 16, head_dim 64 or
+ * 128.  A slot's pages are its own where a call appends.  Appending at a
+ * position drops what the slot held behind the appended tokens: in an e4m3
+ * cache their block's scale may have changed.
  * What a kernel alone can see it checks itself: no lengths, positions or
  * page-table entries, whatever they hold, make it read or write outside the
  * cache.
@@ -341,7 +344,8 @@ corun_status corun_rope_init(const corun_rope_cfg *cfg, corun_rope *out);
  *  valid      uint8 [rows], or NULL: all rows are live
  *  positions  int32 [rows]
  * A live row whose position is outside [0, capacity), or whose page is outside
- * [0, num_pages), appends nothing and its q row is NaN.  rows <= n_slots. */
+ * [0, num_pages), appends nothing and its q row is NaN.  rows <= n_slots; rows
+ * (n_heads + 2 n_kv_heads) at most 2^28. */
 corun_status corun_decode_append(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
                                  const corun_rope *rope, int32_t rows, const void *qkv, int64_t ld_qkv,
                                  const uint8_t *valid, const int32_t *positions, void *q, int64_t ld_q, void *stream);
@@ -384,7 +388,8 @@ int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t n_heads, in
  * rows of q and out as for corun_prefill_append; the query at position
  * starts[i] + t sees tokens 0 .. starts[i] + t of slot slots[i], which earlier
  * calls have appended.  A query that sees a page outside [0, num_pages) gets
- * NaN.  A sequence's results do not depend on the others of the call. */
+ * NaN.  A sequence's results do not depend on the others of the call.  rows
+ * n_heads at most 2^30. */
 corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t n, const int32_t *lens, const int32_t *starts,
                                      const int32_t *slots, const void *q, int64_t ld_q, void *out, int64_t ld_out,

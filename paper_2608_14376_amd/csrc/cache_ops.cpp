@@ -1,6 +1,6 @@
 // cache_ops.cpp -- the cache operators of include/corun.h: host-side checks,
-// then one launch (two for decode attention of long rows).  Nothing here allocates, waits
-// or keeps anything from one call for the next.
+// then one launch (two for decode attention of long rows).  Nothing here
+// allocates, waits or keeps anything from one call for the next.
 #include "cache_ops.h"
 
 #include <hip/hip_runtime.h>
@@ -209,6 +209,17 @@ corun_status sequences(const corun_kv *kv, int32_t n, const int32_t *lens, const
     return CORUN_OK;
 }
 
+// A launch has fewer than 2^32 threads: head_dim / 16 to a head of a row of a
+// decode append, 512 to at most eight units of 32 rows of a head of prefill
+// attention (a sequence's last unit and workgroup may be partly empty).
+corun_status check_total(long long rows, long long heads, int log2_most)
+{
+    if (rows * heads <= 1ll << log2_most) return CORUN_OK;
+    return set_errorf(CORUN_E_SHAPE, "%lld rows of %lld heads in one call: at most 2^%d", rows, heads, log2_most);
+}
+
+long long rows_of(const SeqTable &seq) { return (long long)seq.row0[seq.n - 1] + seq.len[seq.n - 1]; }
+
 corun_status launched(hipError_t e)
 {
     return e == hipSuccess ? CORUN_OK : set_errorf(CORUN_E_HIP, "launch: %s", hipGetErrorString(e));
@@ -250,6 +261,7 @@ extern "C" corun_status corun_decode_append(const corun_kv *kv, int32_t layer, i
     TRY(check_rows("qkv", qkv, ld_qkv, (int64_t)(n_heads + 2 * n_kv_heads) * d));
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * d));
     if (!positions) return set_error(CORUN_E_INVAL, "null positions");
+    TRY(check_total(rows, n_heads + 2 * n_kv_heads, 28));
     QkvRows in;
     in.bf16 = (const uint16_t *)qkv;
     in.ld = ld_qkv;
@@ -326,6 +338,7 @@ extern "C" corun_status corun_prefill_attention(const corun_kv *kv, int32_t laye
     TRY(layer_of(kv, layer, &cl));
     SeqTable seq;
     TRY(sequences(kv, n, lens, starts, slots, &seq));
+    TRY(check_total(rows_of(seq), n_heads, 30));
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * head_dim));
     TRY(check_rows("out", out, ld_out, (int64_t)n_heads * head_dim));
     return launched(launch_attn8_seqs((const uint16_t *)q, ld_q, seq, n_heads, n_kv_heads, head_dim, cache_view(kv), cl,

@@ -169,3 +169,13 @@ def test_workspace_is_checked():
         assert decode_attention(kv, rows=64, ws_bytes=need - 1) == corun.E_CAPACITY
         assert decode_attention(kv, rows=64, ws=None) == corun.E_INVAL
         assert decode_attention(kv, rows=64, ws=P + 8) == corun.E_INVAL
+
+
+def test_launch_limits_refused():
+    kv = _kv(n_slots=65535)
+    assert decode_append(kv, _rope(), nq=4096, nkv=4096, rows=65535, ld=3 * 4096 * 128, ldq=4096 * 128) == corun.E_SHAPE
+    kv = _kv(n_slots=16, max_seq_len=1 << 20)
+    args = dict(n=16, lens=[1 << 20] * 16, starts=[0] * 16, slots=range(16))
+    assert prefill_attention(kv, nq=128, nkv=8, ldq=128 * 128, ldo=128 * 128, **args) == corun.E_SHAPE
+    args["lens"][0] += 16
+    assert prefill_attention(_kv(n_slots=16, max_seq_len=1 << 21), **args) == corun.E_SHAPE      # over 2^24 rows
