@@ -52,6 +52,16 @@ __device__ __forceinline__ Place place(const CacheView &cv, int nkv, int kvh, in
     return {head * cv.kv.max_seq_len + t, head * (cv.kv.max_seq_len >> cv.blk_shift) + (t >> cv.blk_shift)};
 }
 
+// The sequence that unit u of a call belongs to: one load and a count, where a
+// walk through the table would wait for every entry.
+__device__ __forceinline__ int seq_of(const SeqTable &seq, int u)
+{
+    static_assert(sizeof(SeqTable::unit0) == 64 * sizeof(int), "a lane to a sequence");
+    const int lane = threadIdx.x & 63;
+    const bool before = lane < seq.n && seq.unit0[lane] <= u;
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)) - 1);
+}
+
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 .. 127
 
 // The scale exponent that the largest finite magnitude (as bits) needs: the
@@ -420,8 +430,7 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
     const int blk = 1 << cv.blk_shift, tid = threadIdx.x;
     const int gt = blk * LPT, groups = blockDim.x / gt;      // threads of a head group
     const int hg = tid / gt, tok = tid % gt / LPT, j = tid % LPT;
-    int i = 0;
-    while (i + 1 < seq.n && seq.unit0[i + 1] <= (int)blockIdx.x) ++i;
+    const int i = seq_of(seq, blockIdx.x);
     const int start = seq.start[i], len = seq.len[i], slot = seq.slot[i];
     const int t0 = (start / blk + (int)blockIdx.x - seq.unit0[i]) * blk, t = t0 + tok;
     const bool fresh = t >= start && t - start < len;
@@ -918,10 +927,10 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // Prefill attention, causal, no split: keys in tiles of 64 in order, online
 // softmax in base 2.
 //
-// A unit is 32 queries of one query head; a workgroup of eight wavefronts takes
-// eight units of one kv head in [query block][head] order, latest first, one to
-// a wavefront, on shared key and value tiles.  A tile's codes are read into
-// registers one tile ahead, and become 16-bit LDS rows once for all eight
+// A unit is 32 queries of one query head; a workgroup of NW = 4 or 8 wavefronts
+// takes NW units of one kv head in [query block][head] order, latest first, one
+// to a wavefront, on shared key and value tiles.  A tile's codes are read into
+// registers one tile ahead, and become 16-bit LDS rows once for all its
 // wavefronts: keys in bf16 with their scale (exact), values in fp16 under a
 // common exponent `top`, the largest scale of the values so far (exact down to
 // 2^-15 of it; what is smaller yet keeps an absolute error of 2^-25 of that
@@ -936,13 +945,13 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // of the weights before they are rounded) carries 2^P_UP too, and the output
 // takes 2^(top - V_UP) back.
 //
-// A wavefront loads rows of one 16-token group of a tile, so its page and row
-// base are scalars and the loop has no vector address arithmetic.  Future keys
+// A wavefront's load takes rows of one 16-token group of a tile, so its page and
+// row base are scalars and the loop has no vector address arithmetic.  Future keys
 // and those past the sequence are masked by selection, value codes past it are
 // cleared.  A NaN among the values would reach queries that do not see it
 // (0 NaN), and a page that is none is read as page 0: a wavefront whose sums
-// hold a NaN, or whose workgroup met such a page, does its rows again one by
-// one (attend_row).
+// hold a NaN, or whose keys reach such a page, does its rows again one by one
+// (attend_row).
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -1025,12 +1034,12 @@ __device__ __forceinline__ void attend_row(const uint16_t *q, int n, int kvh, in
 template <int KCH>
 __device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
 
-template <int D, bool PAGED>
-__global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq, int G,
+template <int D, bool PAGED, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq, int G,
                                                        int nkv, CacheView cv, CacheLayer cl, uint16_t *__restrict__ out,
                                                        long long ldo)
 {
-    constexpr int NW = 8, QB = 32, BKT = 64;          // wavefronts; queries of a unit; keys of a tile
+    constexpr int QB = 32, BKT = 64;                  // queries of a unit; keys of a tile
     constexpr int DT = D / 32, KS = D / 16, KCH = D / 8;
     constexpr int UNITS = BKT * KCH;                  // 16-byte units of a tile's 16-bit keys, or values
     constexpr int OPITCH = D + 8;
@@ -1039,9 +1048,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     __shared__ int lost;
 
     const int kvh = blockIdx.x % nkv;
-    int si = 0;
-    while (si + 1 < seq.n && seq.unit0[si + 1] <= (int)(blockIdx.x / nkv)) ++si;
-    const int grp = (int)(blockIdx.x / nkv) - seq.unit0[si];
+    const int si = seq_of(seq, blockIdx.x / nkv), grp = (int)(blockIdx.x / nkv) - seq.unit0[si];
     const int n = seq.len[si], p0 = seq.start[si], slot = seq.slot[si], Lk = p0 + n;
     q += (size_t)seq.row0[si] * ldq;
     out += (size_t)seq.row0[si] * ldo;
@@ -1056,95 +1063,109 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     const int my_last_q = active ? p0 + min(n, q0 + QB) - 1 : -1;
     const int ntiles = __builtin_amdgcn_readfirstlane(wg_last_q / BKT + 1);
 
-    // Loads: for heads of 128 a wavefront takes eight rows of a tile's keys and
-    // values, for heads of 64 sixteen rows of keys (wavefronts 0 .. 3) or values:
-    // 16-byte unit c of row `row`, in 16-token group `sub` of the tile.
-    constexpr bool BOTH = D == 128;
-    const int row = BOTH ? tid >> 3 : (tid & 255) >> 2, c = BOTH ? tid & 7 : tid & 3;
-    const bool has_k = BOTH || wave < 4, has_v = BOTH || wave >= 4;
-    const int sub = BOTH ? wave >> 1 : wave & 3;
+    // Loads: R passes over a tile's rows, in each of which a thread takes 16-byte
+    // unit c of row `row` + r ROWS of keys and values, in 16-token group sub + r
+    // ROWS / 16.
+    constexpr int KB = D / 16, R = BKT * KB / (64 * NW), ROWS = BKT / R;
+    static_assert(R * 64 * NW == BKT * KB, "the threads cover a tile's units");
+    const int row = tid / KB, c = tid % KB, sub = wave * (64 / KB) / 16;
     const int ps = PAGED ? cv.kv.page_size : 0, bs = cv.blk_shift;
     const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
     const size_t head0 = ((size_t)slot * nkv + kvh) * cv.kv.max_seq_len;
     const size_t blk0 = ((size_t)slot * nkv + kvh) * (cv.kv.max_seq_len >> bs);
     const uint32_t off = (uint32_t)((row & 15) * D + 16 * c);      // in the group's rows
     // The next tile to load: its groups start at tokens t + 16 j; paged, page
-    // idx and row `in` of the wavefront's group, and of the group whose value
+    // idx and row `in` of the wavefront's groups, and of the group whose value
     // scale this lane loads (lane & 3).
-    int t = 0, idx = 0, in = 16 * sub, l_idx = 0, l_in = 16 * (lane & 3);
-    int page = 0, l_page = 0;
-    bool bad = false;
+    int t = 0, idx[R], in[R], l_idx = 0, l_in = 16 * (lane & 3);
+    int page[R], l_page = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        idx[r] = page[r] = 0;
+        in[r] = 16 * sub + ROWS * r;
+    }
+    int first_bad = INT32_MAX;                        // first group that this wavefront found on a page that is none
     auto fetch_pages = [&]() {
         if constexpr (PAGED) {
-            while (in >= ps) {
-                in -= ps;
-                ++idx;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                while (in[r] >= ps) {
+                    in[r] -= ps;
+                    ++idx[r];
+                }
+                page[r] = 0;
+                if (t + 16 * sub + ROWS * r < Lk) page[r] = pt[idx[r]];
             }
             const int step = (int)(((float)l_in + 0.5f) * cv.page_inv);   // l_in < page_size + 64: exact
             l_idx += step;
             l_in -= step * ps;
-            page = l_page = 0;
-            if (t + 16 * sub < Lk) page = pt[idx];
+            l_page = 0;
             if (t + 16 * (lane & 3) < Lk) l_page = pt[l_idx];
         }
     };
-    uint4 kraw, vraw;
-    uint32_t kb = 0, vb = 0;                          // scale bytes: of the wavefront's group's keys, of group lane & 3's values
+    uint4 kraw[R], vraw[R];
+    uint32_t kb[R] = {}, vb = 0;                      // scale bytes: of the wavefront's groups' keys, of group lane & 3's values
     auto load = [&]() {
-        kraw = vraw = (uint4){0u, 0u, 0u, 0u};
-        size_t base, kblk, vblk;
-        if constexpr (PAGED) {
-            page = __builtin_amdgcn_readfirstlane(page);
-            if ((unsigned)page >= (unsigned)cv.num_pages) {
-                bad = true;
-                page = 0;
+        size_t vblk;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int t16 = t + 16 * sub + ROWS * r;
+            kraw[r] = vraw[r] = (uint4){0u, 0u, 0u, 0u};
+            size_t base, kblk;
+            if constexpr (PAGED) {
+                int pg = __builtin_amdgcn_readfirstlane(page[r]);
+                if ((unsigned)pg >= (unsigned)cv.num_pages) {
+                    first_bad = min(first_bad, t16);
+                    pg = 0;
+                }
+                const size_t head = (size_t)pg * nkv + kvh;
+                base = head * ps + in[r];
+                kblk = head * (ps >> bs) + (in[r] >> bs);
+                in[r] += BKT;
+            } else {
+                base = head0 + t16;
+                kblk = blk0 + (t16 >> bs);
             }
+            if (t16 < Lk) {                           // the whole group stands in the slot
+                kraw[r] = *(const uint4 *)((const uint8_t *)cl.k + base * D + off);
+                kb[r] = cl.ks[kblk];
+                vraw[r] = *(const uint4 *)((const uint8_t *)cl.v + base * D + off);
+            }
+        }
+        if constexpr (PAGED) {
             if ((unsigned)l_page >= (unsigned)cv.num_pages) l_page = 0;
-            const size_t head = (size_t)page * nkv + kvh;
-            base = head * ps + in;
-            kblk = head * (ps >> bs) + (in >> bs);
             vblk = ((size_t)l_page * nkv + kvh) * (ps >> bs) + (l_in >> bs);
-            in += BKT;
             l_in += BKT;
         } else {
-            base = head0 + t + 16 * sub;
-            kblk = blk0 + ((t + 16 * sub) >> bs);
             vblk = blk0 + ((t + 16 * (lane & 3)) >> bs);
-        }
-        if (t + 16 * sub < Lk) {                      // the whole group stands in the slot
-            if (has_k) {
-                kraw = *(const uint4 *)((const uint8_t *)cl.k + base * D + off);
-                kb = cl.ks[kblk];
-            }
-            if (has_v) vraw = *(const uint4 *)((const uint8_t *)cl.v + base * D + off);
         }
         if (t + 16 * (lane & 3) < Lk) vb = cl.vs[vblk];
         t += BKT;
     };
     // The loaded tile, from key k0, to LDS buffer b; `top` becomes the common
     // exponent byte of its values.
-    const int kw0 = pf_swz<KCH>(row, 2 * c), kw1 = pf_swz<KCH>(row, 2 * c + 1);
-    const int vw0 = row * KCH + ((2 * c) ^ val16_swz<KCH>(row)), vw1 = row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row));
     auto store = [&](int k0, int b, int &top) {
         const int v0 = __builtin_amdgcn_readlane(vb, 0), v1 = __builtin_amdgcn_readlane(vb, 1);
         const int v2 = __builtin_amdgcn_readlane(vb, 2), v3 = __builtin_amdgcn_readlane(vb, 3);
         top = max(top, max(max(v0, v1), max(v2, v3)));
         uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
         uint4 lo, hi;
-        if (has_k) {
-            codes_16<false>(kraw, __uint_as_float(__builtin_amdgcn_readfirstlane(kb) << 23), lo, hi);
-            K[kw0] = lo;
-            K[kw1] = hi;
-        }
-        if (has_v) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int rw = row + ROWS * r;
+            codes_16<false>(kraw[r], __uint_as_float(__builtin_amdgcn_readfirstlane(kb[r]) << 23), lo, hi);
+            K[pf_swz<KCH>(rw, 2 * c)] = lo;
+            K[pf_swz<KCH>(rw, 2 * c + 1)] = hi;
+            uint4 w = vraw[r];
             if (k0 + BKT > Lk) {
-                const uint32_t use = k0 + row < Lk ? 0xffffffffu : 0u;
-                vraw = (uint4){vraw.x & use, vraw.y & use, vraw.z & use, vraw.w & use};
+                const uint32_t use = k0 + rw < Lk ? 0xffffffffu : 0u;
+                w = (uint4){w.x & use, w.y & use, w.z & use, w.w & use};
             }
-            const int e = max((sub == 0 ? v0 : sub == 1 ? v1 : sub == 2 ? v2 : v3) - top + V_UP, -60);
-            codes_16<true>(vraw, exp2_int(e), lo, hi);
-            V[vw0] = lo;
-            V[vw1] = hi;
+            const int grp16 = sub + ROWS / 16 * r;
+            const int e = max((grp16 == 0 ? v0 : grp16 == 1 ? v1 : grp16 == 2 ? v2 : v3) - top + V_UP, -60);
+            codes_16<true>(w, exp2_int(e), lo, hi);
+            V[rw * KCH + ((2 * c) ^ val16_swz<KCH>(rw))] = lo;
+            V[rw * KCH + ((2 * c + 1) ^ val16_swz<KCH>(rw))] = hi;
         }
     };
 
@@ -1168,7 +1189,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     // MFMA row stands for; transposed value reads (see vread)
     const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
 
-    if (tid == 0) lost = 0;
+    if (tid == 0) lost = INT32_MAX;
     int top_next = 0;
     fetch_pages();
     load();
@@ -1291,7 +1312,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if (bad) lost = 1;
+    if (PAGED && lane == 0 && first_bad != INT32_MAX) atomicMin(&lost, first_bad);
     __syncthreads();                                  // every wavefront is done with the tiles
 
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]; through LDS for whole rows
@@ -1312,7 +1333,7 @@ __global__ __launch_bounds__(512) void k_attn8_prefill(const uint16_t *__restric
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wavefront's staging writes are done
     if (!active) return;
-    if (lost || __ballot(nan && q0 + r32 < n)) {
+    if (lost <= my_last_q || __ballot(nan && q0 + r32 < n)) {
 #pragma unroll 1
         for (int r = 0; r < QB && q0 + r < n; ++r)
             attend_row<D>(q + (size_t)(q0 + r) * ldq + (size_t)hq * D, p0 + q0 + r + 1, kvh, nkv, slot, cv, cl,
@@ -1449,23 +1470,50 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
     return hipGetLastError();
 }
 
-hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
+hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &given, int nq, int nkv, int d, const CacheView &cv,
                              const CacheLayer &cl, uint16_t *out, long long ldo, hipStream_t st)
 {
-    const int G = nq / nkv;
+    const int G = nq / nkv, n = given.n;
+    if (n < 1 || n > 64) return hipErrorInvalidValue;
+    // longest sequences first: the last workgroups of a call are short ones (12
+    // prompts of 100 to 600 tokens: 47 us in the order given, 40 so)
+    int by[64];
+    for (int i = 0; i < n; ++i) by[i] = i;
+    const auto keys = [&](int i) { return given.start[i] + given.len[i]; };
+    std::stable_sort(by, by + n, [&](int a, int b) { return keys(a) > keys(b); });
+    SeqTable seq;
+    seq.n = n;
+    long long groups8 = 0;
+    for (int i = 0; i < n; ++i) {
+        seq.row0[i] = given.row0[by[i]];
+        seq.len[i] = given.len[by[i]];
+        seq.start[i] = given.start[by[i]];
+        seq.slot[i] = given.slot[by[i]];
+        groups8 += ((seq.len[i] + 31) / 32 * G + 7) / 8;
+    }
+    // Eight wavefronts share a tile's conversion; four are twice the workgroups,
+    // and a tile takes them 1.7 us on a CU of their own where eight need 1.9.
+    // Heads of 128 take four where eight would leave half of the 256 CUs idle
+    // (1024 rows at 8192: 260 us, 280 with eight; 1536 rows: 342, 297) and where no
+    // sequence has many tiles (1000 tokens: 37 us, 40 with eight; 2000: 72, 73; 4000:
+    // 186, 155).  Heads of 64 always do (600, 2000, 6000 tokens: 18, 45, 211 us; 21,
+    // 54, 251 with eight).  A row's arithmetic is the same either way.
+    const int NW = d == 64 || groups8 * nkv <= 128 || keys(by[0]) <= 2048 ? 4 : 8;
     int groups = 0;
-    for (int i = 0; i < seq.n; ++i) {
+    for (int i = 0; i < n; ++i) {
         seq.unit0[i] = groups;
-        groups += ((seq.len[i] + 31) / 32 * G + 7) / 8;
+        groups += ((seq.len[i] + 31) / 32 * G + NW - 1) / NW;
     }
     const dim3 grid((unsigned)groups * nkv);
     const bool paged = cv.kv.layout == 1;
-#define CORUN_PREFILL8(D_, P_) \
-    KLAUNCH((k_attn8_prefill<D_, P_>), grid, dim3(512), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo)
-    if (d == 128 && paged) CORUN_PREFILL8(128, true);
-    else if (d == 128) CORUN_PREFILL8(128, false);
-    else if (d == 64 && paged) CORUN_PREFILL8(64, true);
-    else if (d == 64) CORUN_PREFILL8(64, false);
+#define CORUN_PREFILL8(D_, P_, NW_) \
+    KLAUNCH((k_attn8_prefill<D_, P_, NW_>), grid, dim3(64 * NW_), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo)
+    if (d == 128 && paged && NW == 8) CORUN_PREFILL8(128, true, 8);
+    else if (d == 128 && paged) CORUN_PREFILL8(128, true, 4);
+    else if (d == 128 && NW == 8) CORUN_PREFILL8(128, false, 8);
+    else if (d == 128) CORUN_PREFILL8(128, false, 4);
+    else if (d == 64 && paged) CORUN_PREFILL8(64, true, 4);
+    else if (d == 64) CORUN_PREFILL8(64, false, 4);
     else return hipErrorInvalidValue;
 #undef CORUN_PREFILL8
     return hipGetLastError();

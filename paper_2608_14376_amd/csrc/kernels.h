@@ -393,7 +393,7 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
                               int nkv, int d, int max_len, int chunk, uint16_t *out, long long ldo, hipStream_t st);
 // Causal attention of a prefill call's queries: row row0 + t of sequence i
 // sees tokens 0 .. start + t of its slot.
-hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
+hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
                              const CacheLayer &cl, uint16_t *out, long long ldo, hipStream_t st);
 
 }  // namespace corun

@@ -512,6 +512,33 @@ def test_prefill_attention_long():
     check_prefill(hc, x, out, seqs_of(lens, starts, slots))
 
 
+@pytest.mark.parametrize("page", [0, 192])
+def test_prefill_attention_of_many_rows_and_long_sequences(page):
+    """Workgroups of eight wavefronts (over 2048 keys, more than 128 such workgroups); a sequence's bits alone,
+    where there are few; rows before, around and behind a page that is none."""
+    d, nkv, G, blk, cap = 128, 8, 16, 32, 2304
+    hc = HostCache(nkv, d, 3, cap, blk, page, seed=74)
+    a, b = hc.at(0, 2290)
+    hc.v[a, 3, b, 7] = 0x7F
+    cache = hc.device_cache(corun)
+    lens, starts, slots = [1, 270, 40], [5, 2034, 2200], [1, 2, 0]
+    x, q = rows_of(sum(lens), nkv * G, d, 75, pad=8, loud=False)
+    out = run_prefill(cache, q, lens, starts, slots)
+    check_prefill(hc, x, out, [(0, 1, 5, 1), (1, 270, 2034, 2)], every=45)
+    check_prefill(hc, x, out, [(271, 40, 2200, 0)], every=80)
+    for row, n, p0, slot in seqs_of(lens, starts, slots):
+        if n < 270:
+            assert same(run_prefill(cache, q[row:row + n], [n], [p0], [slot]), out[row:row + n])
+    if page:
+        hc.table[2, 11] = -1                          # tokens 2112 .., rows 78 .. of the second sequence
+        bad = run_prefill(hc.device_cache(corun), q, lens, starts, slots)
+        assert same(bad[:65], out[:65]) and same(bad[271:], out[271:])
+        assert torch.isnan(bad[1 + 78:271]).all()
+        hc.table[2, 11] = 0                           # any page: rows 64 .. 77 do not see it
+        check_prefill(hc, x, bad, [(65, 14, 2098, 2)], every=6)
+
+
+
 # --------------------------------------------------------------------------
 # Together, as a layer calls them
 # --------------------------------------------------------------------------
