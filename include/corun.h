@@ -388,12 +388,19 @@ int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t n_heads, in
  * rows of q and out as for corun_prefill_append; the query at position
  * starts[i] + t sees tokens 0 .. starts[i] + t of slot slots[i], which earlier
  * calls have appended.  A query that sees a page outside [0, num_pages) gets
- * NaN.  A sequence's results do not depend on the others of the call.  rows
- * n_heads at most 2^30. */
+NaN.  A sequence's results do not depend on the others of the call.  rows
+ * n_heads at most 2^30.
+ *  ws         workspace as for corun_decode_attention: ws_bytes at least what
+ *             corun_prefill_attention_workspace returns for the same sequences,
+ *             which is 0 (ws may be NULL) unless a sequence of few rows starts
+ *             behind many tokens */
 corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t n, const int32_t *lens, const int32_t *starts,
                                      const int32_t *slots, const void *q, int64_t ld_q, void *out, int64_t ld_out,
-                                     void *stream);
+                                     void *ws, int64_t ws_bytes, void *stream);
+/* Bytes (>= 0), or a negative corun_status.  Host only. */
+int64_t corun_prefill_attention_workspace(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          int32_t n, const int32_t *lens, const int32_t *starts);
 
 /* The engine's fixed batch size, model configuration and KV description
  * (copies; the k/v/page-table pointers are the caller's borrowed ones).

@@ -30,7 +30,8 @@ EXPORTS = ("corun_engine_create", "corun_engine_destroy", "corun_decode_step", "
            "corun_sched_create", "corun_sched_destroy", "corun_sched_add_request", "corun_sched_step",
            "corun_sched_output", "corun_sched_state", "corun_sched_last_error",
            "corun_rope_init", "corun_decode_append", "corun_prefill_append", "corun_decode_attention",
-           "corun_decode_attention_workspace", "corun_prefill_attention")
+           "corun_decode_attention_workspace", "corun_prefill_attention",
+           "corun_prefill_attention_workspace")
 
 # kernel ids of corun_time_kernel
 K_QKV_GEMM, K_O_GEMM, K_GATE_UP_GEMM, K_DOWN_GEMM, K_LM_HEAD, K_ATTN_SPLIT, K_ATTN_MERGE, K_RMSNORM, \
@@ -170,7 +171,9 @@ def load():
     L.corun_decode_attention_workspace.restype = i64
     L.corun_decode_attention_workspace.argtypes = [ptr, i32, i32, i32, i32, i32]
     L.corun_prefill_attention.restype = st
-    L.corun_prefill_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr, i64, ptr]
+    L.corun_prefill_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr, i64, ptr, i64, ptr]
+    L.corun_prefill_attention_workspace.restype = i64
+    L.corun_prefill_attention_workspace.argtypes = [ptr, i32, i32, i32, i32, ptr, ptr]
     L.corun_last_error.restype = C.c_char_p
     L.corun_last_error.argtypes = []
     _lib = L
@@ -385,6 +388,15 @@ def _stream(cache, stream):
     return _torch.stream(cache.index) if stream is None else stream.cuda_stream
 
 
+def _scratch(q, size, stream):
+    """A buffer of the stream's own: what its allocator hands out there, later work of that stream alone reuses."""
+    import torch
+    if stream is None:
+        return torch.empty(size, dtype=torch.uint8, device=q.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(size, dtype=torch.uint8, device=q.device)
+
+
 class _Torch:
     """What the operators' checks take from torch, which this module imports
     only where it is used.  The current stream's handle comes from torch's own
@@ -430,7 +442,7 @@ def _sequences(lens, starts, slots, rows):
     if ln.ndim != 1 or sl.shape != ln.shape or (sr is not None and sr.shape != ln.shape):
         raise ValueError("lens, starts and slots: one entry for each sequence")
     total = int(ln.sum(dtype=np.int64))
-    if total != rows:
+    if rows is not None and total != rows:
         raise ValueError(f"the sequences have {total} tokens, the tensors {rows} rows")
     return ln, sr, sl
 
@@ -476,14 +488,37 @@ def decode_attention(cache, layer, q, lens, out, ws, valid=None, max_len=0, stre
                                          _stream(cache, stream)))
 
 
-def prefill_attention(cache, layer, q, lens, starts, slots, out, stream=None) -> None:
+def prefill_attention_workspace(cache, n_heads, lens, starts=None) -> int:
+    """Bytes of workspace that prefill_attention needs for these sequences."""
+    ln, sr, _ = _sequences(lens, starts, lens, None)
+    n = load().corun_prefill_attention_workspace(cache._at, n_heads, cache.n_kv_heads, cache.head_dim, ln.size,
+                                                 ln.ctypes.data, None if sr is None else sr.ctypes.data)
+    if n < 0:
+        raise CorunError(n, last_error())
+    return n
+
+
+def prefill_attention(cache, layer, q, lens, starts, slots, out, ws=None, stream=None) -> None:
     """corun_prefill_attention: causal attention of n sequences' queries (rows
-    as for prefill_append) over an e4m3 cache that holds their tokens."""
+    as for prefill_append) over an e4m3 cache that holds their tokens.  ws: a
+    device uint8 tensor of prefill_attention_workspace bytes, not shared by
+    calls that may overlap; None: torch's allocator gives one for the call."""
     rows, nq, ldq, ldo = _attention_rows(cache, q, out)
     ln, sr, sl = _sequences(lens, starts, slots, rows)
+    sp = None if sr is None else sr.ctypes.data
+    wp, size = None, 0
+    if ws is not None:
+        size = ws.numel()
+        wp = _vec(cache, ws, _torch.flags[:1], size, "ws")
+    else:
+        need = load().corun_prefill_attention_workspace(cache._at, nq, cache.n_kv_heads, cache.head_dim, ln.size,
+                                                        ln.ctypes.data, sp)
+        if need > 0:
+            ws, size = _scratch(q, need, stream), need
+            wp = ws.data_ptr()
     _check(load().corun_prefill_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, ln.size,
-                                          ln.ctypes.data, None if sr is None else sr.ctypes.data, sl.ctypes.data,
-                                          q.data_ptr(), ldq, out.data_ptr(), ldo, _stream(cache, stream)))
+                                          ln.ctypes.data, sp, sl.ctypes.data, q.data_ptr(), ldq, out.data_ptr(), ldo, wp,
+                                          size, _stream(cache, stream)))
 
 
 class SchedCfg(C.Structure):

@@ -924,8 +924,10 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 }
 
 // ---------------------------------------------------------------------------
-// Prefill attention, causal, no split: keys in tiles of 64 in order, online
-// softmax in base 2.
+// Prefill attention, causal: keys in tiles of 64 in order, online softmax in
+// base 2.  A sequence of few rows behind many tokens is split over its tiles
+// (attn8_seq_splits, a function of the sequence alone): each split's result and
+// its maximum and sum go to the workspace, and k_attn8_join weighs them in order.
 //
 // A unit is 32 queries of one query head; a workgroup of NW = 4 or 8 wavefronts
 // takes NW units of one kv head in [query block][head] order, latest first, one
@@ -951,11 +953,18 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // cleared.  A NaN among the values would reach queries that do not see it
 // (0 NaN), and a page that is none is read as page 0: a wavefront whose sums
 // hold a NaN, or whose keys reach such a page, does its rows again one by one
-// (attend_row).
+// (attend_row); a split notes a NaN maximum for such a row and the join does it.
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int P_UP = 8, P_LAG = 7, V_UP = 6;
+constexpr int MOST_SPLITS = 64;
+
+// Tiles of each of ns splits of Lk keys.
+__host__ __device__ __forceinline__ int tiles_of_split(int Lk, int ns)
+{
+    return ((Lk + 63) / 64 + ns - 1) / ns;
+}
 
 // Sixteen codes times a power of two, as 32 bytes of bf16 or fp16.
 template <bool F16>
@@ -1034,10 +1043,16 @@ __device__ __forceinline__ void attend_row(const uint16_t *q, int n, int kvh, in
 template <int KCH>
 __device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
 
+// Floats that a split leaves of a unit: its rows' results, [D / 4][32 rows][4],
+// then their maxima (log2) and sums, [32][2].
+template <int D>
+constexpr int PART = 32 * D + 64;
+
 template <int D, bool PAGED, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq, int G,
-                                                       int nkv, CacheView cv, CacheLayer cl, uint16_t *__restrict__ out,
-                                                       long long ldo)
+__global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq,
+                                                              SplitTable sp, int G, int nkv, CacheView cv, CacheLayer cl,
+                                                              uint16_t *__restrict__ out, long long ldo,
+                                                              float *__restrict__ ws)
 {
     constexpr int QB = 32, BKT = 64;                  // queries of a unit; keys of a tile
     constexpr int DT = D / 32, KS = D / 16, KCH = D / 8;
@@ -1048,7 +1063,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     __shared__ int lost;
 
     const int kvh = blockIdx.x % nkv;
-    const int si = seq_of(seq, blockIdx.x / nkv), grp = (int)(blockIdx.x / nkv) - seq.unit0[si];
+    const int si = seq_of(seq, blockIdx.x / nkv), in_seq = (int)(blockIdx.x / nkv) - seq.unit0[si];
+    const int ns = sp.splits[si];
+    const int grp = ns == 1 ? in_seq : in_seq / ns, split = in_seq - grp * ns;
     const int n = seq.len[si], p0 = seq.start[si], slot = seq.slot[si], Lk = p0 + n;
     q += (size_t)seq.row0[si] * ldq;
     out += (size_t)seq.row0[si] * ldo;
@@ -1061,7 +1078,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     const int qb = active ? u / G : 0, g = active ? u % G : 0, hq = kvh * G + g, q0 = qb * QB;
     const int wg_last_q = p0 + min(n, ((units - 1 - grp * NW) / G + 1) * QB) - 1;
     const int my_last_q = active ? p0 + min(n, q0 + QB) - 1 : -1;
-    const int ntiles = __builtin_amdgcn_readfirstlane(wg_last_q / BKT + 1);
+    const int per = ns == 1 ? INT32_MAX : tiles_of_split(Lk, ns);
+    const int tile0 = ns == 1 ? 0 : split * per;      // a split's tiles: tile0 .. ntiles - 1
+    const int ntiles = __builtin_amdgcn_readfirstlane(min(wg_last_q / BKT + 1, ns == 1 ? INT32_MAX : tile0 + per));
+    if (tile0 >= ntiles) return;                      // all of the split is in the workgroup's future
 
     // Loads: R passes over a tile's rows, in each of which a thread takes 16-byte
     // unit c of row `row` + r ROWS of keys and values, in 16-token group sub + r
@@ -1077,12 +1097,17 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     // The next tile to load: its groups start at tokens t + 16 j; paged, page
     // idx and row `in` of the wavefront's groups, and of the group whose value
     // scale this lane loads (lane & 3).
-    int t = 0, idx[R], in[R], l_idx = 0, l_in = 16 * (lane & 3);
+    int t = BKT * tile0, idx[R], in[R], l_idx = 0, l_in = 16 * (lane & 3);
     int page[R], l_page = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        idx[r] = page[r] = 0;
-        in[r] = 16 * sub + ROWS * r;
+        idx[r] = PAGED ? t / ps : 0;
+        in[r] = (PAGED ? t % ps : 0) + 16 * sub + ROWS * r;
+        page[r] = 0;
+    }
+    if constexpr (PAGED) {
+        l_idx = t / ps;
+        l_in += t % ps;
     }
     int first_bad = INT32_MAX;                        // first group that this wavefront found on a page that is none
     auto fetch_pages = [&]() {
@@ -1194,11 +1219,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     fetch_pages();
     load();
     fetch_pages();
-    store(0, 0, top_next);
+    store(BKT * tile0, tile0 & 1, top_next);
     int top_acc = top_next;
     load();
     fetch_pages();
-    for (int i = 0; i < ntiles; ++i) {
+    for (int i = tile0; i < ntiles; ++i) {
         const int k0 = i * BKT, b = i & 1;
         __syncthreads();                              // tile i is in LDS, and tile i - 1's buffers are free
         const int top = top_next;
@@ -1315,12 +1340,33 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     if (PAGED && lane == 0 && first_bad != INT32_MAX) atomicMin(&lost, first_bad);
     __syncthreads();                                  // every wavefront is done with the tiles
 
-    // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]; through LDS for whole rows
-    uint16_t *ost = (uint16_t *)ring + (size_t)wave * QB * OPITCH;
+    // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]
     bool nan = false;
+    const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
+    const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]), inv = 1.0f / sum;
+    if (ns > 1) {
+        if (!active || my_last_q < BKT * tile0) return;   // no row of the unit sees the split's tiles
+        const size_t all = (size_t)(units / G) * G * nkv, unit = (size_t)kvh * units + u;
+        float *part = ws + ((size_t)sp.part0[si] + split * all + unit) * PART<D>;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                float4 v;
+                v.x = __builtin_amdgcn_ldexpf(acc[dt][j] * inv, top_acc - 127 - V_UP);
+                v.y = __builtin_amdgcn_ldexpf(acc[dt][j + 1] * inv, top_acc - 127 - V_UP);
+                v.z = __builtin_amdgcn_ldexpf(acc[dt][j + 2] * inv, top_acc - 127 - V_UP);
+                v.w = __builtin_amdgcn_ldexpf(acc[dt][j + 3] * inv, top_acc - 127 - V_UP);
+                nan |= v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w;
+                *(float4 *)(part + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = v;
+            }
+        const unsigned long long bad = __ballot(nan || lost <= qq);
+        if (h == 0) *(float2 *)(part + 32 * D + 2 * r32) = {((bad | bad >> 32) >> r32) & 1 ? QNAN : mrow, sum};
+        return;
+    }
+    // through LDS for whole rows
+    uint16_t *ost = (uint16_t *)ring + (size_t)wave * QB * OPITCH;
     {
-        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
-        const float inv = 1.0f / (__uint_as_float(two[0]) + __uint_as_float(two[1]));
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -1345,6 +1391,69 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
         const int qr = it / (D / 8), c8 = it % (D / 8), qo = q0 + qr;
         if (qo < n) *(uint4 *)(out + (size_t)qo * ldo + (size_t)hq * D + 8 * c8) = *(const uint4 *)(ost + qr * OPITCH + 8 * c8);
     }
+}
+
+// The splits of a unit's rows, weighed by their maxima and sums in order.
+// Workgroup: one unit (x), D / 4 slices of 8 dimension fours (y); thread (four,
+// row).  A row counts the splits that it sees; rows with a NaN maximum are done
+// again by the first slice.
+template <int D>
+__global__ __launch_bounds__(256) void k_attn8_join(const float *__restrict__ ws, const uint16_t *__restrict__ q,
+                                                    long long ldq, SeqTable seq, SplitTable sp, int G, int nkv, CacheView cv,
+                                                    CacheLayer cl, uint16_t *__restrict__ out, long long ldo)
+{
+    __shared__ float w[MOST_SPLITS][32], l[MOST_SPLITS][32];
+    __shared__ uint32_t again;
+    const int si = seq_of(seq, blockIdx.x), ns = sp.splits[si], n = seq.len[si], p0 = seq.start[si], slot = seq.slot[si];
+    const int unit = (int)blockIdx.x - seq.unit0[si], units = (n + 31) / 32 * G;
+    const int kvh = unit / units, u = unit % units, q0 = u / G * 32, hq = kvh * G + u % G;
+    const int tid = threadIdx.x, r = tid & 31, sl = tid >> 5, t = q0 + r;
+    const int span = 64 * tiles_of_split(p0 + n, ns), seen = t < n ? (p0 + t) / span + 1 : 0;   // <= ns
+    const size_t stride = (size_t)units * nkv * PART<D>;
+    const float *part = ws + ((size_t)sp.part0[si] + unit) * PART<D>;
+    for (int s = sl; s < seen; s += 8) {
+        const float2 ml = *(const float2 *)(part + s * stride + 32 * D + 2 * r);
+        w[s][r] = ml.x;
+        l[s][r] = ml.y;
+    }
+    __syncthreads();
+    if (tid < 32) {
+        float M = -INFINITY, L = 0.f;
+        bool bad = false;
+        for (int s = 0; s < seen; ++s) {
+            bad |= w[s][r] != w[s][r];
+            M = fmaxf(M, w[s][r]);
+        }
+        for (int s = 0; s < seen; ++s) {
+            const float x = l[s][r] * __builtin_amdgcn_exp2f(w[s][r] - M);
+            w[s][r] = x;
+            L += x;
+        }
+        for (int s = 0; s < seen; ++s) w[s][r] /= L;
+        const uint32_t rows = (uint32_t)__ballot(bad);
+        if (tid == 0) again = rows;
+    }
+    __syncthreads();
+    const uint32_t rows = again;
+    const int c = 8 * blockIdx.y + sl;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < seen; ++s) {
+        const float4 v = *(const float4 *)(part + s * stride + 4 * (c * 32 + r));
+        const float x = w[s][r];
+        o.x += x * v.x;
+        o.y += x * v.y;
+        o.z += x * v.z;
+        o.w += x * v.w;
+    }
+    if (t < n && !((rows >> r) & 1))
+        *(uint2 *)(out + (size_t)(seq.row0[si] + t) * ldo + (size_t)hq * D + 4 * c) = (uint2){f2bf2(o.x, o.y), f2bf2(o.z, o.w)};
+    if (blockIdx.y != 0) return;
+#pragma unroll 1
+    for (int i = tid >> 6; i < 32; i += 4)
+        if ((rows >> i) & 1)                          // set for rows of the sequence only
+            attend_row<D>(q + (size_t)(seq.row0[si] + q0 + i) * ldq + (size_t)hq * D, p0 + q0 + i + 1, kvh, nkv, slot, cv, cl,
+                          out + (size_t)(seq.row0[si] + q0 + i) * ldo + (size_t)hq * D);
 }
 
 struct Freqs {
@@ -1470,8 +1579,41 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
     return hipGetLastError();
 }
 
-hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &given, int nq, int nkv, int d, const CacheView &cv,
-                             const CacheLayer &cl, uint16_t *out, long long ldo, hipStream_t st)
+// Splits of a sequence over its tiles, from nothing but itself, so that its
+// results stay the same beside others: where its workgroups of four would fill at
+// most half of the chip's room for 512, as many as fill it, of at least eight
+// tiles each (starting a split and joining it cost about four), or 32 where more
+// than a quarter is filled already.  Heads of 8 over 32, at 8192 tokens: 1 row
+// 32 us, 231 unsplit; 256 rows 59, 234; 512 rows 93, 244.
+static int attn8_seq_splits(int rows, int start, int nq, int nkv)
+{
+    const int G = nq / nkv, tiles = (int)(((long long)start + rows + 63) / 64);
+    const long long wgs = (((long long)rows + 31) / 32 * G + 3) / 4 * nkv;
+    if (wgs > 256) return 1;
+    const int most = std::min({(int)(512 / wgs), tiles / (wgs > 128 ? 32 : 8), MOST_SPLITS});
+    if (most < 2) return 1;
+    const int per = (tiles + most - 1) / most;
+    return (tiles + per - 1) / per;                   // no split without tiles
+}
+
+static size_t part_bytes(int d) { return (d == 128 ? PART<128> : PART<64>) * sizeof(float); }
+
+// Splits times workgroups are at most 512, of at most four units each.
+size_t attn8_seq_ws_max(int d) { return 2048 * part_bytes(d); }
+
+size_t attn8_seqs_ws(const SeqTable &seq, int nq, int nkv, int d)
+{
+    size_t units = 0;
+    for (int i = 0; i < seq.n; ++i) {
+        const int ns = attn8_seq_splits(seq.len[i], seq.start[i], nq, nkv);
+        if (ns > 1) units += (size_t)ns * ((seq.len[i] + 31) / 32) * nq;
+    }
+    return units * part_bytes(d);
+}
+
+hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &given, int nq, int nkv, int d,
+                             const CacheView &cv, const CacheLayer &cl, uint16_t *out, long long ldo, float *ws,
+                             hipStream_t st)
 {
     const int G = nq / nkv, n = given.n;
     if (n < 1 || n > 64) return hipErrorInvalidValue;
@@ -1481,16 +1623,33 @@ hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &g
     for (int i = 0; i < n; ++i) by[i] = i;
     const auto keys = [&](int i) { return given.start[i] + given.len[i]; };
     std::stable_sort(by, by + n, [&](int a, int b) { return keys(a) > keys(b); });
-    SeqTable seq;
+    SeqTable seq, joined;
+    SplitTable sp, jp;
     seq.n = n;
+    joined.n = 0;
     long long groups8 = 0;
+    int parts = 0, join_units = 0;
     for (int i = 0; i < n; ++i) {
         seq.row0[i] = given.row0[by[i]];
         seq.len[i] = given.len[by[i]];
         seq.start[i] = given.start[by[i]];
         seq.slot[i] = given.slot[by[i]];
-        groups8 += ((seq.len[i] + 31) / 32 * G + 7) / 8;
+        sp.splits[i] = attn8_seq_splits(seq.len[i], seq.start[i], nq, nkv);
+        sp.part0[i] = parts;
+        groups8 += ((seq.len[i] + 31) / 32 * G + 7) / 8 * sp.splits[i];
+        if (sp.splits[i] == 1) continue;
+        const int units = (seq.len[i] + 31) / 32 * nq, j = joined.n++;
+        parts += units * sp.splits[i];
+        joined.row0[j] = seq.row0[i];
+        joined.len[j] = seq.len[i];
+        joined.start[j] = seq.start[i];
+        joined.slot[j] = seq.slot[i];
+        joined.unit0[j] = join_units;
+        jp.splits[j] = sp.splits[i];
+        jp.part0[j] = sp.part0[i];
+        join_units += units;
     }
+    if (joined.n > 0 && ws == nullptr) return hipErrorInvalidValue;
     // Eight wavefronts share a tile's conversion; four are twice the workgroups,
     // and a tile takes them 1.7 us on a CU of their own where eight need 1.9.
     // Heads of 128 take four where eight would leave half of the 256 CUs idle
@@ -1502,12 +1661,13 @@ hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &g
     int groups = 0;
     for (int i = 0; i < n; ++i) {
         seq.unit0[i] = groups;
-        groups += ((seq.len[i] + 31) / 32 * G + NW - 1) / NW;
+        groups += ((seq.len[i] + 31) / 32 * G + NW - 1) / NW * sp.splits[i];
     }
     const dim3 grid((unsigned)groups * nkv);
     const bool paged = cv.kv.layout == 1;
 #define CORUN_PREFILL8(D_, P_, NW_) \
-    KLAUNCH((k_attn8_prefill<D_, P_, NW_>), grid, dim3(64 * NW_), 0, st, q, ldq, seq, G, nkv, cv, cl, out, ldo)
+    KLAUNCH((k_attn8_prefill<D_, P_, NW_>), grid, dim3(64 * NW_), 0, st, q, ldq, seq, sp, G, nkv, cv, cl, out, ldo, \
+            ws)
     if (d == 128 && paged && NW == 8) CORUN_PREFILL8(128, true, 8);
     else if (d == 128 && paged) CORUN_PREFILL8(128, true, 4);
     else if (d == 128 && NW == 8) CORUN_PREFILL8(128, false, 8);
@@ -1516,6 +1676,13 @@ hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &g
     else if (d == 64) CORUN_PREFILL8(64, false, 4);
     else return hipErrorInvalidValue;
 #undef CORUN_PREFILL8
+    if (joined.n > 0) {
+        const dim3 jgrid(join_units, d / 32);
+        if (d == 128)
+            KLAUNCH((k_attn8_join<128>), jgrid, dim3(256), 0, st, ws, q, ldq, joined, jp, G, nkv, cv, cl, out, ldo);
+        else
+            KLAUNCH((k_attn8_join<64>), jgrid, dim3(256), 0, st, ws, q, ldq, joined, jp, G, nkv, cv, cl, out, ldo);
+    }
     return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
 // cache_ops.cpp -- the cache operators of include/corun.h: host-side checks,
-// then one launch (two for decode attention of long rows).  Nothing here
+// then one launch (two for attention that is split).  Nothing here
 // allocates, waits or keeps anything from one call for the next.
 #include "cache_ops.h"
 
@@ -178,10 +178,11 @@ corun_status check_step_rows(const corun_kv *kv, int32_t rows)
     return CORUN_OK;
 }
 
+// slots == nullptr: only the sizes are looked at
 corun_status sequences(const corun_kv *kv, int32_t n, const int32_t *lens, const int32_t *starts, const int32_t *slots,
                        SeqTable *out)
 {
-    if (!lens || !slots) return set_error(CORUN_E_INVAL, "null argument");
+    if (!lens) return set_error(CORUN_E_INVAL, "null argument");
     if (n < 1 || n > CORUN_MAX_PREFILL_BATCH)
         return set_errorf(CORUN_E_INVAL, "n = %d outside [1, %d]", n, CORUN_MAX_PREFILL_BATCH);
     static_assert(CORUN_MAX_PREFILL_BATCH == sizeof(SeqTable::len) / sizeof(int), "a call's sequences fit the table");
@@ -195,14 +196,15 @@ corun_status sequences(const corun_kv *kv, int32_t n, const int32_t *lens, const
         if ((long long)start + lens[i] > cap)
             return set_errorf(CORUN_E_CAPACITY, "sequence %d: positions %d .. %lld exceed the cache capacity %lld", i, start,
                               (long long)start + lens[i] - 1, cap);
-        if (slots[i] < 0 || slots[i] >= kv->n_slots)
-            return set_errorf(CORUN_E_INVAL, "slots[%d] = %d outside [0, %d)", i, slots[i], kv->n_slots);
-        for (int j = 0; j < i; ++j)
-            if (slots[j] == slots[i]) return set_errorf(CORUN_E_INVAL, "slot %d given twice", slots[i]);
+        const int slot = slots ? slots[i] : 0;
+        if (slot < 0 || slot >= kv->n_slots)
+            return set_errorf(CORUN_E_INVAL, "slots[%d] = %d outside [0, %d)", i, slot, kv->n_slots);
+        for (int j = 0; slots && j < i; ++j)
+            if (slots[j] == slot) return set_errorf(CORUN_E_INVAL, "slot %d given twice", slot);
         out->row0[i] = (int)rows;
         out->len[i] = lens[i];
         out->start[i] = start;
-        out->slot[i] = slots[i];
+        out->slot[i] = slot;
         rows += lens[i];
     }
     if (rows > (1 << 24)) return set_errorf(CORUN_E_SHAPE, "%lld rows in one call: at most 2^24", rows);
@@ -219,6 +221,14 @@ corun_status check_total(long long rows, long long heads, int log2_most)
 }
 
 long long rows_of(const SeqTable &seq) { return (long long)seq.row0[seq.n - 1] + seq.len[seq.n - 1]; }
+
+corun_status check_ws(const void *ws, int64_t bytes, int64_t need)
+{
+    if (need > 0 && (!ws || !aligned16(ws))) return set_error(CORUN_E_INVAL, "the workspace must start on 16 bytes");
+    if (bytes < need)
+        return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)bytes, (long long)need);
+    return CORUN_OK;
+}
 
 corun_status launched(hipError_t e)
 {
@@ -279,6 +289,7 @@ extern "C" corun_status corun_prefill_append(const corun_kv *kv, int32_t layer, 
     TRY(check_heads(kv, n_heads, n_kv_heads, d));
     CacheLayer cl;
     TRY(layer_of(kv, layer, &cl));
+    if (!slots) return set_error(CORUN_E_INVAL, "null argument");
     SeqTable seq;
     TRY(sequences(kv, n, lens, starts, slots, &seq));
     TRY(check_rows("qkv", qkv, ld_qkv, (int64_t)(n_heads + 2 * n_kv_heads) * d));
@@ -314,9 +325,7 @@ extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * head_dim));
     TRY(check_rows("out", out, ld_out, (int64_t)n_heads * head_dim));
     if (!lens) return set_error(CORUN_E_INVAL, "null lens");
-    if (need > 0 && (!ws || !aligned16(ws))) return set_error(CORUN_E_INVAL, "the workspace must start on 16 bytes");
-    if (ws_bytes < need)
-        return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)ws_bytes, (long long)need);
+    TRY(check_ws(ws, ws_bytes, need));
     const CacheView cv = cache_view(kv);
     const int most = longest(kv, max_len), chunk = attn8_chunk(rows, n_kv_heads, most);
     const bool one = chunk >= most;                    // one split to a row: written straight to out
@@ -328,19 +337,31 @@ extern "C" corun_status corun_decode_attention(const corun_kv *kv, int32_t layer
                                        (uint16_t *)out, ld_out, (hipStream_t)stream));
 }
 
+extern "C" int64_t corun_prefill_attention_workspace(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads,
+                                                     int32_t head_dim, int32_t n, const int32_t *lens,
+                                                     const int32_t *starts)
+{
+    TRY(check_attention(kv, n_heads, n_kv_heads, head_dim));
+    SeqTable seq;
+    TRY(sequences(kv, n, lens, starts, nullptr, &seq));
+    return (int64_t)attn8_seqs_ws(seq, n_heads, n_kv_heads, head_dim);
+}
+
 extern "C" corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
                                                 int32_t head_dim, int32_t n, const int32_t *lens, const int32_t *starts,
                                                 const int32_t *slots, const void *q, int64_t ld_q, void *out,
-                                                int64_t ld_out, void *stream)
+                                                int64_t ld_out, void *ws, int64_t ws_bytes, void *stream)
 {
     TRY(check_attention(kv, n_heads, n_kv_heads, head_dim));
     CacheLayer cl;
     TRY(layer_of(kv, layer, &cl));
+    if (!slots) return set_error(CORUN_E_INVAL, "null argument");
     SeqTable seq;
     TRY(sequences(kv, n, lens, starts, slots, &seq));
     TRY(check_total(rows_of(seq), n_heads, 30));
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * head_dim));
     TRY(check_rows("out", out, ld_out, (int64_t)n_heads * head_dim));
+    TRY(check_ws(ws, ws_bytes, (int64_t)attn8_seqs_ws(seq, n_heads, n_kv_heads, head_dim)));
     return launched(launch_attn8_seqs((const uint16_t *)q, ld_q, seq, n_heads, n_kv_heads, head_dim, cache_view(kv), cl,
-                                      (uint16_t *)out, ld_out, (hipStream_t)stream));
+                                      (uint16_t *)out, ld_out, (float *)ws, (hipStream_t)stream));
 }

@@ -446,7 +446,7 @@ struct corun_engine {
     int pf_max = 0;
     char *pws = nullptr;
     size_t pws_bytes = 0;
-    float *pf_x = nullptr, *pf_part = nullptr, *pf_logits = nullptr;
+    float *pf_x = nullptr, *pf_part = nullptr, *pf_logits = nullptr, *pf_split = nullptr;
     uint16_t *pf_h = nullptr, *pf_q = nullptr, *pf_o = nullptr, *pf_a = nullptr, *pf_hlast = nullptr;
     int32_t *pf_pos = nullptr, *pf_tok = nullptr, *pf_next = nullptr;
     int32_t *pf_rowpos = nullptr, *pf_rowslot = nullptr, *pf_seq = nullptr;   // batched prefill
@@ -1248,6 +1248,10 @@ static corun_status alloc_prefill(corun_engine *e)
             cv.take(&e->rt_pf_logit, (size_t)c.n_layers * L * c.n_experts);
         }
     }
+    // e4m3: what the attention's splits of a call's sequences leave (of a batch,
+    // whose prompts start at 0, only those of more than 960 tokens are split)
+    const int split_seqs = bi_pf ? std::clamp(L / 960, 1, CORUN_MAX_PREFILL_BATCH) : 1;
+    cv.take(&e->pf_split, e->e4m3 ? split_seqs * attn8_seq_ws_max(d) / sizeof(float) : 4);
     cv.take(&e->pf_pos, (size_t)std::max(L, kv_capacity(&e->kv)));   // positions of any chunk
     cv.take(&e->pf_tok, (size_t)L);
     cv.take(&e->pf_amax, (size_t)lrows * gemm_col_blocks(c.vocab));
@@ -1258,7 +1262,7 @@ static corun_status alloc_prefill(corun_engine *e)
     e->pws_bytes = total;
     HIP_TRY(hipMalloc(&e->pws, total));
     HIP_TRY(hipMemsetAsync(e->pws, 0, total, e->st));
-    rebase(e->pf_x, e->pws); rebase(e->pf_part, e->pws); 
+    rebase(e->pf_x, e->pws); rebase(e->pf_part, e->pws); rebase(e->pf_split, e->pws);
     rebase(e->pf_logits, e->pws); rebase(e->pf_h, e->pws); rebase(e->pf_q, e->pws);
     rebase(e->pf_o, e->pws); rebase(e->pf_a, e->pws); rebase(e->pf_hlast, e->pws);
     if (e->moe) {
@@ -1734,7 +1738,7 @@ extern "C" corun_status corun_prefill_chunk(corun_engine *e, const int32_t *toke
         ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_pos + start, nullptr, slot, table));
         if (e->e4m3)
             HIP_TRY(launch_attn8_seqs(e->pf_q, (long long)nq * d, table, nq, nkv, d, e->cview, e->layers[l], e->pf_o,
-                                      (long long)nq * d, st));
+                                      (long long)nq * d, e->pf_split, st));
         else
             HIP_TRY(launch_prefill_attn(e->pf_q, Lp, start, nq, nkv, d, slot, e->kc[l], e->vc[l], e->view, e->pf_o, st));
         HIP_TRY(proj(e, e->pf_o, nq * d, W_O, l, po, Lp, e->pf_part, (long long)Lp * H, H));
@@ -1869,7 +1873,7 @@ extern "C" corun_status corun_prefill_batch(corun_engine *e, const int32_t *toke
         ST_TRY(prefill_qkv(e, l, pq, Lp, e->pf_rowpos, e->pf_rowslot, -1, table));
         if (e->e4m3)
             HIP_TRY(launch_attn8_seqs(e->pf_q, (long long)nq * d, table, nq, nkv, d, e->cview, e->layers[l], e->pf_o,
-                                      (long long)nq * d, st));
+                                      (long long)nq * d, e->pf_split, st));
         else
             HIP_TRY(launch_prefill_attn_multi(e->pf_q, e->pf_seq, n, groups, nq, nkv, d, e->kc[l], e->vc[l], e->view,
                                               e->pf_o, st));

@@ -361,6 +361,11 @@ struct SeqTable {
     int n = 0;
     int row0[64], len[64], start[64], slot[64], unit0[64];
 };
+// How they are split over their keys, and where their partial results start (in
+// units of 32 rows of a head).
+struct SplitTable {
+    int splits[64], part0[64];
+};
 
 // cos / sin table of frequencies freq[i] (radians per position) of the d / 2 half
 // pairs of a head, as launch_rope_table's.
@@ -392,8 +397,12 @@ hipError_t launch_attn8_split(const uint16_t *q, long long ldq, int rows, const 
 hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, const int32_t *lens, int plus_one, int nq,
                               int nkv, int d, int max_len, int chunk, uint16_t *out, long long ldo, hipStream_t st);
 // Causal attention of a prefill call's queries: row row0 + t of sequence i
-// sees tokens 0 .. start + t of its slot.
-hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &seq, int nq, int nkv, int d, const CacheView &cv,
-                             const CacheLayer &cl, uint16_t *out, long long ldo, hipStream_t st);
+// sees tokens 0 .. start + t of its slot (unit0 is not looked at).  ws:
+// attn8_seqs_ws bytes on a 16-byte boundary.
+size_t attn8_seqs_ws(const SeqTable &seq, int nq, int nkv, int d);
+size_t attn8_seq_ws_max(int d);                // the most that one sequence adds to it
+hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &given, int nq, int nkv, int d,
+                             const CacheView &cv, const CacheLayer &cl, uint16_t *out, long long ldo, float *ws,
+                             hipStream_t st);
 
 }  // namespace corun

@@ -44,9 +44,10 @@ def decode_attention(kv, nq=8, nkv=2, d=128, rows=2, q=P, ldq=1024, lens=P, max_
                                                ldo, ws, ws_bytes, None)
 
 
-def prefill_attention(kv, n=2, lens=(3, 4), starts=(0, 5), slots=(0, 1), nq=8, nkv=2, d=128, q=P, ldq=1024, out=P, ldo=1024):
+def prefill_attention(kv, n=2, lens=(3, 4), starts=(0, 5), slots=(0, 1), nq=8, nkv=2, d=128, q=P, ldq=1024, out=P, ldo=1024,
+                      ws=P, ws_bytes=1 << 40):
     return corun.load().corun_prefill_attention(C.addressof(kv), 0, nq, nkv, d, n, _i32(*lens), _i32(*starts),
-                                                _i32(*slots), q, ldq, out, ldo, None)
+                                                _i32(*slots), q, ldq, out, ldo, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw", [
@@ -179,3 +180,31 @@ def test_launch_limits_refused():
     assert prefill_attention(kv, nq=128, nkv=8, ldq=128 * 128, ldo=128 * 128, **args) == corun.E_SHAPE
     args["lens"][0] += 16
     assert prefill_attention(_kv(n_slots=16, max_seq_len=1 << 21), **args) == corun.E_SHAPE      # over 2^24 rows
+
+
+def prefill_workspace(kv, lens, starts=None, nq=8, nkv=2, d=128):
+    return corun.load().corun_prefill_attention_workspace(C.addressof(kv), nq, nkv, d, len(lens), _i32(*lens),
+                                                          _i32(*starts) if starts else None)
+
+
+def test_prefill_workspace_and_its_refusals():
+    kv = _kv(max_seq_len=1 << 14)
+    unit = 4 * (32 * 128 + 64)                        # a split's rows of a head, their maxima and sums
+    # 33 rows behind 4000 tokens: two blocks of rows, four workgroups, 64 tiles: eight splits of eight
+    assert prefill_workspace(kv, [33], [4000]) == 8 * 2 * 8 * unit
+    assert prefill_workspace(kv, [33], [4000], d=64) == 8 * 2 * 8 * 4 * (32 * 64 + 64)
+    assert prefill_workspace(kv, [33, 5, 33], [4000, 0, 4000]) == 16 * 2 * 8 * unit
+    assert prefill_workspace(kv, [900]) == 0          # 15 tiles
+    assert prefill_workspace(kv, [2049], [8000]) == 3 * 65 * 8 * unit   # 130 workgroups, 158 tiles
+    assert prefill_workspace(kv, [2049], [1900]) == 0
+    assert prefill_workspace(kv, [4100], [8000]) == 0  # 129 blocks of rows: 258 workgroups
+    assert prefill_workspace(kv, [0]) == corun.E_INVAL
+    assert prefill_workspace(kv, [1], [1 << 14]) == corun.E_CAPACITY
+    assert prefill_workspace(kv, [1], nq=9) == corun.E_SHAPE
+    args = dict(n=1, lens=[33], starts=[4000], slots=[1])
+    need = prefill_workspace(kv, [33], [4000])
+    assert prefill_attention(kv, ws=None, **args) == corun.E_INVAL
+    assert prefill_attention(kv, ws=P + 8, **args) == corun.E_INVAL
+    assert prefill_attention(kv, ws_bytes=need - 1, **args) == corun.E_CAPACITY
+    assert prefill_attention(kv, ws=None, ws_bytes=0, **args) == corun.E_INVAL
+    assert prefill_attention(kv, ws=None, ws_bytes=-1, n=1, lens=[3], starts=[0], slots=[0]) == corun.E_CAPACITY

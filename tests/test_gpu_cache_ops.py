@@ -539,6 +539,73 @@ def test_prefill_attention_of_many_rows_and_long_sequences(page):
 
 
 
+@pytest.mark.parametrize("d,nkv,G,n,start,blk,page", [
+    (128, 2, 1, 1, 4990, 64, 0), (64, 1, 3, 70, 3001, 16, 48), (128, 8, 4, 33, 2047, 32, 32), (128, 1, 16, 100, 4000, 64, 192),
+    (64, 4, 8, 129, 1100, 32, 0), (128, 4, 7, 31, 1025, 16, 16)])
+def test_prefill_attention_of_few_rows_behind_many(d, nkv, G, n, start, blk, page):
+    """Sequences that are split over their keys: alone, beside others, and with whatever was in the workspace."""
+    cap = (start + n + 767) // 768 * 768
+    hc = HostCache(nkv, d, 3, cap, blk, page, seed=76)
+    cache = hc.device_cache(corun)
+    lens, starts, slots = [40, n, 5], [0, start, 1600 if start > 2000 else 7], [1, 2, 0]
+    x, q = rows_of(sum(lens), nkv * G, d, 77, pad=8, loud=False)
+    need = corun.prefill_attention_workspace(cache, nkv * G, lens, starts)
+    assert need >= corun.prefill_attention_workspace(cache, nkv * G, [n], [start]) > 0
+    out = run_prefill(cache, q, lens, starts, slots)
+    check_prefill(hc, x, out, seqs_of(lens, starts, slots), every=max(1, n // 5))
+    alone = torch.full((n, nkv * G * d), 5.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)     # NaN, were any of it read before it is written
+    corun.prefill_attention(cache, 0, q[40:40 + n], [n], [start], [2], alone, ws=ws)
+    torch.cuda.synchronize()
+    assert same(alone.cpu(), out[40:40 + n])
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_prefill_attention_split_rows_with_nan_and_bad_pages(page):
+    """NaN values and a lost page inside a split: rows before them are as without, rows behind are NaN."""
+    d, nkv, G, blk, n, start, cap = 128, 1, 2, 32, 300, 2000, 2304
+    hc = HostCache(nkv, d, 1, cap, blk, page, seed=78)
+    x, q = rows_of(n, nkv * G, d, 79, loud=False)
+    assert corun.prefill_attention_workspace(hc.device_cache(corun), nkv * G, [n], [start]) > 0
+    good = run_prefill(hc.device_cache(corun), q, [n], [start], [0])
+    check_prefill(hc, x, good, [(0, n, start, 0)], every=60)
+    a, b = hc.at(0, 2150)
+    code = int(hc.v[a, 0, b, 11])
+    hc.v[a, 0, b, 11] = 0x7F
+    out = run_prefill(hc.device_cache(corun), q, [n], [start], [0])
+    dims = torch.arange(nkv * G * d) % d == 11
+    assert torch.equal(torch.isnan(out), (torch.arange(n) >= 150)[:, None] & dims[None])
+    assert same(out[:96], good[:96])                  # units that take the tile of the NaN do their rows another way
+    hc.v[a, 0, b, 11] = code
+    check_prefill(hc, x, torch.where(dims[None], good, out), [(0, n, start, 0)], every=23)
+    hc.v[a, 0, b, 11] = 0x7F
+    if page:
+        hc.table[0, 34] = hc.k.shape[0]               # tokens 2176 ..
+        out = run_prefill(hc.device_cache(corun), q, [n], [start], [0])
+        assert torch.isnan(out[176:]).all() and not torch.isnan(out[:150]).any() and same(out[:96], good[:96])
+
+
+def test_prefill_attention_split_replays_from_a_graph():
+    d, nkv, G, blk, n, start, cap = 128, 2, 4, 32, 50, 3000, 3136
+    hc = HostCache(nkv, d, 2, cap, blk, seed=80)
+    cache = hc.device_cache(corun)
+    qs = [rows_of(n, nkv * G, d, 81 + i)[1] for i in range(3)]
+    want = [run_prefill(cache, q, [n], [start], [1]) for q in qs]
+    q, out = qs[0].clone(), torch.zeros_like(qs[0])
+    ws = torch.zeros(corun.prefill_attention_workspace(cache, nkv * G, [n], [start]), dtype=torch.uint8, device=DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        corun.prefill_attention(cache, 0, q, [n], [start], [1], out, ws=ws)
+    for i in (1, 0, 2, 1):
+        q.copy_(qs[i])
+        out.zero_()
+        ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        assert same(out.cpu(), want[i])
+
+
+
 # --------------------------------------------------------------------------
 # Together, as a layer calls them
 # --------------------------------------------------------------------------
