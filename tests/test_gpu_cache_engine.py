@@ -5,8 +5,6 @@ reads the engine's cache as the engine left it (codes times scales), so that a
 code's rounding, checked on its own, does not move the comparison.  Then the
 properties that every engine here has: position invariance, replays, chunks,
 batched prompts, the scheduler."""
-import ctypes as C
-
 import numpy as np
 import pytest
 import torch
@@ -26,7 +24,7 @@ B, CAP = 6, 384
 class Setup:
     """An engine with its caches; e4m3 ones start as stale random codes."""
 
-    def __init__(self, name="small128", blk=32, page=0, rope=None, seed=5, slots=None, pf=320, Bf=B, W=None, stale=True, **opt):
+    def __init__(self, name="small128", blk=32, page=0, rope=None, seed=5, slots=None, pf=320, Bf=B, W=None, **opt):
         self.cfg = wl.config(name)
         self.Wc = wl.make_weights(self.cfg, seed=51) if W is None else W
         self.W = to_device(self.Wc)
@@ -218,6 +216,24 @@ def test_batched_prompts_are_their_own_prefill():
     for i, (p, sl) in enumerate(zip(prompts, [0, 2, 4, 3])):
         assert s.eng.prefill(p, sl, one) == toks[i] and torch.equal(one, lg[i])
         assert all(torch.equal(x, y) for a, b in zip(together[i], s.bits(sl, len(p))) for x, y in zip(a, b))
+
+
+def test_long_prompts_and_chunks_behind_them(monkeypatch):
+    """Sequences that attention splits over their keys: batched and alone, and a chunk against the reference."""
+    monkeypatch.setitem(globals(), "CAP", 1536)
+    s = Setup("tiny", 32, 0, pf=2432, slots=B, bi_prefill=True)
+    V_ = s.cfg["vocab"]
+    prompts = [wl.make_prompt(V_, n, seed=n) for n in (1300, 60, 1024)]
+    lg = torch.empty((3, V_), dtype=torch.float32, device=DEV)
+    toks = s.eng.prefill_batch(prompts, [3, 0, 5], lg)
+    together = [s.bits(sl, len(p)) for p, sl in zip(prompts, [3, 0, 5])]
+    one = torch.empty(V_, dtype=torch.float32, device=DEV)
+    for i, (p, sl) in enumerate(zip(prompts, [1, 2, 4])):
+        assert s.eng.prefill(p, sl, one) == toks[i] and torch.equal(one, lg[i])
+        assert all(torch.equal(x, y) for a, b in zip(together[i], s.bits(sl, len(p))) for x, y in zip(a, b))
+    more = wl.make_prompt(V_, 70, seed=9)
+    s.eng.prefill_chunk(more, 1300, 1, one)
+    close(one, follow(s, more, 1300, 1))
 
 
 def test_moe_engine_on_an_e4m3_cache():
