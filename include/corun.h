@@ -159,7 +159,8 @@ typedef struct {
 /* Creation options; pass NULL for defaults (all fields 0). */
 typedef struct {
     int32_t attn_chunk;        /* split-KV chunk in tokens (multiple of 64); 0 = chosen from (model, B, capacity);
-                                  a chunk >= the capacity turns split-KV off (one split per row) */
+                                  a chunk >= the capacity turns split-KV off (one split per row); below 2048
+                                  splits on an e4m3 cache */
     int32_t max_prefill_len;   /* prefill workspace in tokens; 0 = none (corun_prefill returns CORUN_E_STATE) */
     int32_t no_graph;          /* 1 = launch the step's kernels eagerly instead of replaying the captured graph */
     int32_t poison_workspace;  /* 1 = fill the workspace with NaN bit patterns at creation (test aid) */

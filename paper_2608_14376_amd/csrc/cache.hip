@@ -577,8 +577,9 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
 // Bound by reading the cache: 162 rows of 512 to 4096 tokens (8 kv heads of 128)
 // take 147 us, 5.2 TB/s, which is what a large copy reaches; 32 paged rows of 1024
 // to 32768 tokens 127 us, 4.7 TB/s, where the longest row's last splits run alone.
-// Three workgroups of 33 KB to a CU keep enough loads in flight; the weights' bf16 halves hi + lo cost matrix instructions that the
-// loads leave idle, where one bf16 weight would lose 8 bits.
+// Three workgroups of 33 KB to a CU keep enough loads in flight; the weights' bf16
+// halves hi + lo cost matrix instructions that the loads leave idle, where one bf16
+// weight would lose 8 bits.
 // ---------------------------------------------------------------------------
 
 // Transposed LDS read of bytes (ds_read_b64_tr_b8): in each group of 16 lanes,

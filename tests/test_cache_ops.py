@@ -208,3 +208,15 @@ def test_prefill_workspace_and_its_refusals():
     assert prefill_attention(kv, ws_bytes=need - 1, **args) == corun.E_CAPACITY
     assert prefill_attention(kv, ws=None, ws_bytes=0, **args) == corun.E_INVAL
     assert prefill_attention(kv, ws=None, ws_bytes=-1, n=1, lens=[3], starts=[0], slots=[0]) == corun.E_CAPACITY
+
+
+def test_engine_chunks_that_make_too_many_splits():
+    cfg = corun.model_cfg(dict(n_layers=1, hidden=256, n_heads=4, n_kv_heads=2, head_dim=64, ffn=688, vocab=1024, n_experts=0,
+                               top_k=0, expert_ffn=0, rms_eps=1e-6, rope_theta=10000.0))
+    out = (C.c_int32 * 64)()
+    for chunk, ok in ((64, False), (128, True), (0, True)):
+        kv, opt = _kv(max_seq_len=2048 * 64), corun.options(attn_chunk=chunk)
+        n = corun.load().corun_describe_plan(C.byref(cfg), C.byref(kv), 2, C.byref(opt), C.addressof(out), 64)
+        assert n > 0 if ok else n == corun.E_INVAL
+    kv, opt = _kv(max_seq_len=2048 * 64, dtype=corun.KV_BF16), corun.options(attn_chunk=64)
+    assert corun.load().corun_describe_plan(C.byref(cfg), C.byref(kv), 2, C.byref(opt), C.addressof(out), 64) > 0
