@@ -605,7 +605,7 @@ def cpu_baseline(cfg, W, res, budget_s=12.0):
 def kernel_source_sha():
     import hashlib
     h = hashlib.sha256()
-    for f in ("kernels.hip", "kernels.h"):
+    for f in ("kernels.hip", "kernels.h", "device.h"):
         h.update(open(os.path.join(ROOT, "paper_2608_14376_amd", "csrc", f), "rb").read())
     return h.hexdigest()[:16]
 

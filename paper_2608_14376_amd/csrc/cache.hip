@@ -20,8 +20,8 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "cache.h"
 #include "device.h"
-#include "kernels.h"
 
 namespace corun {
 namespace {

@@ -1,8 +1,8 @@
 // cache_ops.h -- a corun_kv's checks and its kernels' view of it, shared by
 // the engine and the cache operators.
 #pragma once
+#include "cache.h"
 #include "corun.h"
-#include "kernels.h"
 
 namespace corun {
 

@@ -34,7 +34,7 @@ XCDS = 8
 
 def source_sha() -> str:
     h = hashlib.sha256()
-    for f in ("kernels.hip", "kernels.h"):
+    for f in ("kernels.hip", "kernels.h", "device.h"):
         h.update(open(os.path.join(HERE, "csrc", f), "rb").read())
     return h.hexdigest()[:16]
 
