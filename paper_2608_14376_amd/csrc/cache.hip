@@ -947,9 +947,8 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // to a wavefront, on shared key and value tiles.  A tile's codes are read into
 // registers one tile ahead, and become 16-bit LDS rows once for all its
 // wavefronts: keys in bf16 with their scale (exact), values in fp16 under a
-// common exponent `top`, the largest scale of the values so far (exact down to
-// 2^-15 of it; what is smaller yet keeps an absolute error of 2^-25 of that
-// scale).  fp16 weights keep 11 bits where bf16 would keep 8.
+// common exponent `top`, the largest scale of the values so far: exact down to
+// 2^-21 of it.  fp16 weights keep 11 bits where bf16 would keep 8.
 //  * S^T = K Q^T on v_mfma_f32_32x32x16_bf16, two 32 x 32 tiles, key rows
 //    permuted (pf_key_of_row) so that lane l ends with eight consecutive keys
 //    16 s + 8 (l / 32) .. + 7 of each step s of query l % 32: the P^T operand of
@@ -964,8 +963,9 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // row base are scalars and the loop has no vector address arithmetic.  Future keys
 // and those past the sequence are masked by selection, value codes past it are
 // cleared.  A NaN among the values would reach queries that do not see it
-// (0 NaN), and a page that is none is read as page 0: a wavefront whose sums
-// hold a NaN, or whose keys reach such a page, does its rows again one by one
+// (0 NaN), values too small for the exponent, be it a later token's, would lose
+// bits, and a page that is none is read as page 0: a wavefront whose sums hold a
+// NaN, or whose keys reach such a group, does its rows again one by one
 // (attend_row); a split notes a NaN maximum for such a row and the join does it.
 //
 // Bound by the matrix units and the softmax's arithmetic of one wavefront in turn:
@@ -1083,7 +1083,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     constexpr int OPITCH = D + 8;
     constexpr int LDS_UNITS = 4 * UNITS > NW * QB * OPITCH / 8 ? 4 * UNITS : NW * QB * OPITCH / 8;
     __shared__ __attribute__((aligned(16))) uint4 ring[LDS_UNITS];    // two key tiles, two value tiles; the output
-    __shared__ int lost;
+    __shared__ int redo;
 
     const int kvh = blockIdx.x % nkv;
     const int si = seq_of(seq, blockIdx.x / nkv), in_seq = (int)(blockIdx.x / nkv) - seq.unit0[si];
@@ -1132,7 +1132,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
         l_idx = t / ps;
         l_in += t % ps;
     }
-    int first_bad = INT32_MAX;                        // first group that this wavefront found on a page that is none
+    // Rows from here on are done again: the first group that this wavefront found
+    // on a page that is none, or whose values are too small for the exponent.
+    int redo_from = INT32_MAX;
     auto fetch_pages = [&]() {
         if constexpr (PAGED) {
 #pragma unroll
@@ -1163,7 +1165,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
             if constexpr (PAGED) {
                 int pg = __builtin_amdgcn_readfirstlane(page[r]);
                 if ((unsigned)pg >= (unsigned)cv.num_pages) {
-                    first_bad = min(first_bad, t16);
+                    redo_from = min(redo_from, t16);
                     pg = 0;
                 }
                 const size_t head = (size_t)pg * nkv + kvh;
@@ -1210,7 +1212,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
                 w = (uint4){w.x & use, w.y & use, w.z & use, w.w & use};
             }
             const int grp16 = sub + ROWS / 16 * r;
-            const int e = max((grp16 == 0 ? v0 : grp16 == 1 ? v1 : grp16 == 2 ? v2 : v3) - top + V_UP, -60);
+            const int up = (grp16 == 0 ? v0 : grp16 == 1 ? v1 : grp16 == 2 ? v2 : v3) - top, e = max(up + V_UP, -60);
+            // 2^-9 times this is below 2^-24: codes lose bits (codes of zero excepted)
+            if (up < -21 && __ballot(((w.x | w.y | w.z | w.w) & 0x7f7f7f7fu) != 0u)) redo_from = min(redo_from, k0 + 16 * grp16);
             codes_16<true>(w, exp2_int(e), lo, hi);
             V[rw * KCH + ((2 * c) ^ val16_swz<KCH>(rw))] = lo;
             V[rw * KCH + ((2 * c + 1) ^ val16_swz<KCH>(rw))] = hi;
@@ -1231,13 +1235,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
     float mrow = -INFINITY, lpart = 0.f;              // reference and sum of the lane's own keys
+    bool shrunk = false;
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);   // log2(e) / sqrt(d)
     const int qq = p0 + q0 + r32;
     // operand addresses in a tile: key unit 2 s + h of the row that this lane's
     // MFMA row stands for; transposed value reads (see vread)
     const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
 
-    if (tid == 0) lost = INT32_MAX;
+    if (tid == 0) redo = INT32_MAX;
     int top_next = 0;
     fetch_pages();
     load();
@@ -1328,6 +1333,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
             const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
             const float a = alpha * exp2_int(max(top_acc - top, -126));
             lpart *= alpha;
+            if (top - top_acc > 100) {                // the sums may lose bits: shrunk unless they are zero
+                float any = 0.f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) any = fmaxf(any, fabsf(acc[dt][j]));
+                shrunk |= any > 0.f;
+            }
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -1360,11 +1373,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if (PAGED && lane == 0 && first_bad != INT32_MAX) atomicMin(&lost, first_bad);
+    if (lane == 0 && redo_from != INT32_MAX) atomicMin(&redo, redo_from);
     __syncthreads();                                  // every wavefront is done with the tiles
 
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]
-    bool nan = false;
+    bool nan = shrunk;
     const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
     const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]), inv = 1.0f / sum;
     if (ns > 1) {
@@ -1383,7 +1396,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
                 nan |= v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w;
                 *(float4 *)(part + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = v;
             }
-        const unsigned long long bad = __ballot(nan || lost <= qq);
+        const unsigned long long bad = __ballot(nan || redo <= qq);
         if (h == 0) *(float2 *)(part + 32 * D + 2 * r32) = {((bad | bad >> 32) >> r32) & 1 ? QNAN : mrow, sum};
         return;
     }
@@ -1402,7 +1415,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wavefront's staging writes are done
     if (!active) return;
-    if (lost <= my_last_q || __ballot(nan && q0 + r32 < n)) {
+    if (redo <= my_last_q || __ballot(nan && q0 + r32 < n)) {
 #pragma unroll 1
         for (int r = 0; r < QB && q0 + r < n; ++r)
             attend_row<D>(q + (size_t)(q0 + r) * ldq + (size_t)hq * D, p0 + q0 + r + 1, kvh, nkv, slot, cv, cl,

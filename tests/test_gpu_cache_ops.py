@@ -606,6 +606,24 @@ def test_prefill_attention_split_replays_from_a_graph():
 
 
 
+@pytest.mark.parametrize("d,G,page,start", [(128, 4, 0, 0), (64, 2, 48, 0), (128, 2, 16, 1000)])
+def test_prefill_attention_values_of_any_size(d, G, page, start):
+    """Blocks of values many powers of two apart, empty ones, and huge ones that a query does not see yet."""
+    nkv, blk, n = 2, 16, 220
+    cap = 1248 if start else 240
+    hc = HostCache(nkv, d, 1, cap, blk, page, seed=90)
+    first = start // blk
+    for i, byte in ((0, 121), (1, 60), (2, 27), (3, 118), (4, 240), (5, 121), (6, 27), (7, 150), (8, 121), (9, 245), (10, 100)):
+        a, b = hc.at(0, (first + i) * blk)
+        hc.vs[a, i % 2, b // blk] = byte
+        if i in (2, 6):
+            hc.v[a, i % 2, b:b + blk] = 0             # what an append of zeros leaves
+    x, q = rows_of(n, nkv * G, d, 91, loud=False)
+    out = run_prefill(hc.device_cache(corun), q, [n], [start], [0])
+    check_prefill(hc, x, out, [(0, n, start, 0)], every=3)
+
+
+
 # --------------------------------------------------------------------------
 # Together, as a layer calls them
 # --------------------------------------------------------------------------
