@@ -141,7 +141,9 @@ __device__ __forceinline__ float to_odd(double y)
 // sines while it goes from head to head: two runs of eight elements from a0 and
 // b0 on, (8 j, 8 j + rot / 2) for rotated half pairs, otherwise the 16
 // elements from 16 j on, whose pairs stand side by side.  Half pairs of a rot
-// that is no multiple of 16 are read one element at a time (VEC false).
+// that is no multiple of 16 are read one element at a time (VEC false), pair j +
+// t D / 16 in turn, so that a token's threads read side by side (4000 tokens of 32 +
+// 8 + 8 heads, rot 52: 43 us, 78 with eight pairs in a row; rot 64, in runs: 25).
 //
 // q is rotated in fp32 and rounded once to bf16, as are bf16 keys.  Keys that
 // become codes are rotated in 64 bits and rounded to odd, so that a code is the
@@ -152,24 +154,25 @@ __device__ __forceinline__ float to_odd(double y)
 // 8 heads of 128 in 282 us, 4.5 TB/s (a large copy reaches 5.2); cosines are made
 // once per token and pair instead of per head or read from a table.
 // ---------------------------------------------------------------------------
-template <bool VEC>
+template <int D, bool VEC>
 struct Pairs {
-    int a0, b0, first, rot2;       // runs; first pair; rotated pairs of the head
+    int j, a0, b0, rot2;           // thread of the token; runs; rotated pairs of the head
     bool half;
 
-    __device__ __forceinline__ Pairs(const RopeArgs &r, int j)
+    __device__ __forceinline__ Pairs(const RopeArgs &r, int j_)
     {
-        first = 8 * j;
+        j = j_;
         rot2 = r.rot / 2;
-        half = !r.interleaved && first < rot2;
+        half = !r.interleaved && 8 * j < rot2;
         a0 = half ? 8 * j : 16 * j;
         b0 = half ? 8 * j + rot2 : 16 * j + 8;
     }
-    __device__ __forceinline__ bool rotated(int t) const { return first + t < rot2; }
+    __device__ __forceinline__ int pair(int t) const { return VEC ? 8 * j + t : j + t * (D / 16); }
+    __device__ __forceinline__ bool rotated(int t) const { return pair(t) < rot2; }
     // element offsets of pair t where the runs do not hold it
     __device__ __forceinline__ int at(int t, int which) const
     {
-        const int i = first + t;
+        const int i = pair(t);
         return i < rot2 ? i + which * rot2 : 2 * i + which;
     }
 };
@@ -177,11 +180,12 @@ struct Pairs {
 // Cosines and sines of a thread's pairs at a position.
 struct Turn64 {
     double c[8], s[8];
-    __device__ __forceinline__ void init(const RopeArgs &r, int first, int pos)
+    template <class P>
+    __device__ __forceinline__ void init(const RopeArgs &r, const P &p, int pos)
     {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-            turn_cos_sin(r.turns[first + t], (double)pos, c[t], s[t]);
+            turn_cos_sin(r.turns[p.pair(t)], (double)pos, c[t], s[t]);
             c[t] *= r.mag;
             s[t] *= r.mag;
         }
@@ -196,7 +200,7 @@ struct Raw {
 };
 
 template <int D, bool VEC>
-__device__ __forceinline__ Raw load_raw(const QkvRows &in, const Pairs<VEC> &p, long long row, int head)
+__device__ __forceinline__ Raw load_raw(const QkvRows &in, const Pairs<D, VEC> &p, long long row, int head)
 {
     const size_t off = (size_t)row * in.ld + (size_t)head * D;
     Raw r;
@@ -243,8 +247,8 @@ __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // The pairs' first and second elements.
-template <bool VEC>
-__device__ __forceinline__ void to_pairs(const Raw &r, const Pairs<VEC> &p, float (&x0)[8], float (&x1)[8])
+template <int D, bool VEC>
+__device__ __forceinline__ void to_pairs(const Raw &r, const Pairs<D, VEC> &p, float (&x0)[8], float (&x1)[8])
 {
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
@@ -258,8 +262,8 @@ __device__ __forceinline__ void to_pairs(const Raw &r, const Pairs<VEC> &p, floa
     }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void rotate(const Pairs<VEC> &p, const float (&c)[8], const float (&s)[8], float (&x0)[8],
+template <int D, bool VEC>
+__device__ __forceinline__ void rotate(const Pairs<D, VEC> &p, const float (&c)[8], const float (&s)[8], float (&x0)[8],
                                        float (&x1)[8])
 {
 #pragma unroll
@@ -270,8 +274,8 @@ __device__ __forceinline__ void rotate(const Pairs<VEC> &p, const float (&c)[8],
     }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void rotate_exact(const Pairs<VEC> &p, const Turn64 &tu, float (&x0)[8], float (&x1)[8])
+template <int D, bool VEC>
+__device__ __forceinline__ void rotate_exact(const Pairs<D, VEC> &p, const Turn64 &tu, float (&x0)[8], float (&x1)[8])
 {
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
@@ -282,8 +286,8 @@ __device__ __forceinline__ void rotate_exact(const Pairs<VEC> &p, const Turn64 &
     }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store_bf16(uint16_t *dst, const Pairs<VEC> &p, const float (&y0)[8], const float (&y1)[8])
+template <int D, bool VEC>
+__device__ __forceinline__ void store_bf16(uint16_t *dst, const Pairs<D, VEC> &p, const float (&y0)[8], const float (&y1)[8])
 {
     if constexpr (!VEC) {
 #pragma unroll
@@ -308,8 +312,8 @@ __device__ __forceinline__ void store_bf16(uint16_t *dst, const Pairs<VEC> &p, c
     }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t *dst, const Pairs<VEC> &p, const float (&y0)[8], const float (&y1)[8],
+template <int D, bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t *dst, const Pairs<D, VEC> &p, const float (&y0)[8], const float (&y1)[8],
                                             int e)
 {
     const float m = exp2_int(-e);
@@ -361,7 +365,7 @@ __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const
     const uint8_t live = valid != nullptr ? valid[r] : 1;
     const int t = pos[r];
     if (!live) return;                                // nothing of a padding row is read
-    const Pairs<VEC> p(rope, j);
+    const Pairs<D, VEC> p(rope, j);
     const Raw raw = load_raw<D, VEC>(in, p, r, h);
     bool bad = t < 0 || t >= cv.cap;
     int page = 0;
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(256) void k_append_rows(QkvRows in, int rows, const
     }
     Turn64 tu;
     const bool key = h >= nq && h < nq + nkv;
-    if (h < nq + nkv) tu.init(rope, p.first, t);
+    if (h < nq + nkv) tu.init(rope, p, t);
     float x0[8], x1[8];
     to_pairs(raw, p, x0, x1);
     if (h < nq || (key && !E4)) {
@@ -446,9 +450,9 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
         page = page_of(cv, slot, t0);
         bad = page < 0;
     }
-    const Pairs<VEC> p(rope, j);
+    const Pairs<D, VEC> p(rope, j);
     Turn64 tu;
-    tu.init(rope, p.first, t);
+    tu.init(rope, p, t);
     float c[8], s[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
