@@ -1569,13 +1569,16 @@ hipError_t launch_append_seqs(const QkvRows &in, SeqTable &seq, int nq, int nkv,
 // launch that merges (four slots of 128 tokens: 6.8 us a call, 10.2 with
 // two).  Else the smallest chunk from 128 tokens up to 1024 for which rows of
 // max_len have at most 2048 workgroups (162 rows of 512 to 4096 tokens: 154 us
-// at 1024, 156 at 512, 157 at 2048; 32 rows of 1K to 32K: 132, 139, 142); more
-// where a row would have over 512 splits to merge.
+// at 1024, 156 at 512, 157 at 2048; 32 rows of 1K to 32K: 132, 139, 142), or 4096
+// for max_len up to 2048, where few splits divide the work badly (108 rows up to
+// 1282 tokens: 22 us, 32 with 2048; 150 rows up to 700: 19, 26; 200 rows up to 2000:
+// 58 either way); more where a row would have over 512 splits to merge.
 int attn8_chunk(int rows, int nkv, int max_len)
 {
     if (max_len <= 512) return 512;
     long long chunk = 128;
-    while (chunk < 1024 && (long long)rows * nkv * ((max_len + chunk - 1) / chunk) > 2048) chunk *= 2;
+    const int most = max_len <= 2048 ? 4096 : 2048;
+    while (chunk < 1024 && (long long)rows * nkv * ((max_len + chunk - 1) / chunk) > most) chunk *= 2;
     while ((max_len + chunk - 1) / chunk > 512) chunk *= 2;
     return (int)std::min<long long>(chunk, 1 << 30);
 }
