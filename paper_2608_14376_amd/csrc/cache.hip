@@ -950,27 +950,33 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // takes NW units of one kv head in [query block][head] order, latest first, one
 // to a wavefront, on shared key and value tiles.  A tile's codes are read into
 // registers one tile ahead, and become 16-bit LDS rows once for all its
-// wavefronts: keys in bf16 with their scale (exact), values in fp16 under a
-// common exponent `top`, the largest scale of the values so far: exact down to
-// 2^-21 of it.  fp16 weights keep 11 bits where bf16 would keep 8.
+// wavefronts: keys in bf16 with their scale (exact), values in fp16 under the
+// largest scale of the tile (exact), which goes to the weights: these are fp16 of
+// weight times scale, so that what they lose is small beside the largest such
+// product, wherever the large scores and the large values stand; and they keep
+// 11 bits where bf16 would keep 8.
 //  * S^T = K Q^T on v_mfma_f32_32x32x16_bf16, two 32 x 32 tiles, key rows
 //    permuted (pf_key_of_row) so that lane l ends with eight consecutive keys
 //    16 s + 8 (l / 32) .. + 7 of each step s of query l % 32: the P^T operand of
 //  * O^T += V^T P^T on v_mfma_f32_32x32x16_f16, V^T by transposed LDS reads.
-// Weights are 2^(s - ref + P_UP), where ref follows the running maximum once that
-// is more than P_LAG above it (at most 2^15, and what is 2^-22 of the largest is
-// still a normal number), and values code 2^(e - top + V_UP); the row sum (fp32,
-// of the weights before they are rounded) carries 2^P_UP too, and the output
-// takes 2^(top - V_UP) back.
+// Weights are 2^(s + b - ref + P_UP), b the tile's scale byte, where ref follows the
+// running maximum of s + b once that is more than P_LAG above it: at most 2^15;
+// what is 2^-22 of the largest is still a normal number, what is 2^-33 of it
+// becomes zero.  The row sum (fp32, of the weights before they are rounded) takes
+// the scale out again, and the output is their quotient.  Where the groups of 16
+// tokens of a tile have scales more than 2^B_NEAR apart, each group's scale goes
+// to its own weights (`far`).  Bytes are within B_LOW .. B_HIGH (2^-60 .. 2^30; lower
+// ones count as B_LOW, with their codes scaled down instead), so that no weight that
+// the sum needs falls out of fp32.
 //
 // A wavefront's load takes rows of one 16-token group of a tile, so its page and
 // row base are scalars and the loop has no vector address arithmetic.  Future keys
 // and those past the sequence are masked by selection, value codes past it are
 // cleared.  A NaN among the values would reach queries that do not see it
-// (0 NaN), values too small for the exponent, be it a later token's, would lose
-// bits, and a page that is none is read as page 0: a wavefront whose sums hold a
-// NaN, or whose keys reach such a group, does its rows again one by one
-// (attend_row); a split notes a NaN maximum for such a row and the join does it.
+// (0 NaN), scales outside that range would lose weights or codes, and a page that
+// is none is read as page 0: a wavefront whose sums hold a NaN, or whose keys reach
+// such a group, does its rows again one by one (attend_row); a split notes a NaN
+// maximum for such a row and the join does it.
 //
 // Bound by the matrix units and the softmax's arithmetic of one wavefront in turn:
 // a tile's 32 products are 1024 cycles of each SIMD's matrix unit, and with two
@@ -984,7 +990,8 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-constexpr int P_UP = 8, P_LAG = 7, V_UP = 6;
+constexpr int P_UP = 8, P_LAG = 7;
+constexpr int B_LOW = 67, B_HIGH = 157, B_NEAR = 4;
 constexpr int MOST_SPLITS = 64;
 
 // Tiles of each of ns splits of Lk keys.
@@ -1070,13 +1077,16 @@ __device__ __forceinline__ void attend_row(const uint16_t *q, int n, int kvh, in
 template <int KCH>
 __device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
 
+// 256 + b of a byte b, by its bits: a scalar stays one
+__device__ __forceinline__ float byte_256(int b) { return __uint_as_float(0x43800000u | (uint32_t)b << 15); }
+
 // Floats that a split leaves of a unit: its rows' results, [D / 4][32 rows][4],
 // then their maxima (log2) and sums, [32][2].
 template <int D>
 constexpr int PART = 32 * D + 64;
 
 template <int D, bool PAGED, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq,
+__global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void k_attn8_prefill(const uint16_t *__restrict__ q, long long ldq, SeqTable seq,
                                                               SplitTable sp, int G, int nkv, CacheView cv, CacheLayer cl,
                                                               uint16_t *__restrict__ out, long long ldo,
                                                               float *__restrict__ ws)
@@ -1137,7 +1147,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
         l_in += t % ps;
     }
     // Rows from here on are done again: the first group that this wavefront found
-    // on a page that is none, or whose values are too small for the exponent.
+    // on a page that is none, or whose scale no row can hold beside the others.
     int redo_from = INT32_MAX;
     auto fetch_pages = [&]() {
         if constexpr (PAGED) {
@@ -1158,7 +1168,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
         }
     };
     uint4 kraw[R], vraw[R];
-    uint32_t kb[R] = {}, vb = 0;                      // scale bytes: of the wavefront's groups' keys, of group lane & 3's values
+    // scale bytes: of the wavefront's groups' keys, of group lane & 3's values (past
+    // the sequence: of a group before)
+    uint32_t kb[R] = {}, vb = 0;
     auto load = [&]() {
         size_t vblk;
 #pragma unroll
@@ -1196,12 +1208,21 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
         if (t + 16 * (lane & 3) < Lk) vb = cl.vs[vblk];
         t += BKT;
     };
-    // The loaded tile, from key k0, to LDS buffer b; `top` becomes the common
-    // exponent byte of its values.
-    auto store = [&](int k0, int b, int &top) {
+    // The loaded tile, from key k0, to LDS buffer b; sc: the scales of its values.
+    struct Scales {
+        int top, g[4];                                // bytes; top is at least B_LOW
+        bool far;
+    };
+    auto store = [&](int k0, int b, Scales &sc) {
         const int v0 = __builtin_amdgcn_readlane(vb, 0), v1 = __builtin_amdgcn_readlane(vb, 1);
         const int v2 = __builtin_amdgcn_readlane(vb, 2), v3 = __builtin_amdgcn_readlane(vb, 3);
-        top = max(top, max(max(v0, v1), max(v2, v3)));
+        sc.top = max(max(max(v0, v1), max(v2, v3)), B_LOW);
+        sc.g[0] = v0;
+        sc.g[1] = v1;
+        sc.g[2] = v2;
+        sc.g[3] = v3;
+        sc.far = __ballot(max((int)vb, B_LOW) + B_NEAR < sc.top) != 0ull;
+        if (sc.top > B_HIGH) redo_from = min(redo_from, k0);
         uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
         uint4 lo, hi;
 #pragma unroll
@@ -1216,10 +1237,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
                 w = (uint4){w.x & use, w.y & use, w.z & use, w.w & use};
             }
             const int grp16 = sub + ROWS / 16 * r;
-            const int up = (grp16 == 0 ? v0 : grp16 == 1 ? v1 : grp16 == 2 ? v2 : v3) - top, e = max(up + V_UP, -60);
+            const int byte = grp16 == 0 ? v0 : grp16 == 1 ? v1 : grp16 == 2 ? v2 : v3;
+            const int up = max(byte - (sc.far ? max(byte, B_LOW) : sc.top), -60);
             // 2^-9 times this is below 2^-24: codes lose bits (codes of zero excepted)
-            if (up < -21 && __ballot(((w.x | w.y | w.z | w.w) & 0x7f7f7f7fu) != 0u)) redo_from = min(redo_from, k0 + 16 * grp16);
-            codes_16<true>(w, exp2_int(e), lo, hi);
+            if (up < -15 && __ballot(((w.x | w.y | w.z | w.w) & 0x7f7f7f7fu) != 0u)) redo_from = min(redo_from, k0 + 16 * grp16);
+            codes_16<true>(w, exp2_int(up), lo, hi);
             V[rw * KCH + ((2 * c) ^ val16_swz<KCH>(rw))] = lo;
             V[rw * KCH + ((2 * c + 1) ^ val16_swz<KCH>(rw))] = hi;
         }
@@ -1239,7 +1261,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
     float mrow = -INFINITY, lpart = 0.f;              // reference and sum of the lane's own keys
-    bool shrunk = false;
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);   // log2(e) / sqrt(d)
     const int qq = p0 + q0 + r32;
     // operand addresses in a tile: key unit 2 s + h of the row that this lane's
@@ -1247,20 +1268,20 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
 
     if (tid == 0) redo = INT32_MAX;
-    int top_next = 0;
+    Scales next;
     fetch_pages();
     load();
     fetch_pages();
-    store(BKT * tile0, tile0 & 1, top_next);
-    int top_acc = top_next;
+    if (BKT * tile0 + 16 * (lane & 3) >= Lk) vb = __builtin_amdgcn_readlane(vb, 0);
+    store(BKT * tile0, tile0 & 1, next);
     load();
     fetch_pages();
     for (int i = tile0; i < ntiles; ++i) {
         const int k0 = i * BKT, b = i & 1;
         __syncthreads();                              // tile i is in LDS, and tile i - 1's buffers are free
-        const int top = top_next;
+        const Scales sc = next;
         if (i + 1 < ntiles) {
-            store(k0 + BKT, b ^ 1, top_next);
+            store(k0 + BKT, b ^ 1, next);
             load();                                   // past the last tile: groups past the sequence, or a tile not stored
             fetch_pages();
         }
@@ -1294,8 +1315,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
             __builtin_amdgcn_sched_barrier(0);
         }
         // lane: keys k0 + 32 kt + 16 (j / 8) + 8 h + j % 8 of query qq
-        float mt = -INFINITY;
-        if (k0 + BKT - 1 > p0 + q0 || k0 + BKT > Lk) {
+        // the reference stays where the maximum is at most 2^P_LAG above it, so
+        // most tiles rescale nothing
+        auto reference = [&]() {
+            float mt = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
+            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+            mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1]));   // both halves of the query's keys
+            mt = __builtin_fmaf(mt, scale2, byte_256(sc.top));
+            return mt > mrow + P_LAG ? mt : mrow;
+        };
+        // what is added to scores in base 2 for a weight's exponent
+        auto offset = [&](float ref) { return byte_256(sc.top) - ((ref == -INFINITY ? 0.f : ref) - P_UP); };
+        float far = 0.f;
+        if (k0 + BKT - 1 > p0 + q0 || k0 + BKT > Lk || sc.far) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -1303,19 +1339,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
                     const int key = k0 + 32 * kt + 16 * (j >> 3) + 8 * h + (j & 7);
                     st[kt][j] = (key <= qq && key < Lk) ? st[kt][j] : -INFINITY;
                 }
-        }
+            if (sc.far) {                             // each group's scale: on its scores, and out of its sum
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+                for (int f = 0; f < 4; ++f)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
-        {
-            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-            mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * scale2;   // both halves of the query's keys
+                    for (int j = 0; j < 8; ++j) st[f >> 1][8 * (f & 1) + j] += (float)(max(sc.g[f], B_LOW) - sc.top) * (1.0f / scale2);
+                const float at = offset(reference());
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    float part = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        part += __builtin_amdgcn_exp2f(__builtin_fmaf(st[f >> 1][8 * (f & 1) + j], scale2, at));
+                    far += part * exp2_int(min(sc.top - max(sc.g[f], B_LOW), B_HIGH - B_LOW));
+                }
+            }
         }
-        // the reference stays where the maximum is at most 2^P_LAG above it, so
-        // most tiles rescale nothing
-        const float mnew = mt > mrow + P_LAG ? mt : mrow;
-        const float moff = (mnew == -INFINITY ? 0.f : mnew) - P_UP;
+        const float mnew = reference(), at = offset(mnew);
         f16x8 pf[4];
         float ls = 0.f;
 #pragma unroll
@@ -1326,32 +1366,22 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     typedef float f32x2_t __attribute__((ext_vector_type(2)));
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e], scale2, -moff));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e + 1], scale2, -moff));
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e], scale2, at));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kt][8 * half + 2 * e + 1], scale2, at));
                     ls += x + y;
                     w[e] = __builtin_convertvector((f32x2_t){x, y}, f16x2);
                 }
                 pf[2 * kt + half] = __builtin_bit_cast(f16x8, w);
             }
-        if (__ballot(mnew != mrow) || top != top_acc) {
+        if (__ballot(mnew != mrow)) {
             const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
-            const float a = alpha * exp2_int(max(top_acc - top, -126));
             lpart *= alpha;
-            if (top - top_acc > 100) {                // the sums may lose bits: shrunk unless they are zero
-                float any = 0.f;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) any = fmaxf(any, fabsf(acc[dt][j]));
-                shrunk |= any > 0.f;
-            }
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[dt][j] *= a;
-            top_acc = top;
+                for (int j = 0; j < 16; ++j) acc[dt][j] *= alpha;
         }
-        lpart += ls;
+        lpart = __builtin_fmaf(sc.far ? far : ls, exp2_int(127 - sc.top), lpart);
         mrow = mnew;
         // operand f: 16-key step f / DT, output tile f % DT; lane l takes
         // dimension 32 dt + l % 32 of keys 16 s + 8 h .. + 7 by two transposed reads
@@ -1381,9 +1411,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     __syncthreads();                                  // every wavefront is done with the tiles
 
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]
-    bool nan = shrunk;
     const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
     const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]), inv = 1.0f / sum;
+    bool nan = false;
     if (ns > 1) {
         if (!active || my_last_q < BKT * tile0) return;   // no row of the unit sees the split's tiles
         const size_t all = (size_t)(units / G) * G * nkv, unit = (size_t)kvh * units + u;
@@ -1393,10 +1423,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
                 float4 v;
-                v.x = __builtin_amdgcn_ldexpf(acc[dt][j] * inv, top_acc - 127 - V_UP);
-                v.y = __builtin_amdgcn_ldexpf(acc[dt][j + 1] * inv, top_acc - 127 - V_UP);
-                v.z = __builtin_amdgcn_ldexpf(acc[dt][j + 2] * inv, top_acc - 127 - V_UP);
-                v.w = __builtin_amdgcn_ldexpf(acc[dt][j + 3] * inv, top_acc - 127 - V_UP);
+                v.x = acc[dt][j] * inv;
+                v.y = acc[dt][j + 1] * inv;
+                v.z = acc[dt][j + 2] * inv;
+                v.w = acc[dt][j + 3] * inv;
                 nan |= v.x != v.x || v.y != v.y || v.z != v.z || v.w != v.w;
                 *(float4 *)(part + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = v;
             }
@@ -1413,8 +1443,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
             for (int j = 0; j < 16; ++j) {
                 const float v = acc[dt][j] * inv;
                 nan |= v != v;
-                ost[r32 * OPITCH + 32 * dt + 8 * (j >> 2) + 4 * h + (j & 3)] =
-                    f2bf(__builtin_amdgcn_ldexpf(v, top_acc - 127 - V_UP));
+                ost[r32 * OPITCH + 32 * dt + 8 * (j >> 2) + 4 * h + (j & 3)] = f2bf(v);
             }
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0): this wavefront's staging writes are done
@@ -1433,7 +1462,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn8_prefill(const uint16_t *__
     }
 }
 
-// The splits of a unit's rows, weighed by their maxima and sums in order.
+// The splits of a unit's rows, weighed by their maxima and sums in order: by sum
+// 2^maximum, where the sums' own exponents count (they carry their values' scales).
 // Workgroup: one unit (x), D / 4 slices of 8 dimension fours (y); thread (four,
 // row).  A row counts the splits that it sees; rows with a NaN maximum are done
 // again by the first slice.
@@ -1462,10 +1492,11 @@ __global__ __launch_bounds__(256) void k_attn8_join(const float *__restrict__ ws
         bool bad = false;
         for (int s = 0; s < seen; ++s) {
             bad |= w[s][r] != w[s][r];
-            M = fmaxf(M, w[s][r]);
+            M = fmaxf(M, w[s][r] + (float)__builtin_amdgcn_frexp_expf(l[s][r]));
         }
         for (int s = 0; s < seen; ++s) {
-            const float x = l[s][r] * __builtin_amdgcn_exp2f(w[s][r] - M);
+            const float sum = l[s][r], up = w[s][r] - M + (float)__builtin_amdgcn_frexp_expf(sum);
+            const float x = __builtin_amdgcn_frexp_mantf(sum) * __builtin_amdgcn_exp2f(up);
             w[s][r] = x;
             L += x;
         }
