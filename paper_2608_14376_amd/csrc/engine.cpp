@@ -540,7 +540,7 @@ static corun_status check_epilogue(const corun_model_cfg *c, const corun_kv *kv,
     const long long cap = kv->layout == CORUN_KV_PAGED ? (long long)kv->max_pages_per_seq * kv->page_size : kv->max_seq_len;
     if (cap > (1 << 30)) return fail(CORUN_E_CAPACITY, "an e4m3 cache or this rope: at most 2^30 tokens to a slot");
     if (kv->layout == CORUN_KV_PAGED && kv->page_size > (1 << 20)) return fail(CORUN_E_SHAPE, "page_size above 2^20");
-    if (kv->dtype == CORUN_KV_E4M3 && o.attn_chunk > 0 && cap / o.attn_chunk >= 2048)   // the merge's LDS
+    if (kv->dtype == CORUN_KV_E4M3 && o.attn_chunk > 0 && (cap + o.attn_chunk - 1) / o.attn_chunk >= 2048)   // the merge's LDS
         return fail(CORUN_E_INVAL, "attn_chunk %d makes 2048 or more splits of %lld tokens", o.attn_chunk, cap);
     return CORUN_OK;
 }

@@ -220,3 +220,14 @@ def test_engine_chunks_that_make_too_many_splits():
         assert n > 0 if ok else n == corun.E_INVAL
     kv, opt = _kv(max_seq_len=2048 * 64, dtype=corun.KV_BF16), corun.options(attn_chunk=64)
     assert corun.load().corun_describe_plan(C.byref(cfg), C.byref(kv), 2, C.byref(opt), C.addressof(out), 64) > 0
+
+
+def test_engine_chunks_count_a_capacity_s_last_split():
+    """A capacity that is no multiple of the chunk has a further, shorter split."""
+    cfg = corun.model_cfg(dict(n_layers=1, hidden=256, n_heads=4, n_kv_heads=2, head_dim=64, ffn=688, vocab=1024, n_experts=0,
+                               top_k=0, expert_ffn=0, rms_eps=1e-6, rope_theta=10000.0))
+    out, opt = (C.c_int32 * 64)(), corun.options(attn_chunk=64)
+    for cap, ok in ((2047 * 64, True), (2047 * 64 + 16, False), (2046 * 64 + 16, True)):
+        for kv in (_kv(max_seq_len=cap, blk=16), _kv(layout=corun.KV_PAGED, page_size=16, mpp=cap // 16, blk=16)):
+            n = corun.load().corun_describe_plan(C.byref(cfg), C.byref(kv), 2, C.byref(opt), C.addressof(out), 64)
+            assert n > 0 if ok else n == corun.E_INVAL, (cap, n)
