@@ -1461,7 +1461,7 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
 
     const int H = cfg->hidden, d = cfg->head_dim, nq = cfg->n_heads, nkv = cfg->n_kv_heads, F = cfg->ffn;
     const int cap = kv_capacity(kv);
-    const int rope_len = std::max(cap, o.max_prefill_len);
+    const int rope_len = own_epi ? 0 : std::max(cap, o.max_prefill_len);   // launch_append_* make their own cosines
     e->hist_cap = 4096;
     Carver cv;
     const StepInputs in(B);
@@ -1499,7 +1499,7 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
     cv.take(&e->q, (size_t)B * nq * d);
     cv.take(&e->o, (size_t)p.Mp * nq * d);
     cv.take(&e->a, (size_t)p.Mp * F);
-    size_t total = cv.take(&e->rope, (size_t)rope_len * (d / 2));
+    size_t total = cv.take(&e->rope, std::max((size_t)rope_len * (d / 2), (size_t)1));
     e->ws_bytes = total;
     if (hipGetDevice(&e->device) != hipSuccess || hipMalloc(&e->ws, total) != hipSuccess) return bail(fail(CORUN_E_HIP, "workspace allocation of %zu bytes", total));
     rebase(e->d_in, e->ws);
@@ -1530,8 +1530,9 @@ extern "C" corun_status corun_engine_create(const corun_model_cfg *cfg, const co
     const size_t rope_off = (size_t)((char *)e->rope - e->ws);
     if (launch_fill_u32((uint32_t *)e->ws, (long long)(rope_off / 4), fillv, e->st) != hipSuccess ||
         launch_fill_u32((uint32_t *)e->d_counter, 1, (uint32_t)e->hist_cap, e->st) != hipSuccess ||
-        (o.rope ? launch_rope_table_of(e->rope, rope_len, d, rope.freq, e->st)
-                : launch_rope_table(e->rope, rope_len, d, (double)cfg->rope_theta, e->st)) != hipSuccess ||
+        (rope_len == 0 ? hipSuccess
+         : o.rope      ? launch_rope_table_of(e->rope, rope_len, d, rope.freq, e->st)
+                       : launch_rope_table(e->rope, rope_len, d, (double)cfg->rope_theta, e->st)) != hipSuccess ||
         launch_iota(e->d_order, B, e->st) != hipSuccess)   // a valid row order before the first upload
         return bail(fail(CORUN_E_HIP, "workspace initialisation failed"));
 

@@ -164,3 +164,24 @@ def test_moe_against_the_reference(name, blk, page, chunk):
         close(out[slot], follow_moe(s, [int(toks[slot])], len(seq), slot, [slot], 0))
         seq.append(int(toks[slot]))
         toks[slot], toks[4], lens[4] = got[slot], got[4], lens[4] + 1
+
+
+@pytest.mark.parametrize("e4m3", [True, False])
+def test_no_rotary_table_where_no_kernel_reads_one(e4m3):
+    """2^22 positions to a slot: a table of them would be 2 GiB at 64 pairs of 8 bytes."""
+    cfg = wl.config("small128")
+    W = base.to_device(wl.make_weights(cfg, seed=51))
+    cap, dt = 1 << 22, torch.uint8 if e4m3 else torch.bfloat16
+    k, v = ([torch.zeros((4, 2, 16, 128), dtype=dt, device=DEV) for _ in range(cfg["n_layers"])] for _ in range(2))
+    kw = {}
+    if e4m3:
+        ks, vs = ([torch.full((4, 2, 1), 121, dtype=torch.uint8, device=DEV) for _ in range(cfg["n_layers"])] for _ in range(2))
+        kw = dict(k_scale=ks, v_scale=vs, scale_block=16)
+    table = torch.zeros((1, cap // 16), dtype=torch.int32, device=DEV)
+    rope = None if e4m3 else corun.rope(128, layout=corun.ROPE_INTERLEAVED)
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    eng = corun.Engine(cfg, W, 1, k, v, layout=corun.KV_PAGED, page_size=16, page_table=table,
+                       opt=corun.options(rope=rope), **kw)
+    assert before - torch.cuda.mem_get_info()[0] < 1 << 30
+    eng.close()
