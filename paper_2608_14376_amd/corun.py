@@ -367,7 +367,7 @@ def _rows(cache, t, name):
             (n == 3 and shape[1] > 1 and stride[1] != shape[2]):
         raise ValueError(f"{name}: bf16 rows of heads on {cache.device}, the elements of a row contiguous")
     width = shape[1] if n == 2 else shape[1] * shape[2]
-    return shape[0], width, (stride[0] if shape[0] > 1 else max(width, stride[0]))
+    return shape[0], width, (stride[0] if shape[0] > 1 else width)   # one row's stride leads nowhere
 
 
 def _heads(cache, width, name):

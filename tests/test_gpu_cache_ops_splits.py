@@ -134,3 +134,25 @@ def test_append_at_the_farthest_positions(e4m3):
             assert want.abs().max() <= 448 * 2.0**e * (1 + 1e-5) and want.abs().max() > 224 * 2.0**e * (1 - 1e-5)
             assert ((val - want).abs() <= torch.maximum(ref.U_E4M3 * want.abs(), torch.tensor(2.0**(e - 10), dtype=torch.float64))
                     + 2.0**-21 * size[r, nq:] * (1 - h)).all()
+
+
+def test_one_row_whose_stride_is_no_multiple_of_8():
+    """The distance to a row that is not there: a single row cut out of a wider buffer."""
+    lay = Layer(cap=CAP, rows=1)
+    heads = lay.nq + 2 * lay.nkv
+    x = rows_of(1, heads, 128, 41)[1].contiguous()
+    cut = lambda t: torch.cat([t, torch.zeros_like(t[:, :4])], 1).repeat(2, 1)[:1, : t.shape[1]]
+    pos, live = torch.tensor([700], dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.uint8, device=DEV)
+    lay.step(x, pos, pos + 1, live)
+    q, out, xc = cut(lay.q[:1]), cut(lay.out[:1]), cut(x)
+    assert xc.stride(0) % 8 == 4
+    q.zero_(), out.zero_()
+    corun.decode_append(lay.cache, 0, xc, pos, lay.rope, q, valid=live)
+    corun.decode_attention(lay.cache, 0, q, pos + 1, out, lay.ws, valid=live)
+    assert same(q, lay.q[:1]) and same(out, lay.out[:1])
+    out.zero_()
+    corun.prefill_attention(lay.cache, 0, q, [1], [700], [0], out)
+    want = torch.zeros_like(lay.out[:1])
+    corun.prefill_attention(lay.cache, 0, lay.q[:1], [1], [700], [0], want)
+    torch.cuda.synchronize()
+    assert same(out, want)
