@@ -210,7 +210,9 @@ typedef struct {
                                   f_i = rope_theta^(-2 i / head_dim).  Its head_dim is the model's.  With
                                   interleaved pairs, a part of the head or a magnitude, and with an e4m3 cache,
                                   the QKV epilogue is a kernel of its own (corun_decode_append's), in decode and in
-                                  prefill: CORUN_E_INVAL with qkv_epilogue = 2 or small_batch_layer = 1. */
+                                  prefill: CORUN_E_INVAL with qkv_epilogue = 2 or small_batch_layer = 1.  Up to
+                                  B_fixed = 8, where the others are part of attention or of the small-batch layer,
+                                  that costs 3 to 9% of a step on a bf16 cache. */
 } corun_options;
 
 /* Create an engine for one fixed padded batch size B_fixed (Sec. IV,
@@ -389,8 +391,12 @@ int64_t corun_decode_attention_workspace(const corun_kv *kv, int32_t n_heads, in
  * rows of q and out as for corun_prefill_append; the query at position
  * starts[i] + t sees tokens 0 .. starts[i] + t of slot slots[i], which earlier
  * calls have appended.  A query that sees a page outside [0, num_pages) gets
-NaN.  A sequence's results do not depend on the others of the call.  rows
- * n_heads at most 2^30.
+ * NaN.  A sequence's results do not depend on the others of the call.  rows
+ * n_heads at most 2^30.  Weights enter the products as fp16 together with their
+ * values' scales: one whose product with its scale is below 2^-29 of the row's
+ * largest counts for the softmax's sum alone.  Rows that see a NaN value, a scale
+ * byte of values above 157, or one below 56 with codes that are not zero are
+ * computed one by one, some hundred times slower.
  *  ws         workspace as for corun_decode_attention: ws_bytes at least what
  *             corun_prefill_attention_workspace returns for the same sequences,
  *             which is 0 (ws may be NULL) unless a sequence of few rows starts
@@ -562,10 +568,11 @@ enum {
  * launches.  The launches run on the inputs of the last decode step (tokens,
  * valid mask, positions as validated by the call that ran it, uploaded again
  * first: the step itself advanced the positions), so a kernel that appends
- * to the cache rewrites the value that step wrote at that position.  Re-running a kernel rewrites the workspace
- * values it wrote in the step (the residual-folding RMSNorm adds its
- * partials again; the next step recomputes the residual from the
- * embedding).  CORUN_E_STATE before the engine's first decode step. */
+ * to the cache rewrites the value that step wrote at that position (in an e4m3
+ * cache that drops what a later prefill call put behind it in its block).
+ * Re-running a kernel rewrites the workspace values it wrote in the step
+ * (the residual-folding RMSNorm adds its partials again; the next step
+ * recomputes the residual from the embedding).  CORUN_E_STATE before the engine's first decode step. */
 corun_status corun_time_kernel(corun_engine *e, int32_t kernel, int32_t layer, int32_t n_iters, float *avg_us);
 
 /* Measurement aid: n_steps decode steps, each on the inputs of the last

@@ -310,7 +310,9 @@ class KvCache:
     (device int32 [n_slots, max_pages_per_seq]), [num_pages, n_kv_heads,
     page_size, head_dim]; bf16, or e4m3 codes (float8_e4m3fn or uint8) with
     scale bytes (float8_e8m0fnu or uint8) k_scale and v_scale [.., n_kv_heads,
-    tokens / scale_block].  The tensors are borrowed and kept alive."""
+    tokens / scale_block].  The appends take either; the attention operators
+    read e4m3 caches, bf16 ones are an engine's to attend to.  The tensors are
+    borrowed and kept alive."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None, scale_block=0, page_table=None):
         import torch

@@ -579,8 +579,9 @@ __global__ __launch_bounds__(512) void k_append_seqs(QkvRows in, SeqTable seq, i
 // selection, value codes are cleared.
 //
 // Bound by reading the cache: 162 rows of 512 to 4096 tokens (8 kv heads of 128)
-// take 147 us, 5.2 TB/s, which is what a large copy reaches; 32 paged rows of 1024
-// to 32768 tokens 127 us, 4.7 TB/s, where the longest row's last splits run alone.
+// take 147 us, 5.2 TB/s, which is what a large copy reaches, though reads alone can
+// be faster (the bf16 kernel takes these rows at 5.8); 32 paged rows of 1024 to
+// 32768 tokens 127 us, 4.7 TB/s, where the longest row's last splits run alone.
 // Three workgroups of 33 KB to a CU keep enough loads in flight; the weights' bf16
 // halves hi + lo cost matrix instructions that the loads leave idle, where one bf16
 // weight would lose 8 bits.
@@ -981,8 +982,8 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // Bound by the matrix units and the softmax's arithmetic of one wavefront in turn:
 // a tile's 32 products are 1024 cycles of each SIMD's matrix unit, and with two
 // wavefronts to a SIMD a tile takes 1.9 us, about 4500 cycles for 2048 of products.
-// 2048 rows of 32 heads behind 14336 tokens: 525 to 560 us, 0.93 to 0.99 PFLOP/s
-// (a large bf16 matrix product reaches 1.25).  Products of the next tile between
+// 2048 rows of 32 heads behind 14336 tokens: 544 to 554 us, 0.93 to 0.95 PFLOP/s
+// (a large bf16 matrix product reaches 1.25); 615 where every tile is `far`.  Products of the next tile between
 // the steps of this tile's softmax (588 us) and halves of the wavefronts half a
 // tile apart (5% longer) came out slower: two wavefronts already fill each
 // other's gaps, and no reads of keys or values (2% each) or exponentials (5%)
@@ -1022,7 +1023,9 @@ __device__ __forceinline__ void codes_16(uint4 w, float scale, uint4 &lo, uint4 
 
 // One query row over its first n keys, by one wavefront in fp32: 64 keys at a
 // time, a key to a lane for the scores, then D / 64 dimensions to a lane.  For
-// rows that see a NaN or a page that is none (the whole row becomes NaN).
+// rows that see a NaN, a scale out of the other pass's range or a page that is none
+// (the whole row becomes NaN).  Slow: 6000 tokens of 32 heads whose first value
+// holds a NaN take 97 ms (0.33 without it), 600 take 4.3.
 template <int D>
 __device__ __forceinline__ void attend_row(const uint16_t *q, int n, int kvh, int nkv, int slot, const CacheView &cv,
                                         const CacheLayer &cl, uint16_t *out)
@@ -1657,8 +1660,8 @@ hipError_t launch_attn8_merge(const float *ws, int rows, const uint8_t *valid, c
 // results stay the same beside others: where its workgroups of four would fill at
 // most half of the chip's room for 512, as many as fill it, of at least eight
 // tiles each (starting a split and joining it cost about four), or 32 where more
-// than a quarter is filled already.  Heads of 8 over 32, at 8192 tokens: 1 row
-// 32 us, 231 unsplit; 256 rows 59, 234; 512 rows 93, 244.
+// than a quarter is filled already.  Heads of 8 over 32, behind 8192 tokens: 1 row
+// 30 us, 204 unsplit; 256 rows 56, 210; 512 rows 88, 218; 1024 rows 160, 231.
 static int attn8_seq_splits(int rows, int start, int nq, int nkv)
 {
     const int G = nq / nkv, tiles = (int)(((long long)start + rows + 63) / 64);
@@ -1727,10 +1730,10 @@ hipError_t launch_attn8_seqs(const uint16_t *q, long long ldq, const SeqTable &g
     // Eight wavefronts share a tile's conversion; four are twice the workgroups,
     // and a tile takes them 1.7 us on a CU of their own where eight need 1.9.
     // Heads of 128 take four where eight would leave half of the 256 CUs idle
-    // (1024 rows at 8192: 260 us, 280 with eight; 1536 rows: 342, 297) and where no
-    // sequence has many tiles (1000 tokens: 37 us, 40 with eight; 2000: 72, 73; 4000:
-    // 186, 155).  Heads of 64 always do (600, 2000, 6000 tokens: 18, 45, 211 us; 21,
-    // 54, 251 with eight).  A row's arithmetic is the same either way.
+    // (behind 8192 tokens 64 rows: 35 us, 38 with eight; 256 rows: 60, 56; 1536: 318,
+    // 275) and where no sequence has many tiles (600 tokens: 22 us, 26 with eight;
+    // 1000: 32, 36; 2000: 62, 67; 4000: 174, 147).  Heads of 64 have units for four
+    // wavefronts to load only.  A row's arithmetic is the same either way.
     const int NW = d == 64 || groups8 * nkv <= 128 || keys(by[0]) <= 2048 ? 4 : 8;
     int groups = 0;
     for (int i = 0; i < n; ++i) {

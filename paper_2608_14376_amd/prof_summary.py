@@ -9,6 +9,7 @@ line in the summaries it writes):
   python -m paper_2608_14376_amd.prof_summary mfma     --pmc P.csv --trace T.csv ...
   python -m paper_2608_14376_amd.prof_summary fetch    --pmc P.csv --trace T.csv ...
   python -m paper_2608_14376_amd.prof_summary prefill  --pmc P.csv --trace T.csv --call 1 --op qkv=FLOPS ...
+  python -m paper_2608_14376_amd.prof_summary launches --trace T.csv --source cache.hip --source cache.h ...
 
 Dispatch windows follow bench.py's order for the headline batch: `warmup`
 graph steps, `steps` graph steps, one more step, `profile_steps` eagerly
@@ -24,6 +25,7 @@ import collections
 import csv
 import hashlib
 import os
+import re
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -32,9 +34,9 @@ SIMDS = 1024
 XCDS = 8
 
 
-def source_sha() -> str:
+def source_sha(files=("kernels.hip", "kernels.h", "device.h")) -> str:
     h = hashlib.sha256()
-    for f in ("kernels.hip", "kernels.h", "device.h"):
+    for f in files:
         h.update(open(os.path.join(HERE, "csrc", f), "rb").read())
     return h.hexdigest()[:16]
 
@@ -130,6 +132,28 @@ def cmd_kernels(a):
                 lines.append(f"{n:44s} {len(v):8d} {sum(v):9.1f} {sum(v) / len(v):8.2f}")
     for ln in a.note or []:
         lines.append(f"# {ln}")
+    open(a.out, "w").write("\n".join(lines) + "\n")
+    print("\n".join(lines))
+
+
+def cmd_launches(a):
+    """Every kernel and launch shape of the run, in the order of their first launch."""
+    per = collections.OrderedDict()
+    for r in sorted(read(a.trace), key=lambda r: int(r["Start_Timestamp"])):
+        m = re.search(r"\bk_\w+(<[^>]*>)?", r["Kernel_Name"])
+        if not m:
+            continue
+        wg = [int(r[f"Workgroup_Size_{x}"]) for x in "XYZ"]
+        shape = " x ".join(str(int(r[f"Grid_Size_{x}"]) // w) for x, w in zip("XYZ", wg))
+        per.setdefault((m[0], shape, wg[0] * wg[1] * wg[2]), []).append(
+            (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3)
+    lines = [f"# {a.title}", f"# command: {a.command}",
+             f"# kernel_source_sha256_16: {source_sha(a.source)}", f"# (of {', '.join(a.source)})"]
+    lines += [f"# {ln}" for ln in a.note or []]
+    lines += ["", f"{'kernel':34s} {'workgroups':>18s} {'threads':>8s} {'n':>4s} {'min_us':>9s} {'median_us':>9s} {'max_us':>9s}"]
+    for (name, shape, threads), v in per.items():
+        v.sort()
+        lines.append(f"{name:34s} {shape:>18s} {threads:8d} {len(v):4d} {v[0]:9.2f} {v[len(v) // 2]:9.2f} {v[-1]:9.2f}")
     open(a.out, "w").write("\n".join(lines) + "\n")
     print("\n".join(lines))
 
@@ -332,7 +356,7 @@ def cmd_prefill(a):
 def main():
     ap = argparse.ArgumentParser()
     sub = ap.add_subparsers(dest="cmd", required=True)
-    for name in ("kernels", "traffic", "mfma", "fetch", "prefill"):
+    for name in ("kernels", "traffic", "mfma", "fetch", "prefill", "launches"):
         s = sub.add_parser(name)
         s.add_argument("--out", required=True)
         s.add_argument("--title", required=True)
@@ -354,6 +378,9 @@ def main():
             s.add_argument("--kernel", required=True)
             s.add_argument("--first", type=int, required=True)
             s.add_argument("--algorithmic", type=int, required=True)
+        elif name == "launches":
+            s.add_argument("--trace", required=True)
+            s.add_argument("--source", action="append", required=True, help="a file of csrc/ that the kernels are built from")
         elif name == "prefill":
             s.add_argument("--pmc", required=True)
             s.add_argument("--trace", required=True)
@@ -375,7 +402,7 @@ def main():
             parts = item.split("=")
             a.labels[parts[0]] = parts[1] if a.cmd == "mfma" else (parts[1], int(parts[2]))
     {"kernels": cmd_kernels, "traffic": cmd_traffic, "mfma": cmd_mfma, "fetch": cmd_fetch,
-     "prefill": cmd_prefill}[a.cmd](a)
+     "prefill": cmd_prefill, "launches": cmd_launches}[a.cmd](a)
 
 
 if __name__ == "__main__":
