@@ -975,7 +975,7 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // and those past the sequence are masked by selection, value codes past it are
 // cleared.  A NaN among the values would reach queries that do not see it
 // (0 NaN), scales outside that range would lose weights or codes, and a page that
-// is none is read as page 0: a wavefront whose sums hold a NaN, or whose keys reach
+// is none is taken for zeros: a wavefront whose sums hold a NaN, or whose keys reach
 // such a group, does its rows again one by one (attend_row); a split notes a NaN
 // maximum for such a row and the join does it.
 //
@@ -1172,7 +1172,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void k_attn8_prefill(cons
     };
     uint4 kraw[R], vraw[R];
     // scale bytes: of the wavefront's groups' keys, of group lane & 3's values (past
-    // the sequence: of a group before)
+    // the sequence or on a page that is none: of a group before)
     uint32_t kb[R] = {}, vb = 0;
     auto load = [&]() {
         size_t vblk;
@@ -1181,11 +1181,12 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void k_attn8_prefill(cons
             const int t16 = t + 16 * sub + ROWS * r;
             kraw[r] = vraw[r] = (uint4){0u, 0u, 0u, 0u};
             size_t base, kblk;
+            bool real = t16 < Lk;                     // the whole group stands in the slot
             if constexpr (PAGED) {
-                int pg = __builtin_amdgcn_readfirstlane(page[r]);
+                const int pg = __builtin_amdgcn_readfirstlane(page[r]);
                 if ((unsigned)pg >= (unsigned)cv.num_pages) {
                     redo_from = min(redo_from, t16);
-                    pg = 0;
+                    real = false;
                 }
                 const size_t head = (size_t)pg * nkv + kvh;
                 base = head * ps + in[r];
@@ -1195,20 +1196,21 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void k_attn8_prefill(cons
                 base = head0 + t16;
                 kblk = blk0 + (t16 >> bs);
             }
-            if (t16 < Lk) {                           // the whole group stands in the slot
+            if (real) {
                 kraw[r] = *(const uint4 *)((const uint8_t *)cl.k + base * D + off);
                 kb[r] = cl.ks[kblk];
                 vraw[r] = *(const uint4 *)((const uint8_t *)cl.v + base * D + off);
             }
         }
+        bool in_seq16 = t + 16 * (lane & 3) < Lk;
         if constexpr (PAGED) {
-            if ((unsigned)l_page >= (unsigned)cv.num_pages) l_page = 0;
+            in_seq16 &= (unsigned)l_page < (unsigned)cv.num_pages;
             vblk = ((size_t)l_page * nkv + kvh) * (ps >> bs) + (l_in >> bs);
             l_in += BKT;
         } else {
             vblk = blk0 + ((t + 16 * (lane & 3)) >> bs);
         }
-        if (t + 16 * (lane & 3) < Lk) vb = cl.vs[vblk];
+        if (in_seq16) vb = cl.vs[vblk];
         t += BKT;
     };
     // The loaded tile, from key k0, to LDS buffer b; sc: the scales of its values.

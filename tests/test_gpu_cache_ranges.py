@@ -118,3 +118,24 @@ def test_weights_keep_the_bits_of_fp16(d, page):
         x, q = rows_of(24, nkv * G, d, 210 + seed, loud=False)
         out = run_prefill(hc.device_cache(corun), q, [24], [0], [0])
         check(hc, x, out, [(0, 24, 0, 0)], every=1)
+
+
+@pytest.mark.parametrize("start", [0, 1024])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_lost_page_leaves_earlier_rows_alone(start, d):
+    """Rows before a page that is none, in its tile: the same bits whatever stands in the cache's first page."""
+    nkv, G, blk, page, n, cap = 1, 1, 16, 16, 64, 1152
+    hc = HostCache(nkv, d, 2, cap, blk, page, seed=95)
+    hc.table[hc.table == 0] = hc.k.shape[0] - 1       # no sequence has the first page
+    x, q = rows_of(n, nkv * G, d, 96, loud=False)
+    good = run_prefill(hc.device_cache(corun), q, [n], [start], [1])
+    hc.table[1, (start + 48) // page] = -7            # tokens 48 .. 63 of the rows' tile
+    outs = []
+    for code, byte in ((0x38, 121), (0x7F, 121), (0x7E, 140), (0x7E, 247)):
+        hc.v[0], hc.k[0], hc.vs[0] = code, code, byte
+        outs.append(run_prefill(hc.device_cache(corun), q, [n], [start], [1]))
+        assert torch.isnan(outs[-1][48:]).all() and not torch.isnan(outs[-1][:48]).any()
+        assert torch.equal(outs[-1][:48].view(torch.uint8), outs[0][:48].view(torch.uint8)), (code, byte)
+    check(hc, x, good, [(0, 40, start, 1)], every=9)
+    hc.table[1, (start + 48) // page] = 0
+    check(hc, x, outs[0], [(0, 48, start, 1)], every=9)
