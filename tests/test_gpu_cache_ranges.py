@@ -139,3 +139,16 @@ def test_a_lost_page_leaves_earlier_rows_alone(start, d):
     check(hc, x, good, [(0, 40, start, 1)], every=9)
     hc.table[1, (start + 48) // page] = 0
     check(hc, x, outs[0], [(0, 48, start, 1)], every=9)
+
+
+@pytest.mark.parametrize("d,page,start,n", [(128, 0, 0, 130), (64, 32, 0, 70), (128, 16, 1400, 40)])
+@pytest.mark.parametrize("lo,hi", [(27, 52), (50, 75), (60, 90), (150, 165), (200, 240)])
+def test_scales_at_both_ends(d, page, start, n, lo, hi):
+    """Values of about 2^-95 up to 2^118: around the least and the largest scales of the fast pass, and beyond both."""
+    nkv, G, blk, cap = 2, 2, 16, 1536
+    hc = HostCache(nkv, d, 1, cap, blk, page, seed=lo)
+    g = torch.Generator().manual_seed(hi)
+    hc.vs = torch.randint(lo, hi + 1, hc.vs.shape, generator=g).to(torch.uint8)
+    x, q = rows_of(n, nkv * G, d, 7, loud=False)
+    out = run_prefill(hc.device_cache(corun), q, [n], [start], [0])
+    check(hc, x, out, [(0, n, start, 0)], every=max(1, n // 5))
