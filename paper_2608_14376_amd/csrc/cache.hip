@@ -982,12 +982,13 @@ __global__ __launch_bounds__(256) void k_attn8_merge(const float *__restrict__ w
 // Bound by the matrix units and the softmax's arithmetic of one wavefront in turn:
 // a tile's 32 products are 1024 cycles of each SIMD's matrix unit, and with two
 // wavefronts to a SIMD a tile takes 1.9 us, about 4500 cycles for 2048 of products.
-// 2048 rows of 32 heads behind 14336 tokens: 544 to 554 us, 0.93 to 0.95 PFLOP/s
-// (a large bf16 matrix product reaches 1.25); 615 where every tile is `far`.  Products of the next tile between
-// the steps of this tile's softmax (588 us) and halves of the wavefronts half a
-// tile apart (5% longer) came out slower: two wavefronts already fill each
-// other's gaps, and no reads of keys or values (2% each) or exponentials (5%)
-// bound it alone.
+// 2048 rows of 32 heads behind 14336 tokens: 539 to 554 us, 0.93 to 0.96 PFLOP/s
+// (a large bf16 matrix product reaches 1.25); 615 where every tile is `far`.
+// Products of the next tile between the steps of this tile's softmax (588 us) and
+// halves of the wavefronts half a tile apart (5% longer) came out slower: two
+// wavefronts already fill each other's gaps, and no reads of keys or values (2%
+// each) or exponentials (5%) bound it alone.  Heads of 64 are held to the registers
+// of three wavefronts to a SIMD (6000 paged tokens: 218 us, 259 with two).
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
