@@ -409,6 +409,136 @@ corun_status corun_prefill_attention(const corun_kv *kv, int32_t layer, int32_t 
 int64_t corun_prefill_attention_workspace(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                           int32_t n, const int32_t *lens, const int32_t *starts);
 
+/* ---------------------------------------------------------------------------
+ * Operators for sequences that share a beginning (beam search, several samples
+ * of one prompt, one system prompt for a batch), without an engine: the choice of
+ * the best continuations, the pages that the chosen ones hold, and attention that
+ * reads what they share once.  They run as the operators above do: on `stream`
+ * and the current device, without waiting or allocating, capturable into a graph,
+ * on DEVICE buffers unless marked host; workspaces start on 16-byte boundaries,
+ * their contents are free between calls, and calls that may overlap need one
+ * each.  No output overlaps another buffer.  Results do not depend on the order in
+ * which workgroups run.  An engine with a paged cache decodes the chosen
+ * sequences once its page table has been rewritten (unregister a host copy of
+ * the table, or bring it up to date).
+ * ------------------------------------------------------------------------- */
+
+/* Most beams of a group, and most continuations kept of one. */
+#define CORUN_MAX_BEAMS 64
+
+/* Beam search's selection: for each of `groups` groups, the n_keep best
+ * continuations of its `beams` rows (row g beams + b) by one token.  A live row
+ * r has one candidate for every column v of its logits, of score
+ *     scores[r] + logits[r][v] - log sum_u exp(logits[r][u]),
+ * a finished row one candidate, end_token, of score scores[r].  Candidates are
+ * ordered by score times weights[r]; equal ones by row, then by larger logit,
+ * then by token.  Scores that are not finite are no candidates: a row with a
+ * NaN or +inf among its logits, or an infinite or NaN score, has none, and a
+ * logit of -inf is none.  Sums, scores and comparisons are in 64 bits, in a
+ * fixed order that does not depend on the row's place.
+ *  logits     fp32 [groups beams][ld], ld >= vocab; any 4-byte alignment
+ *  scores     fp32 [groups beams]
+ *  valid      uint8 [groups beams], or NULL: all rows are live; nothing of a
+ *             row that is not is used
+ *  finished   uint8 [groups beams], or NULL: none is
+ *  weights    fp32 [groups beams], or NULL: all 1; finite and > 0 (rows with
+ *             another weight have no candidates).  1 / length^a: a length penalty
+ *  end_token  the token that finishes a row, or -1: none does (then finished
+ *             must be NULL)
+ *  tokens, parents, out_scores  int32, int32, fp32 [groups][n_keep]: best first;
+ *             parents are row numbers.  Where a group has fewer candidates:
+ *             -1, -1, -inf
+ *  out_finished  uint8 [groups][n_keep], or NULL: whether the continuation is of
+ *             a finished row or by end_token
+ * beams and n_keep 1 .. CORUN_MAX_BEAMS, vocab 1 .. 2^19, groups beams at most
+ * 65535. */
+corun_status corun_beam_select(const float *logits, int64_t ld, int32_t vocab, int32_t groups, int32_t beams,
+                               const float *scores, const uint8_t *valid, const uint8_t *finished,
+                               const float *weights, int32_t end_token, int32_t n_keep, int32_t *tokens,
+                               int32_t *parents, float *out_scores, uint8_t *out_finished, void *ws,
+                               int64_t ws_bytes, void *stream);
+/* Bytes (>= 0), or a negative corun_status.  Host only. */
+int64_t corun_beam_select_workspace(int32_t vocab, int32_t groups, int32_t beams, int32_t n_keep);
+
+/* Pages of a paged cache, given to slots on the device: every slot r takes the
+ * first keep[r] tokens that slot src[r] holds before the call (its own with
+ * src[r] = r, none with -1), and pages for hold[r] tokens.  One call thereby
+ * reorders beams, forks a sequence, cuts one short, gives pages for the next
+ * tokens and frees those that no slot holds any more.
+ * Slot r holds the pages page_table[r][0 .. held[r] - 1]; a page may be held by
+ * several slots, and pages that none holds are free.  Whole pages of the taken
+ * tokens (keep[r] / page_size of them) are shared; a part-filled one behind them
+ * is slot r's alone, so that it can append there: the lowest slot that takes it
+ * keeps it, unless some slot shares it as a whole page, and the others get a
+ * fresh page with its tokens, copied in all n_layers layers (the tokens are
+ * rounded up to a scale block, 16 in a bf16 cache; the rest of the page stays as it
+ * was).  Then come fresh pages up to hold[r] tokens.  Fresh pages are the free ones
+ * by number, dealt to the slots in order.  A row of the table past the pages held
+ * stays as it was.
+ *  page_table kv's page_table, written
+ *  held       int32 [n_slots], read and written
+ *  src, keep  int32 [n_slots]; a slot of src -1 has held[r] = 0 afterwards, its
+ *             keep and hold are not looked at
+ *  hold       int32 [n_slots], or NULL: keep
+ *  status     int32 [1] out: 0 = done; n > 0 = n fresh pages too few; -1 = src
+ *             outside [-1, n_slots), keep outside what src holds, hold outside
+ *             [keep, capacity], held or a held page outside the table or cache.
+ *             Unless 0, nothing else is written.
+ *  ws         at least corun_pages_workspace bytes
+ * n_slots and num_pages at most 2^20, n_slots max_pages_per_seq at most 2^28. */
+corun_status corun_pages_assign(const corun_kv *kv, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                                int32_t *page_table, int32_t *held, const int32_t *src, const int32_t *keep,
+                                const int32_t *hold, int32_t *status, void *ws, int64_t ws_bytes, void *stream);
+
+/* Moves the held pages, n of them, to the numbers 0 .. n - 1: in order, the held
+ * pages from n on go to the free ones below n, in all n_layers layers, and the
+ * table names them there.  A caller can then shrink the cache, or give the upper
+ * pages to another.
+ *  held       int32 [n_slots]
+ *  status     int32 [1] out: n, or -1 (held or a held page outside the table or
+ *             cache; nothing else is written). */
+corun_status corun_pages_compact(const corun_kv *kv, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t *page_table, const int32_t *held, int32_t *status, void *ws,
+                                 int64_t ws_bytes, void *stream);
+/* Bytes (>= 0) for either call, or a negative corun_status.  Host only. */
+int64_t corun_pages_workspace(const corun_kv *kv);
+
+/* Most groups of one corun_shared_attention call. */
+#define CORUN_MAX_GROUPS 256
+
+/* Attention of a decode step whose rows share prefixes, over a bf16 or e4m3
+ * cache.  The rows are n_groups groups of group_rows[g] rows each, back to back;
+ * row r of group g sees tokens 0 .. prefix_lens[g] - 1 of slot prefix_slots[g],
+ * which are read once for the group, and tokens prefix_lens[g] .. lens[r] - 1 of
+ * slot r: out = softmax(q k / sqrt(head_dim)) v over all of them, sums in fp32.
+ * A prefix of 0 tokens leaves the attention of an ordinary decode step.
+ *  group_rows  host int32 [n_groups], each >= 1; their sum, the rows, at most
+ *              n_slots
+ *  valid       uint8 [rows], or NULL: all rows are live
+ *  lens        int32 [rows], the prefix included
+ *  prefix_slots  int32 [n_groups], or NULL: the slot of each group's first row
+ *  prefix_lens int32 [n_groups]
+ *  max_prefix  longest prefix that the launch covers, max_suffix most tokens of a
+ *              row behind its prefix; 0 = the slots' capacity.  The launch, and the
+ *              order of a row's sums, follow from the sizes given here and not
+ *              from the lengths.
+ *  ws          at least corun_shared_attention_workspace bytes for the same sizes
+ * out rows are zeros for padding rows and for rows that see nothing, NaN where
+ * prefix_lens[g] is outside [0, max_prefix], prefix_slots[g] outside [0, n_slots),
+ * lens[r] outside [prefix_lens[g], prefix_lens[g] + max_suffix] or above the
+ * capacity, or where a page that the row sees is outside [0, num_pages).  A value of
+ * a bf16 cache that is infinite makes the results that see it infinite or NaN. */
+corun_status corun_shared_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t n_groups, const int32_t *group_rows, const void *q,
+                                    int64_t ld_q, const uint8_t *valid, const int32_t *lens,
+                                    const int32_t *prefix_slots, const int32_t *prefix_lens, int32_t max_prefix,
+                                    int32_t max_suffix, void *out, int64_t ld_out, void *ws, int64_t ws_bytes,
+                                    void *stream);
+/* Bytes (>= 0), or a negative corun_status.  Host only. */
+int64_t corun_shared_attention_workspace(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                         int32_t n_groups, const int32_t *group_rows, int32_t max_prefix,
+                                         int32_t max_suffix);
+
 /* The engine's fixed batch size, model configuration and KV description
  * (copies; the k/v/page-table pointers are the caller's borrowed ones).
  * Any out pointer may be NULL. */

@@ -31,7 +31,9 @@ EXPORTS = ("corun_engine_create", "corun_engine_destroy", "corun_decode_step", "
            "corun_sched_output", "corun_sched_state", "corun_sched_last_error",
            "corun_rope_init", "corun_decode_append", "corun_prefill_append", "corun_decode_attention",
            "corun_decode_attention_workspace", "corun_prefill_attention",
-           "corun_prefill_attention_workspace")
+           "corun_prefill_attention_workspace",
+           "corun_beam_select", "corun_beam_select_workspace", "corun_pages_assign", "corun_pages_compact",
+           "corun_pages_workspace", "corun_shared_attention", "corun_shared_attention_workspace")
 
 # kernel ids of corun_time_kernel
 K_QKV_GEMM, K_O_GEMM, K_GATE_UP_GEMM, K_DOWN_GEMM, K_LM_HEAD, K_ATTN_SPLIT, K_ATTN_MERGE, K_RMSNORM, \
@@ -174,6 +176,22 @@ def load():
     L.corun_prefill_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr, i64, ptr, i64, ptr]
     L.corun_prefill_attention_workspace.restype = i64
     L.corun_prefill_attention_workspace.argtypes = [ptr, i32, i32, i32, i32, ptr, ptr]
+    L.corun_beam_select.restype = st
+    L.corun_beam_select.argtypes = [ptr, i64, i32, i32, i32, ptr, ptr, ptr, ptr, i32, i32, ptr, ptr, ptr, ptr, ptr, i64,
+                                    ptr]
+    L.corun_beam_select_workspace.restype = i64
+    L.corun_beam_select_workspace.argtypes = [i32, i32, i32, i32]
+    L.corun_pages_assign.restype = st
+    L.corun_pages_assign.argtypes = [ptr, i32, i32, i32, ptr, ptr, ptr, ptr, ptr, ptr, ptr, i64, ptr]
+    L.corun_pages_compact.restype = st
+    L.corun_pages_compact.argtypes = [ptr, i32, i32, i32, ptr, ptr, ptr, ptr, i64, ptr]
+    L.corun_pages_workspace.restype = i64
+    L.corun_pages_workspace.argtypes = [ptr]
+    L.corun_shared_attention.restype = st
+    L.corun_shared_attention.argtypes = [ptr, i32, i32, i32, i32, i32, ptr, ptr, i64, ptr, ptr, ptr, ptr, i32, i32, ptr,
+                                         i64, ptr, i64, ptr]
+    L.corun_shared_attention_workspace.restype = i64
+    L.corun_shared_attention_workspace.argtypes = [ptr, i32, i32, i32, i32, ptr, i32, i32]
     L.corun_last_error.restype = C.c_char_p
     L.corun_last_error.argtypes = []
     _lib = L
@@ -310,8 +328,9 @@ class KvCache:
     (device int32 [n_slots, max_pages_per_seq]), [num_pages, n_kv_heads,
     page_size, head_dim]; bf16, or e4m3 codes (float8_e4m3fn or uint8) with
     scale bytes (float8_e8m0fnu or uint8) k_scale and v_scale [.., n_kv_heads,
-    tokens / scale_block].  The appends take either; the attention operators
-    read e4m3 caches, bf16 ones are an engine's to attend to.  The tensors are
+    tokens / scale_block].  The appends, the pages' operators and
+    shared_attention take either; decode_attention and prefill_attention read
+    e4m3 caches.  The tensors are
     borrowed and kept alive."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None, scale_block=0, page_table=None):
@@ -341,6 +360,7 @@ class KvCache:
         global _torch
         _torch = _torch or _Torch()
         self._keep = keep = [k, v, k_scale, v_scale, page_table]
+        self.page_table = page_table
         if page_table is None:
             self.kv = kv_struct(KV_CONTIGUOUS, n, k, v, keep, max_seq_len=tokens)
         else:
@@ -407,6 +427,7 @@ class _Torch:
     def __init__(self):
         import torch
         self.bf16, self.ints, self.flags = torch.bfloat16, (torch.int32,), (torch.uint8, torch.bool)
+        self.fp32 = (torch.float32,)
         self.device = torch.cuda.current_device
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -521,6 +542,133 @@ def prefill_attention(cache, layer, q, lens, starts, slots, out, ws=None, stream
     _check(load().corun_prefill_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, ln.size,
                                           ln.ctypes.data, sp, sl.ctypes.data, q.data_ptr(), ldq, out.data_ptr(), ldo, wp,
                                           size, _stream(cache, stream)))
+
+
+# Operators for sequences that share a beginning.
+
+def _need(n):
+    if n < 0:
+        raise CorunError(n, last_error())
+    return n
+
+
+def _beam(t, dtypes, shape, index, name):
+    if t.dtype not in dtypes or t.get_device() != index or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {dtypes[0]} {list(shape)} on cuda:{index}")
+    return t.data_ptr()
+
+
+def beam_select_workspace(vocab, groups, beams, n_keep) -> int:
+    """Bytes of workspace that beam_select needs for these sizes."""
+    return _need(load().corun_beam_select_workspace(vocab, groups, beams, n_keep))
+
+
+def beam_select(logits, scores, beams, tokens, parents, out_scores, ws, valid=None, finished=None, weights=None,
+                end_token=-1, out_finished=None, stream=None) -> None:
+    """corun_beam_select: the best continuations of every group of `beams` rows
+    of logits (device fp32 [groups beams, vocab], rows of any stride) with the
+    rows' scores (device fp32 [groups beams]).  tokens, parents (int32) and
+    out_scores (fp32), [groups, n_keep], are written best first, parents as row
+    numbers; out_finished (uint8), if given, says which continuations are
+    finished.  valid, finished: uint8 [groups beams]; weights: fp32 [groups
+    beams], factors of the scores where they are compared (length penalty).  ws: a
+    device uint8 tensor of beam_select_workspace bytes, not shared by calls that
+    may overlap.  Does not wait."""
+    global _torch
+    _torch = _torch or _Torch()
+    index, shape = logits.get_device(), logits.shape
+    if logits.dtype is not _torch.fp32[0] or index < 0 or len(shape) != 2 or (shape[1] > 1 and logits.stride(1) != 1) or \
+            shape[1] < 1:
+        raise ValueError("logits: fp32 [groups beams, vocab] on the GPU, the elements of a row contiguous")
+    rows, vocab = shape
+    if beams < 1 or rows < 1 or rows % beams:
+        raise ValueError(f"logits: {rows} rows are not groups of {beams}")
+    if tokens.dim() != 2:
+        raise ValueError("tokens: int32 [groups, n_keep]")
+    groups, keep = rows // beams, tokens.shape[1]
+    flat, out = (rows,), (groups, keep)
+    opt = lambda t, dtypes, name, shape=flat: None if t is None else _beam(t, dtypes, shape, index, name)
+    if index != _torch.device():
+        raise ValueError(f"logits are on cuda:{index}, the current device is cuda:{_torch.device()}")
+    size = ws.numel()
+    _check(load().corun_beam_select(
+        logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, groups, beams,
+        _beam(scores, _torch.fp32, flat, index, "scores"), opt(valid, _torch.flags, "valid"),
+        opt(finished, _torch.flags, "finished"), opt(weights, _torch.fp32, "weights"), end_token, keep,
+        _beam(tokens, _torch.ints, out, index, "tokens"), _beam(parents, _torch.ints, out, index, "parents"),
+        _beam(out_scores, _torch.fp32, out, index, "out_scores"), opt(out_finished, _torch.flags, "out_finished", out),
+        _beam(ws, _torch.flags[:1], (size,), index, "ws"), size,
+        _torch.stream(index) if stream is None else stream.cuda_stream))
+
+
+def pages_workspace(cache) -> int:
+    """Bytes of workspace that pages_assign and pages_compact need for a cache."""
+    return _need(load().corun_pages_workspace(cache._at))
+
+
+def _pages(cache, held, status, ws):
+    if cache.page_table is None:
+        raise ValueError("pages of a cache with a page_table are assigned")
+    size = ws.numel()
+    return (_vec(cache, held, _torch.ints, cache.kv.n_slots, "held"), _vec(cache, status, _torch.ints, 1, "status"),
+            _vec(cache, ws, _torch.flags[:1], size, "ws"), size)
+
+
+def pages_assign(cache, held, src, keep, status, ws, hold=None, stream=None) -> None:
+    """corun_pages_assign: every slot r of a paged cache takes the first keep[r]
+    tokens of slot src[r] (-1: none) and pages for hold[r] tokens (None: keep);
+    whole pages are shared, a part-filled one is copied in all layers unless
+    slot r can keep it.  held: pages of each slot, rewritten with the cache's
+    page_table; all int32 [n_slots] on the device.  status: int32 [1], 0 or why
+    nothing was done (pages missing, or -1).  ws: a device uint8 tensor of
+    pages_workspace bytes, not shared by calls that may overlap.  Does not wait."""
+    hp, sp, wp, size = _pages(cache, held, status, ws)
+    n = cache.kv.n_slots
+    a, b = _vec(cache, src, _torch.ints, n, "src"), _vec(cache, keep, _torch.ints, n, "keep")
+    c = None if hold is None else _vec(cache, hold, _torch.ints, n, "hold")
+    _check(load().corun_pages_assign(cache._at, cache.layers, cache.n_kv_heads, cache.head_dim,
+                                     cache.page_table.data_ptr(), hp, a, b, c, sp, wp, size, _stream(cache, stream)))
+
+
+def pages_compact(cache, held, status, ws, stream=None) -> None:
+    """corun_pages_compact: the held pages move to the lowest numbers, in all
+    layers and in the cache's page_table.  status: int32 [1], how many there are,
+    or -1.  held, ws: as for pages_assign.  Does not wait."""
+    hp, sp, wp, size = _pages(cache, held, status, ws)
+    _check(load().corun_pages_compact(cache._at, cache.layers, cache.n_kv_heads, cache.head_dim,
+                                      cache.page_table.data_ptr(), hp, sp, wp, size, _stream(cache, stream)))
+
+
+def shared_attention_workspace(cache, group_rows, n_heads, max_prefix=0, max_suffix=0) -> int:
+    """Bytes of workspace that shared_attention needs for these sizes."""
+    gr = _np(group_rows, np.int32)
+    return _need(load().corun_shared_attention_workspace(cache._at, n_heads, cache.n_kv_heads, cache.head_dim, gr.size,
+                                                         gr.ctypes.data, max_prefix, max_suffix))
+
+
+def shared_attention(cache, layer, q, group_rows, lens, prefix_lens, out, ws, prefix_slots=None, valid=None,
+                     max_prefix=0, max_suffix=0, stream=None) -> None:
+    """corun_shared_attention: attention of one query token per row (bf16 [rows,
+    n_heads head_dim]) over a bf16 or e4m3 cache, where the rows are groups of
+    group_rows[g] (a host sequence) that share the first prefix_lens[g] tokens
+    of slot prefix_slots[g] (None: of each group's first row); row r's own
+    tokens prefix_lens[g] .. lens[r] - 1 are slot r's.  lens, prefix_lens,
+    prefix_slots: device int32; valid: device uint8 [rows].  ws: a device uint8
+    tensor of shared_attention_workspace bytes, not shared by calls that may
+    overlap.  Does not wait."""
+    rows, nq, ldq, ldo = _attention_rows(cache, q, out)
+    gr = _np(group_rows, np.int32)
+    if gr.ndim != 1 or int(gr.sum(dtype=np.int64)) != rows:
+        raise ValueError(f"group_rows: rows of each group, {rows} in all")
+    ln = _vec(cache, lens, _torch.ints, rows, "lens")
+    pl = _vec(cache, prefix_lens, _torch.ints, gr.size, "prefix_lens")
+    ps = None if prefix_slots is None else _vec(cache, prefix_slots, _torch.ints, gr.size, "prefix_slots")
+    vm = None if valid is None else _vec(cache, valid, _torch.flags, rows, "valid")
+    size = ws.numel()
+    wp = _vec(cache, ws, _torch.flags[:1], size, "ws")
+    _check(load().corun_shared_attention(cache._at, _layer(cache, layer), nq, cache.n_kv_heads, cache.head_dim, gr.size,
+                                         gr.ctypes.data, q.data_ptr(), ldq, vm, ln, ps, pl, max_prefix, max_suffix,
+                                         out.data_ptr(), ldo, wp, size, _stream(cache, stream)))
 
 
 class SchedCfg(C.Structure):

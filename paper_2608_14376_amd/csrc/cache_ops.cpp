@@ -108,6 +108,43 @@ RopeArgs rope_args(const corun_rope &r)
     return a;
 }
 
+corun_status check_heads(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    if (!kv) return set_error(CORUN_E_INVAL, "null kv");
+    corun_status s = check_cache(kv);
+    if (s != CORUN_OK) return s;
+    if (kv->n_slots < 1) return set_error(CORUN_E_CAPACITY, "the cache has no slots");
+    if (kv->layout == CORUN_KV_PAGED && kv->page_size > (1 << 20))
+        return set_error(CORUN_E_SHAPE, "page_size above 2^20");
+    if (head_dim != 64 && head_dim != 128) return set_error(CORUN_E_SHAPE, "head_dim must be 64 or 128");
+    if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || n_heads / n_kv_heads > 16 || n_heads > 4096)
+        return set_errorf(CORUN_E_SHAPE, "%d query heads over %d kv heads: groups of 1 to 16 are supported", n_heads,
+                          n_kv_heads);
+    return CORUN_OK;
+}
+
+corun_status check_rows(const char *name, const void *p, int64_t ld, int64_t width)
+{
+    if (!p) return set_errorf(CORUN_E_INVAL, "null %s", name);
+    if (!aligned16(p) || ld % 8 != 0) return set_errorf(CORUN_E_INVAL, "%s rows must start on 16-byte boundaries", name);
+    if (ld < width)
+        return set_errorf(CORUN_E_SHAPE, "%s row stride %lld below its width %lld", name, (long long)ld, (long long)width);
+    return CORUN_OK;
+}
+
+corun_status check_ws(const void *ws, int64_t bytes, int64_t need)
+{
+    if (need > 0 && (!ws || !aligned16(ws))) return set_error(CORUN_E_INVAL, "the workspace must start on 16 bytes");
+    if (bytes < need)
+        return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)bytes, (long long)need);
+    return CORUN_OK;
+}
+
+corun_status launched(hipError_t e)
+{
+    return e == hipSuccess ? CORUN_OK : set_errorf(CORUN_E_HIP, "launch: %s", hipGetErrorString(e));
+}
+
 }  // namespace corun
 
 using namespace corun;
@@ -145,31 +182,6 @@ extern "C" corun_status corun_rope_init(const corun_rope_cfg *c, corun_rope *out
 }
 
 namespace {
-
-// A cache, the heads on it and one of its layers.
-corun_status check_heads(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim)
-{
-    if (!kv) return set_error(CORUN_E_INVAL, "null kv");
-    corun_status s = check_cache(kv);
-    if (s != CORUN_OK) return s;
-    if (kv->n_slots < 1) return set_error(CORUN_E_CAPACITY, "the cache has no slots");
-    if (kv->layout == CORUN_KV_PAGED && kv->page_size > (1 << 20))
-        return set_error(CORUN_E_SHAPE, "page_size above 2^20");
-    if (head_dim != 64 && head_dim != 128) return set_error(CORUN_E_SHAPE, "head_dim must be 64 or 128");
-    if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || n_heads / n_kv_heads > 16 || n_heads > 4096)
-        return set_errorf(CORUN_E_SHAPE, "%d query heads over %d kv heads: groups of 1 to 16 are supported", n_heads,
-                          n_kv_heads);
-    return CORUN_OK;
-}
-
-corun_status check_rows(const char *name, const void *p, int64_t ld, int64_t width)
-{
-    if (!p) return set_errorf(CORUN_E_INVAL, "null %s", name);
-    if (!aligned16(p) || ld % 8 != 0) return set_errorf(CORUN_E_INVAL, "%s rows must start on 16-byte boundaries", name);
-    if (ld < width)
-        return set_errorf(CORUN_E_SHAPE, "%s row stride %lld below its width %lld", name, (long long)ld, (long long)width);
-    return CORUN_OK;
-}
 
 corun_status check_step_rows(const corun_kv *kv, int32_t rows)
 {
@@ -221,19 +233,6 @@ corun_status check_total(long long rows, long long heads, int log2_most)
 }
 
 long long rows_of(const SeqTable &seq) { return (long long)seq.row0[seq.n - 1] + seq.len[seq.n - 1]; }
-
-corun_status check_ws(const void *ws, int64_t bytes, int64_t need)
-{
-    if (need > 0 && (!ws || !aligned16(ws))) return set_error(CORUN_E_INVAL, "the workspace must start on 16 bytes");
-    if (bytes < need)
-        return set_errorf(CORUN_E_CAPACITY, "workspace of %lld bytes, %lld needed", (long long)bytes, (long long)need);
-    return CORUN_OK;
-}
-
-corun_status launched(hipError_t e)
-{
-    return e == hipSuccess ? CORUN_OK : set_errorf(CORUN_E_HIP, "launch: %s", hipGetErrorString(e));
-}
 
 int longest(const corun_kv *kv, int32_t max_len)
 {

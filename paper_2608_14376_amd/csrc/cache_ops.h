@@ -20,5 +20,11 @@ bool plain_rope(const corun_rope &rope);
 corun_status check_rope(const corun_rope *rope);
 CacheView cache_view(const corun_kv *kv);
 RopeArgs rope_args(const corun_rope &rope);
+// A cache and the heads on it; rows of bf16 heads; a workspace.
+corun_status check_heads(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+corun_status check_rows(const char *name, const void *p, int64_t ld, int64_t width);
+corun_status check_ws(const void *ws, int64_t bytes, int64_t need);
+// A launch's status.
+corun_status launched(hipError_t e);
 
 }  // namespace corun

@@ -1,0 +1,65 @@
+// groups.h -- what the kernels for sequences that share a beginning take, and
+// their launchers: beam.hip (selection), pages.hip (pages of a cache given to
+// slots), shared.hip (attention over shared prefixes).
+#pragma once
+#include "cache.h"
+
+namespace corun {
+
+// Beam selection: row r = group beams + beam; the pointers as corun_beam_select's.
+struct BeamArgs {
+    const float *logits;
+    long long ld;
+    int vocab, groups, beams, keep, end_token;
+    const float *scores, *weights;
+    const uint8_t *valid, *finished;
+    int32_t *tokens, *parents;
+    float *out_scores;
+    uint8_t *out_finished;
+};
+size_t beam_ws(int vocab, int groups, int beams, int keep);
+hipError_t launch_beam_select(const BeamArgs &a, void *ws, hipStream_t st);
+
+// A paged cache's pages as they are copied: per kv head `row` bytes of elements
+// to a block of tokens and `blocks` blocks to a page, and one scale byte to a
+// block where the cache has scales.
+struct PageShape {
+    int slots, width, pages, page_size;                // width: entries of a table row
+    int nkv, blocks, block;                            // block: tokens copied together
+    long long row;                                     // bytes of a block of one kv head
+    int scales;
+};
+// Layers of one copying launch, by value.
+constexpr int COPY_LAYERS = 64;
+struct PageLayers {
+    int n;
+    void *k[COPY_LAYERS], *v[COPY_LAYERS];
+    uint8_t *ks[COPY_LAYERS], *vs[COPY_LAYERS];
+};
+size_t pages_ws(int slots, int width, int pages);
+// Plans and carries out an assignment (src, keep, hold) or, src == nullptr, a
+// compaction; `layer` gives the layers from `first` on.
+typedef void (*LayersOf)(const void *of, int first, PageLayers *out);
+hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const int32_t *src, const int32_t *keep,
+                        const int32_t *hold, int32_t *status, int n_layers, LayersOf layers, const void *of, void *ws,
+                        hipStream_t st);
+
+// Groups of rows, by value: group g owns rows row0[g] .. row0[g + 1] - 1.
+struct GroupTable {
+    int n;
+    int row0[257];
+};
+struct SharedArgs {
+    const uint16_t *q;
+    long long ldq;
+    uint16_t *out;
+    long long ldo;
+    const uint8_t *valid;
+    const int32_t *lens, *prefix_slots, *prefix_lens;
+    int nq, nkv, d, max_prefix, max_suffix;
+};
+size_t shared_ws(const GroupTable &g, int nq, int nkv, int d, int max_prefix, int max_suffix);
+hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheView &cv, const CacheLayer &cl, float *ws,
+                         hipStream_t st);
+
+}  // namespace corun

@@ -1,0 +1,328 @@
+// pages.hip -- pages of a paged cache given to slots, on the device: fork,
+// reorder, cut, grow, free (corun_pages_assign) and compact
+// (corun_pages_compact).
+//
+// Nothing is kept between calls but the table and the slots' counts: which pages
+// are in use follows from them.  Four launches, none of which waits for the host:
+//  1 clear    every page free
+//  2 mark     a wavefront to a slot checks what it takes, marks its pages, and
+//             stages its new row of the table (the old rows are still read)
+//  3 plan     one workgroup deals the free pages to the slots in order and lists
+//             the copies; it alone decides whether anything is written
+//  4 carry    rows of the table, and the copies, a (page, layer, k or v, kv head)
+//             to a workgroup
+// Marks are integer minima, so their order does not matter.
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "device.h"
+#include "groups.h"
+
+namespace corun {
+namespace {
+
+constexpr int FREE = INT_MAX, WHOLE = -1;              // marks of a page; >= 0: the lowest slot with it as its part-filled page
+
+// The workspace.
+struct Plan {
+    int32_t *head;                                     // [16]
+    int32_t *mark;                                     // [pages]; compaction: then a page's new number
+    int32_t *list;                                     // [pages] free pages in order
+    int32_t *fresh0, *first, *total, *tail;            // [slots] first of its fresh pages, pages it has, pages it shall have, part-filled page taken
+    int32_t *from, *to, *count;                        // [max(slots, pages)] copies: pages and tokens
+    int32_t *rows;                                     // [slots][width] staged
+};
+enum { BAD = 0, STATUS, COPIES };                      // of head
+
+__host__ __device__ inline size_t up4(size_t n) { return (n + 3) & ~(size_t)3; }
+
+inline Plan plan_of(void *ws, int slots, int width, int pages)
+{
+    Plan p;
+    int32_t *at = (int32_t *)ws;
+    const auto take = [&](size_t n) { int32_t *q = at; at += up4(n); return q; };
+    const size_t moves = (size_t)std::max(slots, pages);
+    p.head = take(16);
+    p.mark = take(pages);
+    p.list = take(pages);
+    p.fresh0 = take(slots);
+    p.first = take(slots);
+    p.total = take(slots);
+    p.tail = take(slots);
+    p.from = take(moves);
+    p.to = take(moves);
+    p.count = take(moves);
+    p.rows = take((size_t)slots * width);
+    return p;
+}
+
+__global__ __launch_bounds__(256) void k_pages_clear(Plan p, int pages)
+{
+    if (blockIdx.x == 0 && threadIdx.x < 16) p.head[threadIdx.x] = 0;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < pages; i += gridDim.x * 256) p.mark[i] = FREE;
+}
+
+// Assignment: one wavefront to a slot.
+__global__ __launch_bounds__(256) void k_pages_mark(PageShape s, Plan p, const int32_t *__restrict__ table,
+                                                    const int32_t *__restrict__ held, const int32_t *__restrict__ src,
+                                                    const int32_t *__restrict__ keep, const int32_t *__restrict__ hold)
+{
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= s.slots) return;
+    const int from = src[r];
+    int nfull = 0, total = 0, tail = -1;
+    bool bad = from < -1 || from >= s.slots;
+    if (!bad && from >= 0) {
+        const int n = keep[r], m = hold == nullptr ? n : hold[r], has = held[from];
+        bad = has < 0 || has > s.width || n < 0 || n > (long long)has * s.page_size || m < n ||
+              m > (long long)s.width * s.page_size;
+        if (!bad) {
+            nfull = n / s.page_size;
+            total = (int)(((long long)m + s.page_size - 1) / s.page_size);
+            const int taken = nfull + (n > nfull * s.page_size);
+            for (int i = lane; i < taken; i += 64) {
+                const int page = table[(size_t)from * s.width + i];
+                if ((unsigned)page >= (unsigned)s.pages) {
+                    bad = true;
+                    continue;
+                }
+                p.rows[(size_t)r * s.width + i] = page;
+                if (i < nfull) atomicMin(&p.mark[page], WHOLE);
+                else {
+                    atomicMin(&p.mark[page], r);
+                    tail = page;
+                }
+            }
+            const unsigned long long has_tail = __ballot(tail >= 0);
+            if (has_tail) tail = __shfl(tail, __ffsll((long long)has_tail) - 1, 64);
+        }
+    }
+    if (bad) p.head[BAD] = 1;
+    if (lane == 0) {
+        p.first[r] = nfull;
+        p.total[r] = total;
+        p.tail[r] = tail;
+    }
+}
+
+// Sums of the workgroup's values before the caller's (exclusive), and of all, by
+// wavefronts of 64 in order.
+__device__ __forceinline__ int before(int v, int *all, int *lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    int x = v;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();                                  // lds is free
+    if (lane == 63) lds[wave] = x;
+    __syncthreads();
+    int sum = 0, mine = 0;
+    for (int w = 0; w < waves; ++w) {
+        mine += w < wave ? lds[w] : 0;
+        sum += lds[w];
+    }
+    *all = sum;
+    return mine + x - v;
+}
+
+// Assignment: deals the free pages.  One workgroup.
+__global__ __launch_bounds__(1024) void k_pages_plan(PageShape s, Plan p, const int32_t *__restrict__ keep,
+                                                     int32_t *status)
+{
+    __shared__ int lds[16];
+    const int tid = threadIdx.x;
+    if (p.head[BAD]) {
+        if (tid == 0) *status = p.head[STATUS] = -1;
+        return;
+    }
+    long long need = 0;
+    int copies = 0;
+    for (int r0 = 0; r0 < s.slots; r0 += 1024) {
+        const int r = r0 + tid;
+        int fresh = 0, copy = 0, have = 0, tail = -1;
+        if (r < s.slots) {
+            tail = p.tail[r];
+            const bool stays = tail >= 0 && p.mark[tail] == r;
+            copy = tail >= 0 && !stays;
+            have = p.first[r] + stays;
+            fresh = p.total[r] - have;
+        }
+        int all;
+        const long long at = need + before(fresh, &all, lds);
+        need += all;
+        const int c = copies + before(copy, &all, lds);
+        copies += all;
+        if (r < s.slots) {
+            p.fresh0[r] = (int)(at < INT_MAX ? at : INT_MAX);
+            p.first[r] = have;
+            if (copy) {
+                p.from[c] = tail;
+                p.to[c] = (int)(at < INT_MAX ? at : INT_MAX);   // a place in the list of free pages, for now
+                const int rest = keep[r] % s.page_size;
+                p.count[c] = (rest + s.block - 1) / s.block;
+            }
+        }
+    }
+    long long found = 0;
+    for (int i0 = 0; i0 < s.pages && found < need; i0 += 1024) {
+        const int i = i0 + tid;
+        const int free = i < s.pages && p.mark[i] == FREE;
+        int all;
+        const int at = (int)found + before(free, &all, lds);
+        if (free) p.list[at] = i;
+        found += all;
+    }
+    __syncthreads();
+    const int left = (int)std::min<long long>(need > found ? need - found : 0, INT_MAX);
+    if (left == 0)
+        for (int c = tid; c < copies; c += 1024) p.to[c] = p.list[p.to[c]];
+    if (tid == 0) {
+        *status = p.head[STATUS] = left;
+        p.head[COPIES] = copies;
+    }
+}
+
+// Compaction: marks of all held pages, one wavefront to a slot.
+__global__ __launch_bounds__(256) void k_pages_held(PageShape s, Plan p, const int32_t *__restrict__ table,
+                                                    const int32_t *__restrict__ held)
+{
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= s.slots) return;
+    const int n = held[r];
+    bool bad = n < 0 || n > s.width;
+    for (int i = lane; !bad && i < n; i += 64) {
+        const int page = table[(size_t)r * s.width + i];
+        if ((unsigned)page >= (unsigned)s.pages) {
+            bad = true;
+            break;
+        }
+        p.mark[page] = WHOLE;
+    }
+    if (bad) p.head[BAD] = 1;
+}
+
+// Compaction: held pages at and above their number go to the free ones below, in
+// order.  One workgroup.
+__global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int32_t *status)
+{
+    __shared__ int lds[16];
+    const int tid = threadIdx.x;
+    if (p.head[BAD]) {
+        if (tid == 0) *status = p.head[STATUS] = -1;
+        return;
+    }
+    int mine = 0, n;
+    for (int i = tid; i < s.pages; i += 1024) mine += p.mark[i] != FREE;
+    before(mine, &n, lds);
+    int high = 0, low = 0;
+    for (int i0 = 0; i0 < s.pages; i0 += 1024) {
+        const int i = i0 + tid;
+        const bool used = i < s.pages && p.mark[i] != FREE;
+        int all;
+        if (i0 < n) {
+            const bool hole = i < n && !used;
+            const int at = low + before(hole, &all, lds);
+            if (hole) p.to[at] = i;
+            low += all;
+        }
+        if (i0 + 1024 > n) {
+            const bool moves = i >= n && used;
+            const int at = high + before(moves, &all, lds);
+            if (moves) p.from[at] = i;
+            high += all;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < s.pages; i += 1024) p.mark[i] = i;
+    __syncthreads();
+    for (int c = tid; c < high; c += 1024) {
+        p.mark[p.from[c]] = p.to[c];
+        p.count[c] = s.blocks;
+    }
+    if (tid == 0) {
+        p.head[COPIES] = high;
+        *status = n;
+        p.head[STATUS] = 0;
+    }
+}
+
+// Carries out the plan: the table's rows (ROWS 1: an assignment's, 2: a
+// compaction's, 0: none), and the copies of layers' pages.
+template <int ROWS>
+__global__ __launch_bounds__(256) void k_pages_carry(PageShape s, Plan p, PageLayers layers, int32_t *__restrict__ table,
+                                                     int32_t *__restrict__ held)
+{
+    if (p.head[STATUS] != 0) return;
+    const int tid = threadIdx.x;
+    if (ROWS == 1)
+        for (int r = blockIdx.x; r < s.slots; r += gridDim.x) {
+            const int total = p.total[r], have = p.first[r], at = p.fresh0[r];
+            for (int i = tid; i < total; i += 256)
+                table[(size_t)r * s.width + i] = i < have ? p.rows[(size_t)r * s.width + i] : p.list[at + i - have];
+            if (tid == 0) held[r] = total;
+        }
+    if (ROWS == 2)
+        for (int r = blockIdx.x; r < s.slots; r += gridDim.x)
+            for (int i = tid; i < held[r]; i += 256) {
+                const int page = table[(size_t)r * s.width + i];
+                table[(size_t)r * s.width + i] = p.mark[page];
+            }
+    const long long items = (long long)p.head[COPIES] * layers.n * 2 * s.nkv;
+    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+        const int h = (int)(it % s.nkv);
+        const long long rest = it / s.nkv;
+        const int which = (int)(rest & 1), l = (int)((rest >> 1) % layers.n), c = (int)((rest >> 1) / layers.n);
+        const int n = p.count[c];
+        const size_t a = (size_t)p.from[c] * s.nkv + h, b = (size_t)p.to[c] * s.nkv + h;
+        uint8_t *base = (uint8_t *)(which ? layers.v[l] : layers.k[l]);
+        const uint4 *from = (const uint4 *)(base + a * s.blocks * s.row);
+        uint4 *to = (uint4 *)(base + b * s.blocks * s.row);
+        const int units = (int)(n * s.row / 16);
+        for (int i = tid; i < units; i += 256) to[i] = from[i];
+        if (s.scales) {
+            uint8_t *sc = which ? layers.vs[l] : layers.ks[l];
+            for (int i = tid; i < n; i += 256) sc[b * s.blocks + i] = sc[a * s.blocks + i];
+        }
+    }
+}
+
+}  // namespace
+
+size_t pages_ws(int slots, int width, int pages)
+{
+    const size_t moves = (size_t)std::max(slots, pages);
+    return 4 * (16 + 2 * up4(pages) + 4 * up4(slots) + 3 * up4(moves) + up4((size_t)slots * width));
+}
+
+hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const int32_t *src, const int32_t *keep,
+                        const int32_t *hold, int32_t *status, int n_layers, LayersOf layers, const void *of, void *ws,
+                        hipStream_t st)
+{
+    const Plan p = plan_of(ws, s.slots, s.width, s.pages);
+    const unsigned by4 = (unsigned)((s.slots + 3) / 4);
+    KLAUNCH(k_pages_clear, dim3(std::min((s.pages + 255) / 256, 1024)), dim3(256), 0, st, p, s.pages);
+    if (src != nullptr) {
+        KLAUNCH(k_pages_mark, dim3(by4), dim3(256), 0, st, s, p, table, held, src, keep, hold);
+        KLAUNCH(k_pages_plan, dim3(1), dim3(1024), 0, st, s, p, keep, status);
+    } else {
+        KLAUNCH(k_pages_held, dim3(by4), dim3(256), 0, st, s, p, table, held);
+        KLAUNCH(k_pages_squeeze, dim3(1), dim3(1024), 0, st, s, p, status);
+    }
+    for (int l = 0; l < n_layers; l += COPY_LAYERS) {
+        PageLayers pl;
+        layers(of, l, &pl);
+        const long long most = (long long)(src != nullptr ? s.slots : (s.pages + 1) / 2) * pl.n * 2 * s.nkv;
+        const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>(most, 8192)));
+        if (l > 0) KLAUNCH((k_pages_carry<0>), grid, dim3(256), 0, st, s, p, pl, table, held);
+        else if (src != nullptr) KLAUNCH((k_pages_carry<1>), grid, dim3(256), 0, st, s, p, pl, table, held);
+        else KLAUNCH((k_pages_carry<2>), grid, dim3(256), 0, st, s, p, pl, table, held);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace corun

@@ -1,0 +1,248 @@
+"""Pages given to slots on the GPU, against lists on the host
+(tests/group_reference.py): tables, counts, status and every element of every
+layer are equal."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_14376_amd import corun
+from tests import group_reference as gref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+class Pool:
+    """A paged cache of random contents beside its host model."""
+
+    def __init__(self, slots=6, width=7, pages=40, ps=32, blk=16, nkv=2, d=64, layers=2, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        shape = (pages, nkv, ps, d)
+        e4m3 = blk > 0
+        make = lambda s: torch.randint(0, 256, s, generator=g, dtype=torch.uint8)
+        if e4m3:
+            self.k, self.v = ([make(shape) for _ in range(layers)] for _ in range(2))
+            self.ks, self.vs = ([make((pages, nkv, ps // blk)) for _ in range(layers)] for _ in range(2))
+        else:
+            bits = lambda: torch.randint(-2**15, 2**15, shape, generator=g, dtype=torch.int16).view(torch.bfloat16)
+            self.k, self.v = ([bits() for _ in range(layers)] for _ in range(2))
+            self.ks = self.vs = []
+        self.blk = blk or 16
+        table = rng.integers(-5, pages + 5, (slots, width)).astype(np.int32)   # what no slot holds may be anything
+        self.model = gref.Pages(table, [0] * slots, pages, ps, self.blk)
+        self.table = torch.from_numpy(table.copy()).to(DEV)
+        self.held = torch.zeros(slots, dtype=torch.int32, device=DEV)
+        self.status = torch.full((1,), 99, dtype=torch.int32, device=DEV)
+        self.dev = [[t.to(DEV) for t in x] for x in (self.k, self.v, self.ks, self.vs)]
+        if e4m3:
+            self.cache = corun.KvCache(*self.dev, blk, self.table)
+        else:
+            self.cache = corun.KvCache(self.dev[0], self.dev[1], page_table=self.table)
+        self.ws = torch.full((corun.pages_workspace(self.cache),), 0xFF, dtype=torch.uint8, device=DEV)
+
+    def host(self, moves):
+        per = lambda t: self.blk if t.dim() == 4 else 1
+        gref.move([(t, per(t)) for x in (self.k, self.v, self.ks, self.vs) for t in x], moves, self.blk)
+
+    def assign(self, src, keep, hold=None, stream=None):
+        d = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device=DEV)
+        args = d(src), d(keep), d(hold)
+        torch.cuda.synchronize()
+        corun.pages_assign(self.cache, self.held, args[0], args[1], self.status, self.ws, hold=args[2], stream=stream)
+        status, moves = self.model.assign(src, keep, keep if hold is None else hold)
+        if status == 0:
+            self.host(moves)
+        self.check(status)
+        return status
+
+    def compact(self):
+        corun.pages_compact(self.cache, self.held, self.status, self.ws)
+        n, moves = self.model.compact()
+        self.host(moves)
+        self.check(n)
+        return n
+
+    def check(self, status):
+        torch.cuda.synchronize()
+        assert self.status.item() == status
+        assert self.held.tolist() == self.model.held
+        assert self.table.tolist() == self.model.table
+        for got, want in zip(self.dev, (self.k, self.v, self.ks, self.vs)):
+            for a, b in zip(got, want):
+                assert torch.equal(a.cpu().view(torch.uint8), b.view(torch.uint8))
+        self.ws.fill_(0xFF)
+        self.status.fill_(99)
+
+
+SHAPES = [dict(), dict(blk=0), dict(blk=0, ps=48, d=128, nkv=1), dict(blk=64, ps=128, d=128, nkv=3, pages=50),
+          dict(blk=16, ps=16, width=20, pages=90, layers=1), dict(blk=32, ps=64, layers=67, nkv=1, pages=30),
+          dict(slots=70, width=3, pages=300, layers=1), dict(slots=1, width=1, pages=1, layers=1),
+          dict(slots=3, width=700, pages=2300, ps=16, layers=1, nkv=1), dict(slots=1100, width=2, pages=2600, ps=16, layers=1, nkv=1)]
+
+
+@pytest.mark.parametrize("kw", SHAPES)
+def test_random_assignments(kw):
+    p = Pool(**kw, seed=len(str(kw)))
+    m, rng = p.model, np.random.default_rng(7)
+    slots, cap = len(m.held), m.width * m.ps
+    for step in range(6 if slots < 1000 else 3):
+        src, keep, hold = [], [], []
+        for r in range(slots):
+            s = int(rng.choice([-1, r, rng.integers(slots)], p=[0.15, 0.35, 0.5]))
+            most = 0 if s < 0 else m.held[s] * m.ps
+            n = int(rng.choice([0, most, rng.integers(most + 1), most // m.ps * m.ps // 2]))
+            more = int(min(cap - n, rng.choice([0, 1, m.ps, rng.integers(3 * m.ps)])))
+            if m.width > 100:
+                more = int(rng.integers(cap - n + 1)) // 2
+            src.append(s)
+            keep.append(n if s >= 0 else int(rng.integers(-9, 9)))
+            hold.append(n + more if s >= 0 else -3)
+        p.assign(src, keep, hold)
+        if step % 3 == 2:
+            p.compact()
+
+
+def test_a_beam_search():
+    """Four beams of one prompt: forked, appended to token by token, reordered, cut short, freed."""
+    p = Pool(slots=5, width=8, pages=24, ps=16, blk=16)
+    assert p.assign([0, -1, -1, -1, -1], [0] * 5, [37, 0, 0, 0, 0]) == 0
+    assert p.assign([0, 0, 0, 0, -1], [37] * 5, [38] * 4 + [0]) == 0
+    assert p.model.table[0][:2] == p.model.table[3][:2] and len({t[2] for t in p.model.table[:4]}) == 4
+    n, rng = 37, np.random.default_rng(3)
+    for _ in range(20):
+        n += 1
+        assert p.assign(rng.integers(0, 4, 4).tolist() + [-1], [n] * 5, [n + 1] * 5) == 0
+    assert p.assign([2, 1, 0, 3, 3], [5, n, 16, 0, n], [5, n + 3, 40, 0, n]) == 0
+    assert p.assign([0, -1, -1, -1, 4], [0] * 5, [128, 0, 0, 0, 0]) == 0
+    assert p.assign([-1] * 5, [0] * 5) == 0 and p.model.held == [0] * 5
+
+
+def test_too_few_pages_change_nothing():
+    p = Pool(slots=4, width=6, pages=10, ps=16)
+    assert p.assign([0, -1, -1, -1], [0] * 4, [70, 0, 0, 0]) == 0                  # 5 pages
+    before = [list(t) for t in p.model.table]
+    assert p.assign([0, 0, 0, 0], [70] * 4, [96] * 4) == 2                         # 4 whole ones, 4 with 6 tokens, 4 behind them
+    assert p.assign([0, 0, 0, 0], [64] * 4, [96] * 4) == 2                         # 4 whole ones, 8 behind them
+    assert before == p.model.table
+    assert p.assign([0, 0, 0, 0], [64] * 4, [80] * 4) == 0                         # 8 in use
+    assert p.assign([0, 1, 2, 3], [80] * 4, [96, 96, 80, 80]) == 0                 # all in use
+    assert p.assign([0, 1, 2, 3], [80] * 4, [96, 96, 96, 80]) == 1
+    assert p.assign([0, 1, 2, 3], [96, 96, 80, 80]) == 0
+
+
+@pytest.mark.parametrize("bad", [
+    dict(src=[-2, 1, 2, 3]), dict(src=[4, 1, 2, 3]), dict(keep=[-1, 0, 0, 0]), dict(keep=[97, 0, 0, 0]), dict(keep=[0, 1, 0, 0]),
+    dict(hold=[11, 0, 0, 0]), dict(hold=[12, 0, 129, 0]), dict(hold=[12, 0, 2**31 - 1, 0]), dict(src=[2**31 - 1, 1, 2, 3]),
+    dict(keep=[2**31 - 1, 0, 0, 0], hold=[2**31 - 1, 0, 0, 0]), dict(src=[-2**31, 1, 2, 3])])
+def test_unsound_arguments_change_nothing(bad):
+    p = Pool(slots=4, width=8, pages=20, ps=16)
+    assert p.assign([0, -1, -1, -1], [0] * 4, [96, 0, 0, 0]) == 0
+    args = dict(src=[0, 1, 2, 3], keep=[12, 0, 0, 0], hold=[12, 0, 0, 0])
+    args.update(bad)
+    if "hold" not in bad and "keep" in bad:
+        args["hold"] = [max(a, b) for a, b in zip(args["keep"], args["hold"])]
+    assert p.assign(**args) == -1
+
+
+@pytest.mark.parametrize("what", ["held", "negative", "page", "page_low"])
+def test_unsound_tables_change_nothing(what):
+    p = Pool(slots=3, width=4, pages=12, ps=16)
+    assert p.assign([0, 1, 2], [0] * 3, [40, 20, 0]) == 0
+    if what in ("held", "negative"):
+        p.model.held[1] = 5 if what == "held" else -1
+        p.held[1] = p.model.held[1]
+    else:
+        p.model.table[1][1] = 12 if what == "page" else -1
+        p.table[1, 1] = p.model.table[1][1]
+    assert p.compact() == -1
+    assert p.assign([0, 1, 2], [40, 20, 0]) == -1
+    assert p.assign([0, -1, 0], [40, 20, 20]) == 0     # what is not taken is not looked at
+    assert p.compact() == 4
+
+
+@pytest.mark.parametrize("blk", [0, 32])
+def test_compact(blk):
+    p = Pool(slots=6, width=5, pages=64, ps=64, blk=blk, layers=3)
+    assert p.assign(list(range(6)), [0] * 6, [320] * 6) == 0
+    assert p.compact() == 30                           # nothing moves
+    assert p.assign([-1, 1, -1, 1, 4, -1], [0, 320, 0, 70, 200, 0]) == 0
+    assert p.compact() == 10
+    assert max(max(t[:n], default=0) for t, n in zip(p.model.table, p.model.held)) == 9
+    assert p.assign([-1] * 6, [0] * 6) == 0
+    assert p.compact() == 0
+
+
+@pytest.mark.parametrize("pages", [1023, 1024, 1025, 3000])
+def test_compact_from_the_top(pages):
+    """Every held page above the count, and pools about the size of a workgroup's pass."""
+    p = Pool(slots=2, width=600, pages=pages, ps=16, layers=1, nkv=1)
+    n = min(500, pages // 2)
+    ids = np.random.default_rng(1).permutation(np.arange(pages - n, pages))
+    p.model.table[0][:n] = ids.tolist()
+    p.model.held[0] = n
+    p.table[0, :n] = torch.from_numpy(ids.astype(np.int32)).to(DEV)
+    p.held[0] = n
+    assert p.compact() == n
+    assert sorted(p.model.table[0][:n]) == list(range(n))
+
+
+def test_captured_calls_replay():
+    """Two graphs that share a workspace, one after another, against the host model at every replay."""
+    p = Pool(slots=4, width=8, pages=24, ps=16, layers=2)
+    assert p.assign([0, -1, -1, -1], [0] * 4, [50, 0, 0, 0]) == 0
+    src, keep, hold = (torch.zeros(4, dtype=torch.int32, device=DEV) for _ in range(3))
+    graphs = []
+    for k in range(2):
+        st, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=st):
+            if k == 0:
+                corun.pages_assign(p.cache, p.held, src, keep, p.status, p.ws, hold=hold)
+            else:
+                corun.pages_compact(p.cache, p.held, p.status, p.ws)
+        graphs.append(g)
+    rng, n = np.random.default_rng(2), 50
+    parents = [0, 0, 0, 0]
+    for step in range(8):
+        a = (parents, [n] * 4, [n + 3] * 4)
+        for t, x in zip((src, keep, hold), a):
+            t.copy_(torch.tensor(x, dtype=torch.int32))
+        graphs[0].replay()
+        status, moves = p.model.assign(*a)
+        assert status == 0
+        p.host(moves)
+        p.check(0)
+        if step % 3 == 1:
+            graphs[1].replay()
+            used, moves = p.model.compact()
+            p.host(moves)
+            p.check(used)
+        n += 3
+        parents = rng.integers(0, 4, 4).tolist()
+
+
+def test_another_stream():
+    p = Pool(slots=4, width=8, pages=24, ps=16)
+    assert p.assign([0, -1, -1, -1], [0] * 4, [50, 0, 0, 0]) == 0
+    assert p.assign([0, 0, 0, 0], [50] * 4, [64] * 4, stream=torch.cuda.Stream()) == 0
+
+
+def test_python_refusals():
+    p = Pool(slots=4)
+    i = torch.zeros(4, dtype=torch.int32, device=DEV)
+    ok = lambda **kw: corun.pages_assign(**{**dict(cache=p.cache, held=p.held, src=i, keep=i, status=p.status, ws=p.ws), **kw})
+    ok()
+    flat = corun.KvCache([torch.zeros((4, 2, 64, 64), dtype=torch.bfloat16, device=DEV)],
+                         [torch.zeros((4, 2, 64, 64), dtype=torch.bfloat16, device=DEV)])
+    for bad in (dict(held=i[:3]), dict(src=i.long()), dict(keep=i.cpu()), dict(hold=i[::2]), dict(status=i),
+                dict(ws=p.ws.int()), dict(cache=flat)):
+        with pytest.raises(ValueError):
+            ok(**bad)
+        if not set(bad) & {"src", "keep", "hold"}:
+            with pytest.raises(ValueError):
+                corun.pages_compact(**{**dict(cache=p.cache, held=p.held, status=p.status, ws=p.ws), **bad})
+    with pytest.raises(corun.CorunError):
+        ok(ws=p.ws[:16])
+    with pytest.raises(corun.CorunError):
+        corun.pages_workspace(flat)
