@@ -45,9 +45,10 @@ hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const
                         hipStream_t st);
 
 // Groups of rows, by value: group g owns rows row0[g] .. row0[g + 1] - 1.
+constexpr int MOST_GROUPS = 256;
 struct GroupTable {
     int n;
-    int row0[257];
+    int row0[MOST_GROUPS + 1];
 };
 struct SharedArgs {
     const uint16_t *q;

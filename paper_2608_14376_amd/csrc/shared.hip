@@ -1,5 +1,19 @@
 // shared.hip -- attention of a decode step whose rows share prefixes
-// (corun_shared_attention).
+// (corun_shared_attention), over bf16 and e4m3 caches.
+//
+// The queries of a group's rows that read one kv head are one matrix: query u =
+// (row in the group) G + head, G query heads to a kv head.  A group's prefix is
+// split over its tokens, and each split is done once for a tile of queries; the
+// tokens that a row has of its own are split likewise, for its G queries alone.
+// Both are workgroups of one launch.  Every split leaves its queries' maximum,
+// sum and weighted values, and a second launch joins them:
+//     M = max_i m_i,  out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i
+// with the prefix's splits before the row's own, in order.  Splits follow from the
+// call's sizes and a row's lengths alone, and a query's arithmetic does not depend
+// on its place in a tile, so rows stay position-invariant.
+//
+// Weights enter the matrix units as two bf16 halves, hi + lo (about 16 bits);
+// bf16 values and the codes of an e4m3 cache times their scale are exact there.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -12,108 +26,773 @@
 namespace corun {
 namespace {
 
-// What row r sees: n tokens, the first `prefix` of them of slot `slot`.  n < 0: the
-// row's lengths are out of the launch's range.
-struct Seen {
-    int n, prefix, slot;
-};
-__device__ __forceinline__ int group_of(const GroupTable &g, int r)
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __forceinline__ float qnan() { return __uint_as_float(0x7fc00000u); }
+
+// The last of n entries of a rising table that is at most u: a load and a count
+// for 64 entries, where a search would wait for one after another.
+__device__ __forceinline__ int last_at_most(const int *t, int n, int u)
 {
-    int lo = 0, hi = g.n - 1;                          // the last group whose first row is at or before r
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (g.row0[mid] <= r) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-__device__ __forceinline__ Seen seen_by(const SharedArgs &a, const GroupTable &g, const CacheView &cv, int gi, int r)
-{
-    const int p = a.prefix_lens[gi], n = a.lens[r], slot = a.prefix_slots == nullptr ? g.row0[gi] : a.prefix_slots[gi];
-    if (a.valid != nullptr && a.valid[r] == 0) return {0, 0, 0};
-    const bool bad = p < 0 || p > a.max_prefix || (unsigned)slot >= (unsigned)cv.n_slots || n < p ||
-                     (long long)n > (long long)p + a.max_suffix || n > cv.cap;
-    return {bad ? -1 : n, p, slot};
+    const int lane = threadIdx.x & 63;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < MOST_GROUPS; i += 64)
+        if (i < n) count += __popcll(__ballot(i + lane < n && t[i + lane] <= u));
+    return __builtin_amdgcn_readfirstlane(count - 1);
 }
 
-// One wavefront to a (row, query head), 64 tokens at a time: a token to a lane
-// for the scores, then D / 64 dimensions to a lane.
-template <int D>
-__global__ __launch_bounds__(64) void k_shared_rows(SharedArgs a, GroupTable gt, CacheView cv, CacheLayer cl)
+// A call's launch: where each group's 32-query blocks (of one kv head) and query
+// tiles start, and the splits.
+struct Shape {
+    int G, mt;                                         // query heads to a kv head; queries of a prefix tile
+    int blocks;                                        // 32-query blocks of a kv head, all groups
+    int chunk_p, splits_p, chunk_s, splits_s;          // tokens of a split, splits
+    int tiles;                                         // query tiles of all groups
+    int qb0[MOST_GROUPS + 1], tile0[MOST_GROUPS + 1];
+};
+
+// A group's prefix.  len < 0: out of the launch's range.
+struct Prefix {
+    int len, slot;
+};
+__device__ __forceinline__ Prefix prefix_of(const SharedArgs &a, const GroupTable &gt, const CacheView &cv, int gi)
 {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x, h = blockIdx.x, r = blockIdx.y, nkv = a.nkv, kvh = h / (a.nq / nkv);
-    const Seen s = seen_by(a, gt, cv, group_of(gt, r), r);
-    uint16_t *out = a.out + (size_t)r * a.ldo + (size_t)h * D + E * lane;
-    const uint16_t *q = a.q + (size_t)r * a.ldq + (size_t)h * D;
-    if (s.n <= 0) {
-        for (int e = 0; e < E; ++e) out[e] = s.n < 0 ? (uint16_t)0x7fc0 : (uint16_t)0;
-        return;
+    const int p = a.prefix_lens[gi], slot = a.prefix_slots == nullptr ? gt.row0[gi] : a.prefix_slots[gi];
+    const bool bad = p < 0 || p > a.max_prefix || (unsigned)slot >= (unsigned)cv.n_slots;
+    return {bad ? -1 : p, slot};
+}
+// Tokens that row r sees, its prefix included: 0 for padding, -1 out of range.
+__device__ __forceinline__ int row_len(const SharedArgs &a, const CacheView &cv, const Prefix &p, int r)
+{
+    const int n = a.lens[r];
+    if (a.valid != nullptr && a.valid[r] == 0) return 0;
+    return p.len < 0 || n < p.len || n - p.len > a.max_suffix || n > cv.cap ? -1 : n;
+}
+
+// What a split leaves of a 32-query block: values [D / 4][32][4], then (maximum in
+// base 2, sum) [32][2].
+template <int D>
+__host__ __device__ constexpr int part_floats() { return 32 * D + 64; }
+template <int D>
+__device__ __forceinline__ float *part_at(float *ws, const Shape &s, int nkv, int split, int kvh, int block)
+{
+    return ws + (((size_t)split * nkv + kvh) * s.blocks + block) * part_floats<D>();
+}
+
+// Transposed LDS read of bytes (ds_read_b64_tr_b8): in each group of 16 lanes,
+// lane a + 2 q points at eight bytes (row q, columns 8 a .. 8 a + 7) and lane i
+// receives column i of rows 0 .. 7.
+__device__ __forceinline__ uint2 read_tr8(const void *lds_ptr)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+        (lds_i32x2 *)(const __attribute__((address_space(3))) void *)lds_ptr);
+    return __builtin_bit_cast(uint2, v);
+}
+
+// Four codes times a power of two, in bf16: exact.
+__device__ __forceinline__ uint2 codes4(uint32_t w, float scale)
+{
+    uint2 o;
+    o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+    o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
+    return o;
+}
+__device__ __forceinline__ uint4 codes8(uint32_t w0, uint32_t w1, float scale)
+{
+    const uint2 a = codes4(w0, scale), b = codes4(w1, scale);
+    return (uint4){a.x, a.y, b.x, b.y};
+}
+
+// Where 16 tokens from position t (a multiple of 16) of a slot stand: their first
+// row of one kv head, and their scale block.
+struct Rows16 {
+    size_t row, blk;
+};
+template <bool PAGED>
+__device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, int slot, int page, int t)
+{
+    if constexpr (PAGED) {
+        const int ps = cv.kv.page_size, in = t % ps;
+        const size_t head = (size_t)page * nkv + kvh;
+        return {head * ps + in, head * (ps >> cv.blk_shift) + (in >> cv.blk_shift)};
     }
-    const float scale = 1.0f / sqrtf((float)D);
-    float m = -INFINITY, l = 0.f, acc[E] = {};
-    bool lost = false;
-    for (int b = 0; b < s.n; b += 64) {
-        const int t = min(b + lane, s.n - 1), slot = t < s.prefix ? s.slot : r;
-        size_t row, blk = 0;
-        if (cv.kv.layout == 1) {
-            const int ps = cv.kv.page_size;
-            int page = cv.kv.page_table[(size_t)slot * cv.kv.max_pages_per_seq + t / ps];
-            if ((unsigned)page >= (unsigned)cv.num_pages) {
-                lost = true;
+    const size_t head = (size_t)slot * nkv + kvh;
+    return {head * cv.kv.max_seq_len + t, head * (cv.kv.max_seq_len >> cv.blk_shift) + (t >> cv.blk_shift)};
+}
+
+// ---------------------------------------------------------------------------
+// Up to 16 MT queries over tokens t_lo .. t_end - 1 of one slot: what a row has of
+// its own, and prefixes of few queries.  Four wavefronts, each with all the
+// queries and 32 tokens of a step of 128, on its own: no barrier in the loop.
+//  * S^T = K q^T on 16x16x32 MFMA.  Keys go from the cache to registers: the
+//    contraction may take the dimensions in any order, so lane (row, l / 16) loads
+//    the (l / 16)th quarter of its token's row in one piece, and the queries are
+//    held in the same order.  Tile T's row m is token 8 (m / 4) + 4 T + m % 4, so
+//    that lane l ends with the scores of tokens 8 (l / 16) .. + 7 of query l % 16,
+//    which is the A operand of
+//  * O += P V.  Values go global -> LDS by direct 16-byte loads and come back
+//    through transposed reads.
+// The next step's loads go out once this step's values are in registers.
+// ---------------------------------------------------------------------------
+template <int D, bool E4>
+constexpr int few_lds() { return 4 * (32 * D * (E4 ? 1 : 2) > 16 * D * 4 ? 32 * D * (E4 ? 1 : 2) : 16 * D * 4); }
+
+template <int D, bool E4, bool PAGED, int MT, class QueryOf>
+__device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*cl)[64], int *lost, const CacheView &cv,
+                                           const CacheLayer &layer, int nkv, int kvh, int slot, int t_lo, int t_end,
+                                           int queries, QueryOf &&query, float *part, int u0)
+{
+    constexpr int EB = E4 ? 1 : 2, RB = D * EB, KCH = RB / 16;       // bytes of a row; its 16-byte units
+    constexpr int NK = RB / 64, NV = 32 * RB / 1024, ET = D / 16, KK = D / 32;
+    const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid == 0) *lost = 0;
+    bf16x8 qf[MT][KK];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const uint16_t *q = 16 * m + hl < queries ? query(16 * m + hl) : nullptr;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            uint4 v = {0u, 0u, 0u, 0u};
+            if (q != nullptr) v = *(const uint4 *)(q + kg * (D / 4) + 8 * kk);
+            qf[m][kk] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    const float scale2 = 1.4426950408889634f / sqrtf((float)D);      // scores in base 2
+    f32x4 acc[MT][ET];
+    float mrun[MT], lrun[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        mrun[m] = -INFINITY;
+        lrun[m] = 0.f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et) acc[m][et] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const uint8_t *kc = (const uint8_t *)layer.k, *vc = (const uint8_t *)layer.v;
+    char *mine = lds + wave * 32 * RB;
+    const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
+    bool bad = false;
+    int tb = (t_lo & ~15) + 32 * wave, pg[2] = {0, 0};
+    auto pages = [&](int t) {                          // of the wavefront's two groups of 16 tokens from t
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (t + 16 * j < t_end) pg[j] = pt[(t + 16 * j) / cv.kv.page_size];
+        }
+    };
+    uint4 kr[2][NK];
+    uint32_t ks = 0, vs = 0;                           // scale bytes of this lane's keys, and of its eight value tokens
+    auto issue = [&](int t) {
+        Rows16 at[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            int page = __builtin_amdgcn_readfirstlane(pg[j]);
+            if (PAGED && (unsigned)page >= (unsigned)cv.num_pages) {
+                if (t + 16 * j < t_end) bad = true;
                 page = 0;
             }
-            const size_t head = (size_t)page * nkv + kvh;
-            row = head * ps + t % ps;
-            blk = head * (ps >> cv.blk_shift) + (t % ps >> cv.blk_shift);
-        } else {
-            const size_t head = (size_t)slot * nkv + kvh;
-            row = head * cv.kv.max_seq_len + t;
-            blk = head * (cv.kv.max_seq_len >> cv.blk_shift) + (t >> cv.blk_shift);
+            at[j] = rows16<PAGED>(cv, nkv, kvh, slot, page, t + 16 * j < t_end ? t + 16 * j : t);
+            if (t + 16 * j >= t_end) at[j] = at[0];    // past the end: the first group again, masked below
         }
-        float ksc = 1.f, vsc = 1.f;
-        if (cv.e4m3) {
-            ksc = __uint_as_float((uint32_t)cl.ks[blk] << 23);
-            vsc = __uint_as_float((uint32_t)cl.vs[blk] << 23);
+        const Rows16 ka = hl & 8 ? at[1] : at[0];
+        const uint8_t *kp = kc + (ka.row + 8 * ((hl >> 2) & 1) + (hl & 3)) * RB + kg * (RB / 4);
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+            for (int j = 0; j < NK; ++j) kr[T][j] = *(const uint4 *)(kp + 4 * T * RB + 16 * j);
+        if constexpr (E4) {
+            ks = layer.ks[ka.blk];
+            vs = layer.vs[(kg & 2 ? at[1] : at[0]).blk];
         }
-        const auto value = [&](const void *base, size_t i) {
-            return cv.e4m3 ? __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)base)[i], 0) : bf2f(((const uint16_t *)base)[i]);
-        };
-        float sc = 0.f;
-#pragma unroll 1
-        for (int i = 0; i < D; ++i) sc += bf2f(q[i]) * value(cl.k, row * D + i);
-        sc *= ksc * scale;
-        const bool on = b + lane < s.n;
-        float mt = on ? sc : -INFINITY;
-        for (int o = 32; o; o >>= 1) mt = fmaxf(mt, __shfl_xor(mt, o, 64));
-        const float mn = fmaxf(m, mt), off = mn == -INFINITY ? 0.f : mn;
-        const float al = __expf(m - off), pe = on ? __expf(sc - off) : 0.f;
-        float sum = pe;
-        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        l = l * al + sum;
-        m = mn;
-        for (int e = 0; e < E; ++e) acc[e] *= al;
-        for (int i = 0; i < min(64, s.n - b); ++i) {
-            const float w = __shfl(pe, i, 64), vs = __shfl(vsc, i, 64);
-            const size_t vr = __shfl((unsigned long long)row, i, 64);
-            for (int e = 0; e < E; ++e) acc[e] += w * (value(cl.v, vr * D + E * lane + e) * vs);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int tk = (j * 64 + lane) / KCH, p = (j * 64 + lane) % KCH;
+            int c;
+            if constexpr (E4) c = p ^ (KCH == 8 ? (tk >> 1) & 7 : (tk >> 2) & 3);
+            else c = p ^ vtile_swz<KCH>(tk);
+            const size_t row = (j * 64 / KCH >= 16 ? at[1] : at[0]).row;
+            __builtin_amdgcn_global_load_lds((const void *)(vc + row * RB + (tk & 15) * RB + 16 * c),
+                                             (lds_void *)(mine + 1024 * j), 16, 0, 0);
+        }
+    };
+    if (tb < t_end) {
+        pages(tb);
+        issue(tb);
+        pages(tb + 128);
+    }
+    for (; tb < t_end; tb += 128) {
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        asm volatile("" ::: "memory");
+        // operands out of the buffers that the next step's loads fill
+        bf16x8 kf[2][KK];
+        const float ksc = __uint_as_float(ks << 23), vsc = __uint_as_float(vs << 23);
+#pragma unroll
+        for (int T = 0; T < 2; ++T)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if constexpr (E4) {
+                    const uint4 w = kr[T][kk / 2];
+                    kf[T][kk] = __builtin_bit_cast(bf16x8, kk & 1 ? codes8(w.z, w.w, ksc) : codes8(w.x, w.y, ksc));
+                } else {
+                    kf[T][kk] = __builtin_bit_cast(bf16x8, kr[T][kk]);
+                }
+            }
+        uint4 vr[ET];                                  // e4m3: the codes in the first two words
+#pragma unroll
+        for (int et = 0; et < ET; ++et) {
+            if constexpr (E4) {
+                const int t = 8 * kg + (hl >> 1), swz = KCH == 8 ? (t >> 1) & 7 : (t >> 2) & 3;
+                const uint2 w = read_tr8(mine + 16 * (t * KCH + (et ^ swz)) + 8 * (hl & 1));
+                vr[et] = (uint4){w.x, w.y, 0u, 0u};
+            } else {
+                uint2 w[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int t = 8 * kg + 4 * r + (hl >> 2), c = 2 * et + ((hl & 3) >> 1);
+                    w[r] = lds_read_tr16(mine + 16 * (t * KCH + (c ^ vtile_swz<KCH>(t))) + 8 * (hl & 1));
+                }
+                vr[et] = (uint4){w[0].x, w[0].y, w[1].x, w[1].y};
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the values are in registers
+        asm volatile("" ::: "memory");
+        if (tb + 128 < t_end) {
+            issue(tb + 128);
+            pages(tb + 256);
+        }
+        const bool edge = tb < t_lo || tb + 32 > t_end;   // wave-uniform: some of the 32 tokens are masked
+        const int first = t_lo - (tb + 8 * kg), behind = t_end - (tb + 8 * kg);   // this lane's real tokens: first .. behind - 1 of 8
+        if (edge) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool off = e < first || e >= behind;
+#pragma unroll
+                for (int et = 0; et < ET; ++et) {
+                    uint32_t *w = (uint32_t *)&vr[et];
+                    if constexpr (E4) w[e / 4] &= off ? ~(0xffu << (8 * (e % 4))) : ~0u;
+                    else w[e / 2] &= off ? ~(0xffffu << (16 * (e % 2))) : ~0u;
+                }
+            }
+        }
+        bf16x8 vf[ET];
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+            vf[et] = __builtin_bit_cast(bf16x8, E4 ? codes8(vr[et].x, vr[et].y, vsc) : vr[et]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            f32x4 st[2];
+            float mt = -INFINITY;
+#pragma unroll
+            for (int T = 0; T < 2; ++T) {
+                st[T] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    st[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T][kk], qf[m][kk], st[T], 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float sv = st[T][e] * scale2;
+                    if (edge) sv = 4 * T + e >= first && 4 * T + e < behind ? sv : -INFINITY;
+                    st[T][e] = sv;
+                    mt = fmaxf(mt, sv);
+                }
+            }
+            mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+            mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+            const float mnew = fmaxf(mrun[m], mt);
+            const float alpha = mnew == mrun[m] ? 1.f : __builtin_amdgcn_exp2f(mrun[m] - mnew);
+            const float moff = mnew == -INFINITY ? 0.f : mnew;
+            uint32_t hi[4], lo[4];
+            float ls = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = __builtin_amdgcn_exp2f(st[i / 2][2 * (i % 2)] - moff);
+                const float b = __builtin_amdgcn_exp2f(st[i / 2][2 * (i % 2) + 1] - moff);
+                ls += a + b;
+                const uint32_t w = f2bf2(a, b);
+                hi[i] = w;
+                lo[i] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+            }
+            lrun[m] = lrun[m] * alpha + ls;
+            mrun[m] = mnew;
+            if (__ballot(alpha != 1.f)) {              // lane l's sums belong to queries 4 (l / 16) + e
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float ae = __shfl(alpha, 4 * kg + e, 64);
+#pragma unroll
+                    for (int et = 0; et < ET; ++et) acc[m][et][e] *= ae;
+                }
+            }
+            const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+            for (int et = 0; et < ET; ++et) {
+                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vf[et], acc[m][et], 0, 0, 0);
+                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vf[et], acc[m][et], 0, 0, 0);
+            }
         }
     }
-    lost = __ballot(lost) != 0ull;
-    for (int e = 0; e < E; ++e) out[e] = f2bf(lost ? __builtin_nanf("") : acc[e] / l);
+    // the four wavefronts in order, 16 queries at a time, through the idle buffers
+    __syncthreads();
+    if (bad) *lost = 1;
+    float *ca = (float *)lds;                          // [4][16][D]
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        lrun[m] += __shfl_xor(lrun[m], 16, 64);
+        lrun[m] += __shfl_xor(lrun[m], 32, 64);
+        if (lane < 16) {
+            cm[wave][16 * m + lane] = mrun[m];
+            cl[wave][16 * m + lane] = lrun[m];
+        }
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ca[(wave * 16 + 4 * kg + e) * D + 16 * et + hl] = acc[m][et][e];
+        __syncthreads();
+        const int here = min(16, queries - 16 * m);
+        for (int i = tid; i < here * (D / 4); i += 256) {
+            const int g = i / (D / 4), d4 = i % (D / 4), u = u0 + 16 * m + g;
+            float M = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) M = fmaxf(M, cm[w][16 * m + g]);
+            const float off = M == -INFINITY ? 0.f : M;
+            float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f(cm[w][16 * m + g] - off);
+                const float4 x = *(const float4 *)(ca + (w * 16 + g) * D + 4 * d4);
+                L += cl[w][16 * m + g] * f;
+                o.x += x.x * f;
+                o.y += x.y * f;
+                o.z += x.z * f;
+                o.w += x.w * f;
+            }
+            float *dst = part + (u / 32) * part_floats<D>();
+            *(float4 *)(dst + (d4 * 32 + u % 32) * 4) = o;
+            if (d4 == 0) *(float2 *)(dst + 32 * D + 2 * (u % 32)) = {*lost ? qnan() : M, L};
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// A tile of 128 queries over tokens t0 .. t_end - 1 of a prefix: four wavefronts
+// of 32 queries each on shared tiles of 64 tokens.  Wavefront w loads the w-th 16
+// tokens of the next tile into registers while this one is computed, and writes
+// them as bf16 (codes times their scale) to the other of two LDS buffers.
+//  * S^T = K Q^T on 32x32x16 MFMA, key rows permuted (pf_key_of_row) so that lane l
+//    ends with eight consecutive keys 16 s + 8 (l / 32) .. + 7 of query l % 32 in
+//    each step s of 16 keys: the operand P^T of
+//  * O^T += V^T P^T, V^T by transposed reads.
+// ---------------------------------------------------------------------------
+template <int KCH>
+__device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
+
+template <int D>
+constexpr int many_lds() { return 4 * 64 * D * 2; }
+
+template <int D, bool E4, bool PAGED, class QueryOf>
+__device__ __forceinline__ void attend_many(char *lds, int *lost, const CacheView &cv, const CacheLayer &layer, int nkv,
+                                            int kvh, int slot, int t0, int t_end, int queries, QueryOf &&query,
+                                            float *part)
+{
+    constexpr int EB = E4 ? 1 : 2, RB = D * EB, RU = RB / 16;        // a row's bytes and 16-byte units in the cache
+    constexpr int NR = 16 * RB / 1024, KCH = D / 8, UNITS = 64 * KCH, DT = D / 32, KS = D / 16;
+    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool active = 32 * wave < queries;           // wave-uniform
+    uint4 *ring = (uint4 *)lds;                        // keys of both buffers, then values
+    if (tid == 0) *lost = 0;
+    bf16x8 qf[KS];
+    {
+        const uint16_t *q = 32 * wave + r32 < queries ? query(32 * wave + r32) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            uint4 v = {0u, 0u, 0u, 0u};
+            if (q != nullptr) v = *(const uint4 *)(q + 16 * ks + 8 * h);
+            qf[ks] = __builtin_bit_cast(bf16x8, v);
+        }
+    }
+    const uint8_t *kc = (const uint8_t *)layer.k, *vc = (const uint8_t *)layer.v;
+    const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
+    int next = t0 + 16 * wave, page = 0;               // the wavefront's group of the next tile to load
+    bool bad = false;
+    auto fetch_page = [&]() {
+        if constexpr (PAGED)
+            if (next < t_end) page = pt[next / cv.kv.page_size];
+    };
+    // the wavefront's next group: whether there is one, and where it stands
+    auto locate = [&](Rows16 &at) -> bool {
+        const bool real = next < t_end;
+        if (real) {
+            int pg = __builtin_amdgcn_readfirstlane(page);
+            if (PAGED && (unsigned)pg >= (unsigned)cv.num_pages) {
+                bad = true;
+                pg = 0;
+            }
+            at = rows16<PAGED>(cv, nkv, kvh, slot, pg, next);
+        }
+        next += 64;
+        return real;
+    };
+    // e4m3: to registers, and from there converted to buffer b of the tile from token k0
+    uint4 kraw[NR] = {}, vraw[NR] = {};
+    uint32_t ks8 = 0, vs8 = 0;
+    auto load = [&]() {                                // past the end: what was loaded before, masked below
+        Rows16 at;
+        if (!locate(at)) return;
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            kraw[j] = *(const uint4 *)(kc + at.row * RB + 1024 * j + 16 * lane);
+            vraw[j] = *(const uint4 *)(vc + at.row * RB + 1024 * j + 16 * lane);
+        }
+        ks8 = layer.ks[at.blk];
+        vs8 = layer.vs[at.blk];
+    };
+    auto store = [&](int k0, int b) {
+        uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
+        const float ksc = __uint_as_float(__builtin_amdgcn_readfirstlane(ks8) << 23);
+        const float vsc = __uint_as_float(__builtin_amdgcn_readfirstlane(vs8) << 23);
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            const int u = 64 * j + lane, row = 16 * wave + u / RU, c = u % RU;
+            uint4 w = vraw[j];
+            if (k0 + 64 > t_end) {
+                const uint32_t use = k0 + row < t_end ? ~0u : 0u;
+                w = (uint4){w.x & use, w.y & use, w.z & use, w.w & use};
+            }
+            K[pf_swz<KCH>(row, 2 * c)] = codes8(kraw[j].x, kraw[j].y, ksc);
+            K[pf_swz<KCH>(row, 2 * c + 1)] = codes8(kraw[j].z, kraw[j].w, ksc);
+            V[row * KCH + ((2 * c) ^ val16_swz<KCH>(row))] = codes8(w.x, w.y, vsc);
+            V[row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row))] = codes8(w.z, w.w, vsc);
+        }
+    };
+    // bf16: straight to buffer b; values past the end are cleared once they have landed
+    auto direct = [&](int b) {
+        Rows16 at;
+        if (!locate(at)) return;
+        uint4 *K = ring + b * UNITS + 16 * wave * KCH, *V = ring + (2 + b) * UNITS + 16 * wave * KCH;
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            const int u = 64 * j + lane, row = u / KCH, p = u % KCH;
+            const size_t off = (at.row + row) * RB;
+            const int ck = pf_swz<KCH>(row, p) % KCH, cv16 = p ^ val16_swz<KCH>(row);   // rows of a group: the same swizzles at any group
+            __builtin_amdgcn_global_load_lds((const void *)(kc + off + 16 * ck), (lds_void *)(K + 64 * j), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const void *)(vc + off + 16 * cv16), (lds_void *)(V + 64 * j), 16, 0, 0);
+        }
+    };
+    auto clear = [&](int k0, int b) {
+        uint4 *V = ring + (2 + b) * UNITS + 16 * wave * KCH;
+        for (int u = lane; u < 16 * KCH; u += 64)
+            if (k0 + 16 * wave + u / KCH >= t_end) V[u] = (uint4){0u, 0u, 0u, 0u};
+    };
+    f32x16 acc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
+    float mrow = -INFINITY, lpart = 0.f;
+    const float scale2 = 1.4426950408889634f / sqrtf((float)D);
+    const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
+
+    fetch_page();
+    if constexpr (E4) {
+        load();
+        fetch_page();
+        store(t0, 0);
+        load();
+    } else {
+        direct(0);
+    }
+    fetch_page();
+    for (int k0 = t0, b = 0; k0 < t_end; k0 += 64, b ^= 1) {
+        if constexpr (!E4) {
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+            asm volatile("" ::: "memory");
+            if (k0 + 64 > t_end) clear(k0, b);
+        }
+        __syncthreads();                               // the tile is in LDS, and the one before is done with
+        if (k0 + 64 < t_end) {
+            if constexpr (E4) {
+                store(k0 + 64, b ^ 1);
+                load();
+            } else {
+                direct(b ^ 1);
+            }
+            fetch_page();
+        }
+        if (!active) continue;
+        const uint4 *Kt = ring + b * UNITS, *Vt = ring + (2 + b) * UNITS;
+        f32x16 st[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) st[kt][j] = 0.f;
+        constexpr int KD = 2;                          // key operands are read that many steps ahead
+        bf16x8 kf[KD + 1][2];
+        int kr = krow;
+        asm volatile("" : "+v"(kr));                   // the steps' addresses are made anew: kept, they cost registers
+        auto kread = [&](int ks) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+                kf[ks % (KD + 1)][kt] = __builtin_bit_cast(bf16x8, Kt[pf_swz<KCH>(32 * kt + kr, 2 * ks + h)]);
+        };
+#pragma unroll
+        for (int ks = 0; ks < KD; ++ks) kread(ks);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + KD < KS) kread(ks + KD);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+                st[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks % (KD + 1)][kt], qf[ks], st[kt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // lane: keys k0 + 32 kt + 16 (j / 8) + 8 h + j % 8 of its query
+        if (k0 + 64 > t_end) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    st[kt][j] = k0 + 32 * kt + 16 * (j >> 3) + 8 * h + (j & 7) < t_end ? st[kt][j] : -INFINITY;
+        }
+        float mt = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
+        const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
+        mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * scale2;   // both halves of the query's keys
+        const float mnew = fmaxf(mrow, mt), moff = mnew == -INFINITY ? 0.f : mnew;
+        if (__ballot(mnew != mrow)) {
+            const float alpha = mnew == mrow ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
+            lpart *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[dt][j] *= alpha;
+            mrow = mnew;
+        }
+        bf16x8 ph[4], pl[4];
+        float ls = 0.f;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e], scale2, -moff));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e + 1], scale2, -moff));
+                ls += x + y;
+                const uint32_t w = f2bf2(x, y);
+                hi[e] = w;
+                lo[e] = f2bf2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
+            }
+            ph[s] = __builtin_bit_cast(bf16x8, hi);
+            pl[s] = __builtin_bit_cast(bf16x8, lo);
+        }
+        lpart += ls;
+        // operand f: step f / DT of 16 keys, dimensions 32 (f % DT) + l % 32
+        constexpr int VD = 3;
+        bf16x8 vf[VD + 1];
+        auto vread = [&](int f) {
+            uint2 w[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int key = 16 * (f / DT) + 8 * h + 4 * r + qv, c = 4 * (f % DT) + 2 * half16 + (a4 >> 1);
+                w[r] = lds_read_tr16((const char *)(Vt + key * KCH + (c ^ val16_swz<KCH>(key))) + 8 * (a4 & 1));
+            }
+            vf[f % (VD + 1)] = __builtin_bit_cast(bf16x8, (uint4){w[0].x, w[0].y, w[1].x, w[1].y});
+        };
+#pragma unroll
+        for (int f = 0; f < VD; ++f) vread(f);
+#pragma unroll
+        for (int f = 0; f < 4 * DT; ++f) {
+            if (f + VD < 4 * DT) vread(f + VD);
+            __builtin_amdgcn_sched_barrier(0);
+            acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % (VD + 1)], ph[f / DT], acc[f % DT], 0, 0, 0);
+            acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % (VD + 1)], pl[f / DT], acc[f % DT], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (bad) *lost = 1;
+    __syncthreads();
+    if (!active) return;
+    // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]
+    const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
+    const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+    float *dst = part + wave * part_floats<D>();
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+            *(float4 *)(dst + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = {acc[dt][j], acc[dt][j + 1], acc[dt][j + 2], acc[dt][j + 3]};
+    if (h == 0) *(float2 *)(dst + 32 * D + 2 * r32) = {*lost ? qnan() : mrow, sum};
+}
+
+// Prefix workgroups first (kv head, query tile, split, the kv head running
+// fastest), then the rows' own (kv head, split, row).
+template <int D, bool E4, bool PAGED, int MT>
+__global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
+                                                         CacheLayer layer, float *__restrict__ ws)
+{
+    constexpr int LDS = MT == 128 && many_lds<D>() > few_lds<D, E4>() ? many_lds<D>() : few_lds<D, E4>();
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    __shared__ float cm[4][64], cl[4][64];
+    __shared__ int lost;
+    const int nkv = a.nkv, G = s.G, kvh = blockIdx.x % nkv, unit = blockIdx.x / nkv;
+    if (unit < s.tiles * s.splits_p) {
+        const int tile = unit % s.tiles, split = unit / s.tiles;
+        const int gi = last_at_most(s.tile0, gt.n, tile);
+        const Prefix p = prefix_of(a, gt, cv, gi);
+        const int t0 = split * s.chunk_p;
+        if (t0 >= p.len) return;
+        const int t_end = min(p.len, t0 + s.chunk_p), u0 = (tile - s.tile0[gi]) * MT, row0 = gt.row0[gi];
+        const int queries = min(MT, (gt.row0[gi + 1] - row0) * G - u0);
+        const auto query = [&](int m) {
+            return a.q + (size_t)(row0 + (u0 + m) / G) * a.ldq + (size_t)(kvh * G + (u0 + m) % G) * D;
+        };
+        float *part = part_at<D>(ws, s, nkv, split, kvh, s.qb0[gi]);
+        if constexpr (MT == 128)
+            attend_many<D, E4, PAGED>(lds, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
+                                      part + (u0 / 32) * part_floats<D>());
+        else
+            attend_few<D, E4, PAGED, MT / 16>(lds, cm, cl, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
+                                              part, u0);
+        return;
+    }
+    const int v = unit - s.tiles * s.splits_p, split = v % s.splits_s, r = v / s.splits_s;
+    const int gi = last_at_most(gt.row0, gt.n, r);
+    const Prefix p = prefix_of(a, gt, cv, gi);
+    const int n = row_len(a, cv, p, r), t0 = (p.len & ~15) + split * s.chunk_s;
+    if (n <= p.len || t0 >= n) return;
+    const auto query = [&](int m) { return a.q + (size_t)r * a.ldq + (size_t)(kvh * G + m) * D; };
+    attend_few<D, E4, PAGED, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, r, max(t0, p.len), min(n, t0 + s.chunk_s), G, query,
+                                part_at<D>(ws, s, nkv, s.splits_p + split, kvh, s.qb0[gi]), (r - gt.row0[gi]) * G);
+}
+
+// Joins the splits: a workgroup takes four dimension fours (y) of a 32-query block
+// of a kv head (x); thread (four, query).
+template <int D>
+__global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
+                                                     float *__restrict__ ws)
+{
+    constexpr int PF = 8;                              // splits whose values are in flight at once
+    const int nkv = a.nkv, G = s.G, kvh = blockIdx.x % nkv, block = blockIdx.x / nkv;
+    const int tid = threadIdx.x, u32 = tid & 31, d4 = 4 * blockIdx.y + (tid >> 5);
+    const int gi = last_at_most(s.qb0, gt.n, block);
+    const int u = 32 * (block - s.qb0[gi]) + u32, r = gt.row0[gi] + u / G;
+    if (r >= gt.row0[gi + 1]) return;
+    const Prefix p = prefix_of(a, gt, cv, gi);
+    const int n = row_len(a, cv, p, r);
+    uint16_t *out = a.out + (size_t)r * a.ldo + (size_t)(kvh * G + u % G) * D + 4 * d4;
+    if (n <= 0) {
+        const uint32_t w = n < 0 ? 0x7fc07fc0u : 0u;
+        *(uint2 *)out = {w, w};
+        return;
+    }
+    const int np = (p.len + s.chunk_p - 1) / s.chunk_p;
+    const int parts = np + (n > p.len ? (n - (p.len & ~15) + s.chunk_s - 1) / s.chunk_s : 0);
+    const auto at = [&](int i) { return part_at<D>(ws, s, nkv, i < np ? i : s.splits_p + i - np, kvh, block); };
+    float M = -INFINITY, L = 0.f;
+    for (int i = 0; i < parts; ++i) M = fmaxf(M, at(i)[32 * D + 2 * u32]);
+    const float off = M == -INFINITY ? 0.f : M;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < parts; i0 += PF) {
+        float4 x[PF];
+        float2 ml[PF];
+#pragma unroll
+        for (int j = 0; j < PF; ++j) {
+            const float *b = at(min(i0 + j, parts - 1));
+            x[j] = *(const float4 *)(b + (d4 * 32 + u32) * 4);
+            ml[j] = *(const float2 *)(b + 32 * D + 2 * u32);
+        }
+#pragma unroll
+        for (int j = 0; j < PF; ++j) {
+            if (i0 + j >= parts) break;
+            const float f = __builtin_amdgcn_exp2f(ml[j].x - off);
+            L += ml[j].y * f;
+            o.x += x[j].x * f;
+            o.y += x[j].y * f;
+            o.z += x[j].z * f;
+            o.w += x[j].w * f;
+        }
+    }
+    const float inv = 1.0f / L;
+    *(uint2 *)out = {f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv)};
+}
+
+Shape shape_of(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix)
+{
+    Shape s;
+    s.G = nq / nkv;
+    int most = 0;
+    for (int i = 0; i < g.n; ++i) most = std::max(most, (g.row0[i + 1] - g.row0[i]) * s.G);
+    s.mt = most <= 16 ? 16 : most <= 32 ? 32 : 128;
+    s.blocks = s.tiles = 0;
+    for (int i = 0; i < g.n; ++i) {
+        const int queries = (g.row0[i + 1] - g.row0[i]) * s.G;
+        s.qb0[i] = s.blocks;
+        s.tile0[i] = s.tiles;
+        s.blocks += (queries + 31) / 32;
+        s.tiles += (queries + s.mt - 1) / s.mt;
+    }
+    s.qb0[g.n] = s.blocks;
+    s.tile0[g.n] = s.tiles;
+    const auto splits = [&](long long tokens, long long wgs, int least) {   // tokens of a split: 512 workgroups in all
+        long long n = std::max<long long>(1, 512 / std::max<long long>(1, wgs));
+        n = std::min<long long>({n, (tokens + least - 1) / least, 256});
+        const long long per = (tokens + n - 1) / n;
+        return (int)std::min<long long>((per + 127) / 128 * 128, 1 << 30);
+    };
+    s.chunk_p = splits(max_prefix, (long long)s.tiles * nkv, 128);
+    s.splits_p = (int)(((long long)max_prefix + s.chunk_p - 1) / s.chunk_p);
+    const long long suffix = (long long)max_suffix + 15;
+    s.chunk_s = splits(suffix, (long long)g.row0[g.n] * nkv, 256);
+    s.splits_s = (int)((suffix + s.chunk_s - 1) / s.chunk_s);
+    return s;
 }
 
 }  // namespace
 
-size_t shared_ws(const GroupTable &, int, int, int, int, int) { return 0; }
+size_t shared_ws(const GroupTable &g, int nq, int nkv, int d, int max_prefix, int max_suffix)
+{
+    const Shape s = shape_of(g, nq, nkv, max_prefix, max_suffix);
+    return (size_t)(s.splits_p + s.splits_s) * nkv * s.blocks * (d == 128 ? part_floats<128>() : part_floats<64>()) *
+           sizeof(float);
+}
 
-hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheView &cv, const CacheLayer &cl, float *,
+hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheView &cv, const CacheLayer &cl, float *ws,
                          hipStream_t st)
 {
-    const dim3 grid(a.nq, g.row0[g.n]);
-    if (a.d == 128) KLAUNCH(k_shared_rows<128>, grid, dim3(64), 0, st, a, g, cv, cl);
-    else if (a.d == 64) KLAUNCH(k_shared_rows<64>, grid, dim3(64), 0, st, a, g, cv, cl);
+    const Shape s = shape_of(g, a.nq, a.nkv, a.max_prefix, a.max_suffix);
+    const long long wgs = ((long long)s.tiles * s.splits_p + (long long)g.row0[g.n] * s.splits_s) * a.nkv;
+    if (wgs > (1 << 24) - 1) return hipErrorInvalidValue;
+    const bool paged = cv.kv.layout == 1;
+#define CORUN_SHARED(D_, E_, P_, M_) \
+    KLAUNCH((k_shared_parts<D_, E_, P_, M_>), dim3((unsigned)wgs), dim3(256), 0, st, a, g, s, cv, cl, ws)
+#define CORUN_SHARED_M(D_, E_, P_)                     \
+    do {                                               \
+        if (s.mt == 16) CORUN_SHARED(D_, E_, P_, 16);  \
+        else if (s.mt == 32) CORUN_SHARED(D_, E_, P_, 32); \
+        else CORUN_SHARED(D_, E_, P_, 128);            \
+    } while (0)
+#define CORUN_SHARED_P(D_, E_)                  \
+    do {                                        \
+        if (paged) CORUN_SHARED_M(D_, E_, true); \
+        else CORUN_SHARED_M(D_, E_, false);     \
+    } while (0)
+    if (a.d == 128 && cv.e4m3) CORUN_SHARED_P(128, true);
+    else if (a.d == 128) CORUN_SHARED_P(128, false);
+    else if (a.d == 64 && cv.e4m3) CORUN_SHARED_P(64, true);
+    else if (a.d == 64) CORUN_SHARED_P(64, false);
     else return hipErrorInvalidValue;
+#undef CORUN_SHARED_P
+#undef CORUN_SHARED_M
+#undef CORUN_SHARED
+    const dim3 grid((unsigned)s.blocks * a.nkv, a.d / 16);
+    if (a.d == 128) KLAUNCH(k_shared_join<128>, grid, dim3(128), 0, st, a, g, s, cv, ws);
+    else KLAUNCH(k_shared_join<64>, grid, dim3(128), 0, st, a, g, s, cv, ws);
     return hipGetLastError();
 }
 
