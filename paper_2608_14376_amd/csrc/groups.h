@@ -17,6 +17,7 @@ struct BeamArgs {
     float *out_scores;
     uint8_t *out_finished;
 };
+constexpr int MOST_BEAMS = 64;
 size_t beam_ws(int vocab, int groups, int beams, int keep);
 hipError_t launch_beam_select(const BeamArgs &a, void *ws, hipStream_t st);
 

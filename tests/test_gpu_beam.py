@@ -118,6 +118,25 @@ def test_ties_go_to_the_lower_row_and_token(V, step):
     check(select(x, s, 4, 16), gref.beam_select(x, s, 4, 16))
 
 
+@pytest.mark.parametrize("V", [40, 9000])
+def test_both_zeros_are_equal(V):
+    x = -np.abs(logits_of(4, V, 9)[0])
+    x[:, 3::7] = -0.0
+    x[:, 5::14] = 0.0
+    s = np.array([0.0, -0.0, -1.0, 0.0], np.float32)
+    check(select(x, s, 4, 16), gref.beam_select(x, s, 4, 16))
+
+
+@pytest.mark.parametrize("V,beams", [(30000, 64), (150, 64), (9000, 40)])
+def test_wide_groups_of_equal_logits(V, beams):
+    """All entries of all lists reach any bound: the slow paths of both launches."""
+    x = np.zeros((beams, V), np.float32)
+    s = -(np.arange(beams) // 2).astype(np.float32) * np.float32(0.25)
+    check(select(x, s, beams, 64), gref.beam_select(x, s, beams, 64))
+    s[:] = 0
+    check(select(x, s, beams, 64), gref.beam_select(x, s, beams, 64))
+
+
 def test_logits_of_any_size():
     rng = np.random.default_rng(4)
     x = rng.standard_normal((6, 12000)).astype(np.float32)
