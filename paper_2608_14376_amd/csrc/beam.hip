@@ -36,36 +36,53 @@ struct Best {
 constexpr int CAP = 1024;                              // candidates that a part sorts at once
 constexpr int MOST = 4096;                             // the same of a group
 
-// Rising unsigned keys of floating-point values, the same for both zeros; NaN has none (0).
+// Rising unsigned keys of floating-point values that are no NaN, the same for both
+// zeros, and back.
 __device__ __forceinline__ uint32_t key32(float x)
 {
     const uint32_t u = __float_as_uint(x + 0.f);
-    return x != x ? 0u : u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ uint32_t key_high(double x)   // of the upper half: order kept, ties added
+__device__ __forceinline__ float of_key32(uint32_t k)
+{
+    return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ uint32_t key_high(double x)   // of the upper half: order kept, ties added; never 0
 {
     const uint32_t u = (uint32_t)__double2hiint(x + 0.0);
-    return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+    return max(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u), 1u);
 }
 
-// exp(d) of d <= 0, 64 bits, relative error below 1e-12: 2^n times the series of
-// exp to the tenth power on |x| <= ln(2) / 2 (next term 3e-13).
+// exp(d) of d in [-700, 0], 64 bits, relative error below 1e-13: 2^(n + f) with n
+// the nearest whole number, 2^f by the polynomial of degree 9 that meets it at the
+// Chebyshev points of [-1/2, 1/2] (relative error 2e-14).  Adding 1.5 2^52 leaves
+// n in the low bits, so nothing but additions and multiplications is needed.
 __device__ __forceinline__ double exp_neg(double d)
 {
-    const double t = fmax(d * 1.4426950408889634074, -1100.0), n = __builtin_rint(t);
-    const double x = (t - n) * 0.69314718055994530942;
-    double p = 1.0 / 3628800.0;
-    p = __builtin_fma(p, x, 1.0 / 362880.0);
-    p = __builtin_fma(p, x, 1.0 / 40320.0);
-    p = __builtin_fma(p, x, 1.0 / 5040.0);
-    p = __builtin_fma(p, x, 1.0 / 720.0);
-    p = __builtin_fma(p, x, 1.0 / 120.0);
-    p = __builtin_fma(p, x, 1.0 / 24.0);
-    p = __builtin_fma(p, x, 1.0 / 6.0);
-    p = __builtin_fma(p, x, 0.5);
-    p = __builtin_fma(p, x, 1.0);
-    p = __builtin_fma(p, x, 1.0);
-    return ldexp(p, (int)n);
+    const double magic = 6755399441055744.0, log2e = 1.4426950408889634074;
+    const double z = __builtin_fma(d, log2e, magic);
+    const double f = __builtin_fma(d, log2e, magic - z);
+    double p = 1.0205905366707709e-07;
+    p = __builtin_fma(p, f, 1.3259645242976312e-06);
+    p = __builtin_fma(p, f, 1.5252672925062890e-05);
+    p = __builtin_fma(p, f, 1.5403433751260721e-04);
+    p = __builtin_fma(p, f, 1.3333558200794317e-03);
+    p = __builtin_fma(p, f, 9.6181291939342940e-03);
+    p = __builtin_fma(p, f, 5.5504108664651670e-02);
+    p = __builtin_fma(p, f, 2.4022650695640340e-01);
+    p = __builtin_fma(p, f, 6.9314718055994620e-01);
+    p = __builtin_fma(p, f, 1.0000000000000135);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(z) << 20), __double2loint(p));
+}
+// exp(x - top), what is below exp(-700) as that
+__device__ __forceinline__ double exp_under(float x, float top)
+{
+    return exp_neg(fmax((double)x - (double)top, -700.0));
+}
+// Lanes' places behind `base` where `on`, in lane order.
+__device__ __forceinline__ int place_of(unsigned long long on, int base)
+{
+    return base + __builtin_amdgcn_mbcnt_hi((uint32_t)(on >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)on, 0));
 }
 
 enum { NONE = 0, LIVE, DONE };
@@ -82,34 +99,39 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
     typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
     __shared__ uint32_t maxima[256];
     __shared__ double wsum[4];
-    __shared__ float cl[CAP], wtop[4];
-    __shared__ int cc[CAP];
+    __shared__ float wtop[4];
+    __shared__ unsigned long long cand[CAP];           // key of the logit, then the column, lower ones larger
     __shared__ int count, wat[4];
-    __shared__ uint32_t bound;
+    __shared__ float bound;
     const int part = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.keep;
-    if (row_kind(a, r) != LIVE) return;
     const float *row = a.logits + (size_t)r * a.ld;
     const int first = part * 1024 * J + 4 * tid;
     float x[4 * J];
+    const auto load = [&]() {
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const int c = first + 1024 * j;
-        if (c + 4 <= a.vocab) {
-            const f4u v = *(const f4u *)(row + c);
+        for (int j = 0; j < J; ++j) {
+            const int c = first + 1024 * j;
+            if (c + 4 <= a.vocab) {
+                const f4u v = *(const f4u *)(row + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e] = v[e];
-        } else {
+                for (int e = 0; e < 4; ++e) x[4 * j + e] = v[e];
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e] = c + e < a.vocab ? row[c + e] : -INFINITY;
+                for (int e = 0; e < 4; ++e) x[4 * j + e] = c + e < a.vocab ? row[c + e] : -INFINITY;
+            }
         }
-    }
-    float mine = -INFINITY;
-    bool bad = false;                                  // NaN or +inf: the row has no sum
+    };
+    if (J == 2) load();                                // few workgroups: ahead of the row's flags
+    if (row_kind(a, r) != LIVE) return;
+    if (J != 2) load();
+    float mine = x[0];
+    bool nan = false;
 #pragma unroll
-    for (int i = 0; i < 4 * J; ++i) {
-        mine = fmaxf(mine, x[i]);
-        bad |= !(x[i] < INFINITY);
+    for (int i = 0; i < 4 * J; i += 2) {
+        mine = fmaxf(mine, fmaxf(x[i], x[i + 1]));
+        nan |= __builtin_isunordered(x[i], x[i + 1]);
     }
+    if (mine != mine) mine = -INFINITY;
     float top = mine;
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     if (lane == 0) wtop[wave] = top;
@@ -136,17 +158,17 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
             for (int i = 0; i < 4; ++i) n += __popcll(__ballot(m[i] >= mid));
             if (n >= K) lo = mid;
             else hi = mid;
-            if (n >= K && n <= 2 * K) break;
+            if (n >= K && n <= K + K / 2) break;
         }
-        if (lane == 0) bound = lo;
+        if (lane == 0) bound = fmaxf(of_key32(lo), -3.4028234663852886e38f);   // -inf is no candidate
     }
     // the others go on with the sum
     double s = 0;
     if (top > -INFINITY) {
 #pragma unroll
-        for (int i = 0; i < 4 * J; ++i) s += exp_neg((double)x[i] - (double)top);
+        for (int i = 0; i < 4 * J; ++i) s += exp_under(x[i], top);
     }
-    if (bad) s = __builtin_nan("");
+    if (nan || top == INFINITY) s = __builtin_nan("");
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
     if (lane == 0) wsum[wave] = s;
     __syncthreads();
@@ -155,30 +177,42 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
         b.top[at] = top;
         b.sum[at] = wsum[0] + wsum[1] + wsum[2] + wsum[3];
     }
-    const uint32_t least = max(bound, key32(-INFINITY) + 1);   // -inf is no candidate
+    // a wavefront's candidates are noted side by side
+    const float least = bound;
+    unsigned long long on[4 * J];
+    int noted = 0;
 #pragma unroll
     for (int i = 0; i < 4 * J; ++i) {
-        if (key32(x[i]) >= least) {
-            const int n = atomicAdd(&count, 1);
-            if (n < CAP) {
-                cl[n] = x[i];
-                cc[n] = first + 1024 * (i / 4) + i % 4;
-            }
-        }
+        on[i] = __ballot(x[i] >= least);
+        noted += __popcll(on[i]);
+    }
+    int base = 0;
+    if (lane == 0 && noted > 0) base = atomicAdd(&count, noted);
+    base = __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+    for (int i = 0; i < 4 * J; ++i) {
+        if (on[i] == 0) continue;
+        const int n = place_of(on[i], base);
+        if (x[i] >= least && n < CAP)
+            cand[n] = (unsigned long long)key32(x[i]) << 32 | ~(uint32_t)(first + 1024 * (i / 4) + i % 4);
+        base += __popcll(on[i]);
     }
     __syncthreads();
     const int n = count;
     float *logit = b.logit + at * K;
     int32_t *col = b.col + at * K;
     if (n <= CAP) {
-        for (int i = tid; i < n; i += 256) {
-            const float v = cl[i];
-            const int c = cc[i];
+        // 2^sub threads count for one candidate
+        const int sub = n <= 32 ? 3 : n <= 64 ? 2 : n <= 128 ? 1 : 0;
+        for (int i = tid >> sub; i < n; i += 256 >> sub) {
+            const unsigned long long c = cand[i];
             int place = 0;
-            for (int k = 0; k < n; ++k) place += cl[k] > v || (cl[k] == v && cc[k] < c);
-            if (place < K) {
-                logit[place] = v;
-                col[place] = c;
+#pragma unroll 4
+            for (int k = tid & ((1 << sub) - 1); k < n; k += 1 << sub) place += cand[k] > c;
+            for (int o = 1; o < 1 << sub; o <<= 1) place += __shfl_xor(place, o, 64);
+            if (place < K && (tid & ((1 << sub) - 1)) == 0) {
+                logit[place] = of_key32((uint32_t)(c >> 32));
+                col[place] = (int)~(uint32_t)c;
             }
         }
         for (int i = n + tid; i < K; i += 256) col[i] = -1;
@@ -252,34 +286,50 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
     __shared__ uint32_t wlo[W], whi[W];
     __shared__ double crank[ROOM], wr[W];
     __shared__ float clogit[ROOM];
-    __shared__ int crow[ROOM], ccol[ROOM];
+    __shared__ int crow[ROOM], ccol[ROOM], sel[T == 1024 ? MOST : 1], selected;
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.keep;
-    if (tid == 0) count = 0;
-    for (int i = wave; i < a.beams; i += W) {
-        const int r = g * a.beams + i;
-        int k = row_kind(a, r);
-        double w = a.weights == nullptr ? 1.0 : (double)a.weights[r], l = 0;
-        const double s = a.scores[r];
-        if (!(w > 0 && w < INFINITY) || !(fabs(s) < INFINITY)) k = NONE;
-        if (k == LIVE) {
-            float m = -INFINITY;
-            for (int p = lane; p < parts; p += 64) m = fmaxf(m, b.top[(size_t)r * parts + p]);
-            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-            double sum = 0;
-            for (int p = lane; p < parts; p += 64) {
-                const float t = b.top[(size_t)r * parts + p];
-                const double ps = b.sum[(size_t)r * parts + p];
-                sum += t > -INFINITY || ps != ps ? ps * exp_neg((double)t - (double)m) : 0.0;
-            }
-            for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
-            l = (double)m + log(sum);
-            if (!(fabs(l) < INFINITY)) k = NONE;       // NaN or +inf among the logits, or nothing but -inf
+    if (tid == 0) count = selected = 0;
+    // rows' log-sums: a wavefront to a row, what it reads of its next rows in flight
+    constexpr int AHEAD = T == 1024 ? 4 : 2;
+    for (int i0 = wave; i0 < a.beams; i0 += AHEAD * W) {
+        float top[AHEAD];
+        double sum[AHEAD], w[AHEAD];
+        float s[AHEAD];
+        int k[AHEAD];
+#pragma unroll
+        for (int m = 0; m < AHEAD; ++m) {
+            const int i = min(i0 + m * W, a.beams - 1), r = g * a.beams + i;
+            const size_t at = (size_t)r * parts + min(lane, parts - 1);
+            top[m] = b.top[at];
+            sum[m] = b.sum[at];
+            s[m] = a.scores[r];
+            w[m] = a.weights == nullptr ? 1.0 : (double)a.weights[r];
+            k[m] = row_kind(a, r);
         }
-        if (lane == 0) {
-            lse[i] = l;
-            score[i] = s;
-            weight[i] = w;
-            kind[i] = k;
+#pragma unroll
+        for (int m = 0; m < AHEAD; ++m) {
+            const int i = i0 + m * W;
+            if (i >= a.beams) break;
+            double l = 0;
+            if (!(w[m] > 0 && w[m] < INFINITY) || !(fabsf(s[m]) < INFINITY)) k[m] = NONE;
+            if (k[m] == LIVE) {
+                const size_t at = (size_t)(g * a.beams + i) * parts;
+                float most = lane < parts ? top[m] : -INFINITY;
+                for (int p = lane + 64; p < parts; p += 64) most = fmaxf(most, b.top[at + p]);
+                for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+                const auto part = [&](float t, double x) { return t > -INFINITY || x != x ? x * exp_under(t, most) : 0.0; };
+                double all = lane < parts ? part(top[m], sum[m]) : 0.0;
+                for (int p = lane + 64; p < parts; p += 64) all += part(b.top[at + p], b.sum[at + p]);
+                for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o, 64);
+                l = (double)most + log(all);
+                if (!(fabs(l) < INFINITY)) k[m] = NONE;   // NaN or +inf among the logits, or nothing but -inf
+            }
+            if (lane == 0) {
+                lse[i] = l;
+                score[i] = (double)s[m];
+                weight[i] = w[m];
+                kind[i] = k[m];
+            }
         }
     }
     __syncthreads();
@@ -307,12 +357,13 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
     const int items = all ? lists * K : lists;         // at most LPT T: 64 beams of at most 64 parts
     uint32_t key[LPT], lo = 0xffffffffu, hi = 0;
     int present = 0;
+    Candidate item[LPT];
 #pragma unroll
     for (int m = 0; m < LPT; ++m) {
         const int i = tid + T * m;
-        Candidate c;
+        Candidate &c = item[m];
         const bool is = i < items && (all ? entry(i / K, i % K, c) : entry(i, 0, c));
-        key[m] = is ? max(key_high(c.rank), 1u) : 0u;
+        key[m] = is ? key_high(c.rank) : 0u;
         if (is) {
             lo = min(lo, key[m]);
             hi = max(hi, key[m]);
@@ -349,29 +400,38 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
             for (int w = 0; w < W; ++w) n += wn[step & 1][w];
             if (n >= K) lo = mid;
             else hi = mid;
-            if (n >= K && n <= 2 * K) break;
+            if (n >= K && n <= K + K / 2) break;
         }
     }
-    const auto note = [&](const Candidate &c) {
-        const int n = atomicAdd(&count, 1);
-        if (n >= ROOM) return;
+    const auto note = [&](const Candidate &c, bool is) {   // all lanes of a wavefront
+        const unsigned long long on = __ballot(is);
+        if (on == 0) return;
+        int base = 0;
+        if (lane == 0) base = atomicAdd(&count, __popcll(on));
+        const int n = place_of(on, __builtin_amdgcn_readfirstlane(base));
+        if (!is || n >= ROOM) return;
         crank[n] = c.rank;
         crow[n] = c.row;
         clogit[n] = c.logit;
         ccol[n] = c.col;
     };
+    if (all) {
 #pragma unroll
-    for (int m = 0; m < LPT; ++m) {
-        if (key[m] < lo) continue;
-        const int i = tid + T * m;
-        Candidate c;
-        if (all) {
-            if (entry(i / K, i % K, c)) note(c);
-        } else {
-            for (int j = 0; j < K; ++j) {
-                if (!entry(i, j, c) || max(key_high(c.rank), 1u) < lo) break;
-                note(c);
-            }
+        for (int m = 0; m < LPT; ++m) note(item[m], key[m] >= lo);
+    } else if constexpr (T == 1024) {
+        // the lists whose heads reach the bound, each read by one wavefront, an entry to a lane
+#pragma unroll
+        for (int m = 0; m < LPT; ++m)
+            if (key[m] >= lo) sel[atomicAdd(&selected, 1)] = tid + T * m;
+        __syncthreads();
+        const int ns = selected;
+        for (int i0 = wave; i0 < ns; i0 += 8 * W) {
+            Candidate c[8];
+            bool is[8];
+#pragma unroll
+            for (int m = 0; m < 8; ++m) is[m] = i0 + m * W < ns && lane < K && entry(sel[min(i0 + m * W, ns - 1)], lane, c[m]);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) note(c[m], is[m] && key_high(c[m].rank) >= lo);
         }
     }
     __syncthreads();
@@ -389,15 +449,18 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         if (a.out_finished != nullptr) a.out_finished[o] = any && (kind[c.row] == DONE || c.col == a.end_token);
     };
     if (n <= ROOM) {
-        for (int i = tid; i < n; i += T) {
+        const int sub = n <= T / 16 ? 4 : n <= T / 8 ? 3 : n <= T / 4 ? 2 : 0;   // 2^sub threads count for one candidate
+        for (int i = tid >> sub; i < n; i += T >> sub) {
             const Candidate c{crank[i], crow[i], clogit[i], ccol[i]};
             int place = 0;
-            for (int k = 0; k < n; ++k) {
+#pragma unroll 4
+            for (int k = tid & ((1 << sub) - 1); k < n; k += 1 << sub) {
                 const double x = crank[k];
                 if (x > c.rank) ++place;
                 else if (x == c.rank) place += better({x, crow[k], clogit[k], ccol[k]}, c);
             }
-            if (place < K) result(place, c, true);
+            for (int o = 1; o < 1 << sub; o <<= 1) place += __shfl_xor(place, o, 64);
+            if (place < K && (tid & ((1 << sub) - 1)) == 0) result(place, c, true);
         }
         for (int i = n + tid; i < K; i += T) result(i, {}, false);
         return;
