@@ -85,11 +85,63 @@ __device__ __forceinline__ int place_of(unsigned long long on, int base)
     return base + __builtin_amdgcn_mbcnt_hi((uint32_t)(on >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)on, 0));
 }
 
+// A wavefront's reduction by a commutative operation, the same bits in every lane:
+// lanes' neighbours by data-parallel moves (pairs, quads, eights, sixteens), then
+// the swaps of halves.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) { return __uint_as_float(moved<CTRL>(__float_as_uint(x))); }
+template <int CTRL>
+__device__ __forceinline__ double moved(double x)
+{
+    return __hiloint2double((int)moved<CTRL>((uint32_t)__double2hiint(x)), (int)moved<CTRL>((uint32_t)__double2loint(x)));
+}
+// the value of the other half of 32 (HALF 16) or 64 lanes (HALF 32)
+template <int HALF>
+__device__ __forceinline__ uint32_t other(uint32_t x)
+{
+    const bool upper = threadIdx.x & HALF;
+    if constexpr (HALF == 16) {
+        const auto two = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return upper ? two[0] : two[1];
+    } else {
+        const auto two = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return upper ? two[0] : two[1];
+    }
+}
+template <int HALF>
+__device__ __forceinline__ float other(float x) { return __uint_as_float(other<HALF>(__float_as_uint(x))); }
+template <int HALF>
+__device__ __forceinline__ double other(double x)
+{
+    return __hiloint2double((int)other<HALF>((uint32_t)__double2hiint(x)), (int)other<HALF>((uint32_t)__double2loint(x)));
+}
+template <class T, class F>
+__device__ __forceinline__ T over_wave(T x, F &&f)
+{
+    x = f(x, moved<0xB1>(x));                          // quad_perm [1, 0, 3, 2]
+    x = f(x, moved<0x4E>(x));                          // quad_perm [2, 3, 0, 1]
+    x = f(x, moved<0x141>(x));                         // row_half_mirror
+    x = f(x, moved<0x140>(x));                         // row_mirror
+    x = f(x, other<16>(x));
+    return f(x, other<32>(x));
+}
+template <class T>
+__device__ __forceinline__ T wave_max(T x) { return over_wave(x, [](T a, T b) { return a > b ? a : b; }); }
+template <class T>
+__device__ __forceinline__ T wave_min(T x) { return over_wave(x, [](T a, T b) { return a < b ? a : b; }); }
+__device__ __forceinline__ double wave_sum(double x) { return over_wave(x, [](double a, double b) { return a + b; }); }
+
 enum { NONE = 0, LIVE, DONE };
 __device__ __forceinline__ int row_kind(const BeamArgs &a, int r)
 {
-    if (a.valid != nullptr && a.valid[r] == 0) return NONE;
-    return a.finished != nullptr && a.finished[r] != 0 ? DONE : LIVE;
+    const uint8_t *v = a.valid, *f = a.finished;       // both loads in flight together
+    const int live = v == nullptr ? 1 : v[r], done = f == nullptr ? 0 : f[r];
+    return live == 0 ? NONE : done != 0 ? DONE : LIVE;
 }
 
 // A part: 1024 J columns, 4 J to a thread, in registers.
@@ -132,8 +184,7 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
         nan |= __builtin_isunordered(x[i], x[i + 1]);
     }
     if (mine != mine) mine = -INFINITY;
-    float top = mine;
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    float top = wave_max(mine);
     if (lane == 0) wtop[wave] = top;
     maxima[tid] = key32(mine);
     if (tid == 0) count = 0;
@@ -148,8 +199,7 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
             m[i] = maxima[64 * i + lane];
             lo = min(lo, m[i]);
         }
-        for (int o = 32; o; o >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-        lo = __builtin_amdgcn_readfirstlane(lo);
+        lo = __builtin_amdgcn_readfirstlane(wave_min(lo));
         hi = __builtin_amdgcn_readfirstlane(key32(top)) + 1;
         while (hi - lo > 1) {
             const uint32_t mid = lo + (hi - lo) / 2;
@@ -169,7 +219,7 @@ __global__ __launch_bounds__(256) void k_beam_part(BeamArgs a, Best b, int parts
         for (int i = 0; i < 4 * J; ++i) s += exp_under(x[i], top);
     }
     if (nan || top == INFINITY) s = __builtin_nan("");
-    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
+    s = wave_sum(s);
     if (lane == 0) wsum[wave] = s;
     __syncthreads();
     const size_t at = (size_t)r * parts + part;
@@ -276,19 +326,31 @@ __device__ __forceinline__ bool better(const Candidate &x, const Candidate &y)
 }
 
 // One group.  Items are all of the group's entries, or where these are more than
-// 4 T, its lists' heads, whose lists are then walked as far as the bound.
+// 4 T, its lists' heads; then the lists of those that reach the bound are read.
 template <int T>
 __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
 {
-    constexpr int W = T / 64, LPT = 4, ROOM = MOST * T / 1024;
+    constexpr int W = T / 64, LPT = 4, ROOM = MOST;
     __shared__ double lse[MOST_BEAMS], score[MOST_BEAMS], weight[MOST_BEAMS];
     __shared__ int kind[MOST_BEAMS], wn[2][W], wi[W], count;
     __shared__ uint32_t wlo[W], whi[W];
     __shared__ double crank[ROOM], wr[W];
     __shared__ float clogit[ROOM];
-    __shared__ int crow[ROOM], ccol[ROOM], sel[T == 1024 ? MOST : 1], selected;
+    __shared__ int crow[ROOM], ccol[ROOM], sel[LPT * T], selected;
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.keep;
     if (tid == 0) count = selected = 0;
+    // the items' logits and columns, in flight while the rows' sums are formed
+    const int lists = a.beams * parts;
+    const bool all_entries = lists * K <= LPT * T;
+    const int items = all_entries ? lists * K : lists;     // at most LPT T
+    Candidate item[LPT];
+#pragma unroll
+    for (int m = 0; m < LPT; ++m) {
+        const size_t i = min(tid + T * m, items - 1);
+        const size_t at = (size_t)g * lists * K + (all_entries ? i : i * K);
+        item[m].logit = b.logit[at];
+        item[m].col = b.col[at];
+    }
     // rows' log-sums: a wavefront to a row, what it reads of its next rows in flight
     constexpr int AHEAD = T == 1024 ? 4 : 2;
     for (int i0 = wave; i0 < a.beams; i0 += AHEAD * W) {
@@ -316,11 +378,11 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
                 const size_t at = (size_t)(g * a.beams + i) * parts;
                 float most = lane < parts ? top[m] : -INFINITY;
                 for (int p = lane + 64; p < parts; p += 64) most = fmaxf(most, b.top[at + p]);
-                for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+                most = wave_max(most);
                 const auto part = [&](float t, double x) { return t > -INFINITY || x != x ? x * exp_under(t, most) : 0.0; };
                 double all = lane < parts ? part(top[m], sum[m]) : 0.0;
                 for (int p = lane + 64; p < parts; p += 64) all += part(b.top[at + p], b.sum[at + p]);
-                for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o, 64);
+                all = wave_sum(all);
                 l = (double)most + log(all);
                 if (!(fabs(l) < INFINITY)) k[m] = NONE;   // NaN or +inf among the logits, or nothing but -inf
             }
@@ -333,8 +395,8 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         }
     }
     __syncthreads();
-    const int lists = a.beams * parts;
-    const auto entry = [&](int list, int j, Candidate &c) -> bool {
+    // completes a candidate, of which the logit and column are there: entry j of a list
+    const auto complete = [&](int list, int j, Candidate &c) -> bool {
         const int i = list / parts;
         c.row = i;
         if (kind[i] == NONE) return false;
@@ -344,25 +406,25 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
             c.col = a.end_token;
             c.logit = 0.f;
         } else {
-            const size_t at = ((size_t)g * lists + list) * K + j;
-            c.col = b.col[at];
-            c.logit = b.logit[at];
             if (c.col < 0) return false;
             s += (double)c.logit - lse[i];
         }
         c.rank = s * weight[i];
         return fabs(s) < INFINITY && fabs(c.rank) < INFINITY;
     };
-    const bool all = lists * K <= LPT * T;
-    const int items = all ? lists * K : lists;         // at most LPT T: 64 beams of at most 64 parts
+    const auto entry = [&](int list, int j, Candidate &c) -> bool {
+        const size_t at = ((size_t)g * lists + list) * K + j;
+        c.logit = b.logit[at];
+        c.col = b.col[at];
+        return complete(list, j, c);
+    };
     uint32_t key[LPT], lo = 0xffffffffu, hi = 0;
     int present = 0;
-    Candidate item[LPT];
 #pragma unroll
     for (int m = 0; m < LPT; ++m) {
         const int i = tid + T * m;
         Candidate &c = item[m];
-        const bool is = i < items && (all ? entry(i / K, i % K, c) : entry(i, 0, c));
+        const bool is = i < items && (all_entries ? complete(i / K, i % K, c) : complete(i, 0, c));
         key[m] = is ? key_high(c.rank) : 0u;
         if (is) {
             lo = min(lo, key[m]);
@@ -370,10 +432,8 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         }
         present += __popcll(__ballot(is));
     }
-    for (int o = 32; o; o >>= 1) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
-    }
+    lo = wave_min(lo);
+    hi = wave_max(hi);
     if (lane == 0) {
         wlo[wave] = lo;
         whi[wave] = hi;
@@ -415,10 +475,10 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         clogit[n] = c.logit;
         ccol[n] = c.col;
     };
-    if (all) {
+    if (all_entries) {
 #pragma unroll
         for (int m = 0; m < LPT; ++m) note(item[m], key[m] >= lo);
-    } else if constexpr (T == 1024) {
+    } else {
         // the lists whose heads reach the bound, each read by one wavefront, an entry to a lane
 #pragma unroll
         for (int m = 0; m < LPT; ++m)
@@ -528,7 +588,7 @@ hipError_t launch_beam_select(const BeamArgs &a, void *ws, hipStream_t st)
     const dim3 grid(parts, a.groups * a.beams);
     if (per == 2048) KLAUNCH(k_beam_part<2>, grid, dim3(256), 0, st, a, b, parts);
     else KLAUNCH(k_beam_part<8>, grid, dim3(256), 0, st, a, b, parts);
-    if (a.beams * parts * a.keep <= 1024) KLAUNCH(k_beam_pick<256>, dim3(a.groups), dim3(256), 0, st, a, b, parts);
+    if (a.beams <= 8 && a.beams * parts <= 1024) KLAUNCH(k_beam_pick<256>, dim3(a.groups), dim3(256), 0, st, a, b, parts);
     else KLAUNCH(k_beam_pick<1024>, dim3(a.groups), dim3(1024), 0, st, a, b, parts);
     return hipGetLastError();
 }
