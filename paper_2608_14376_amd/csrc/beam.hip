@@ -130,6 +130,14 @@ __device__ __forceinline__ T over_wave(T x, F &&f)
     x = f(x, other<16>(x));
     return f(x, other<32>(x));
 }
+template <class T, class F>
+__device__ __forceinline__ T over_row(T x, F &&f)          // of sixteen lanes
+{
+    x = f(x, moved<0xB1>(x));
+    x = f(x, moved<0x4E>(x));
+    x = f(x, moved<0x141>(x));
+    return f(x, moved<0x140>(x));
+}
 template <class T>
 __device__ __forceinline__ T wave_max(T x) { return over_wave(x, [](T a, T b) { return a > b ? a : b; }); }
 template <class T>
@@ -327,71 +335,59 @@ __device__ __forceinline__ bool better(const Candidate &x, const Candidate &y)
 
 // One group.  Items are all of the group's entries, or where these are more than
 // 4 T, its lists' heads; then the lists of those that reach the bound are read.
+// The launch has few workgroups, and most of its time is waiting for loads that
+// depend on one another and for instructions, so loops are left rolled.
 template <int T>
 __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
 {
-    constexpr int W = T / 64, LPT = 4, ROOM = MOST;
+    constexpr int W = T / 64, LPT = 4, ROOM = MOST, NEAR = 8;
     __shared__ double lse[MOST_BEAMS], score[MOST_BEAMS], weight[MOST_BEAMS];
-    __shared__ int kind[MOST_BEAMS], wn[2][W], wi[W], count;
+    __shared__ int kind[MOST_BEAMS], wn[2][W], wi[W], count, selected, longer;
     __shared__ uint32_t wlo[W], whi[W];
     __shared__ double crank[ROOM], wr[W];
     __shared__ float clogit[ROOM];
-    __shared__ int crow[ROOM], ccol[ROOM], sel[LPT * T], selected;
+    __shared__ int crow[ROOM], ccol[ROOM], sel[LPT * T], rest[LPT * T];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = a.keep;
-    if (tid == 0) count = selected = 0;
+    if (tid == 0) count = selected = longer = 0;
     // the items' logits and columns, in flight while the rows' sums are formed
     const int lists = a.beams * parts;
-    const bool all_entries = lists * K <= LPT * T;
-    const int items = all_entries ? lists * K : lists;     // at most LPT T
+    const bool all = lists * K <= LPT * T;
+    const int items = all ? lists * K : lists;         // at most LPT T
     Candidate item[LPT];
 #pragma unroll
     for (int m = 0; m < LPT; ++m) {
         const size_t i = min(tid + T * m, items - 1);
-        const size_t at = (size_t)g * lists * K + (all_entries ? i : i * K);
+        const size_t at = (size_t)g * lists * K + (all ? i : i * K);
         item[m].logit = b.logit[at];
         item[m].col = b.col[at];
     }
-    // rows' log-sums: a wavefront to a row, what it reads of its next rows in flight
-    constexpr int AHEAD = T == 1024 ? 4 : 2;
-    for (int i0 = wave; i0 < a.beams; i0 += AHEAD * W) {
-        float top[AHEAD];
-        double sum[AHEAD], w[AHEAD];
-        float s[AHEAD];
-        int k[AHEAD];
-#pragma unroll
-        for (int m = 0; m < AHEAD; ++m) {
-            const int i = min(i0 + m * W, a.beams - 1), r = g * a.beams + i;
-            const size_t at = (size_t)r * parts + min(lane, parts - 1);
-            top[m] = b.top[at];
-            sum[m] = b.sum[at];
-            s[m] = a.scores[r];
-            w[m] = a.weights == nullptr ? 1.0 : (double)a.weights[r];
-            k[m] = row_kind(a, r);
+    // rows' log-sums: sixteen lanes to a row
+    for (int i = tid >> 4; i < a.beams; i += T / 16) {
+        const int r = g * a.beams + i, l16 = tid & 15;
+        const float *top = b.top + (size_t)r * parts;
+        const double *sum = b.sum + (size_t)r * parts;
+        int k = row_kind(a, r);
+        const double w = a.weights == nullptr ? 1.0 : (double)a.weights[r];
+        const float s = a.scores[r];
+        float most = -INFINITY;
+        for (int p = l16; p < parts; p += 16) most = fmaxf(most, top[p]);
+        most = over_row(most, [](float x, float y) { return x > y ? x : y; });
+        double total = 0;
+#pragma unroll 2
+        for (int p = l16; p < parts; p += 16) {
+            const float t = top[p];
+            const double x = sum[p];
+            total += t > -INFINITY || x != x ? x * exp_under(t, most) : 0.0;
         }
-#pragma unroll
-        for (int m = 0; m < AHEAD; ++m) {
-            const int i = i0 + m * W;
-            if (i >= a.beams) break;
-            double l = 0;
-            if (!(w[m] > 0 && w[m] < INFINITY) || !(fabsf(s[m]) < INFINITY)) k[m] = NONE;
-            if (k[m] == LIVE) {
-                const size_t at = (size_t)(g * a.beams + i) * parts;
-                float most = lane < parts ? top[m] : -INFINITY;
-                for (int p = lane + 64; p < parts; p += 64) most = fmaxf(most, b.top[at + p]);
-                most = wave_max(most);
-                const auto part = [&](float t, double x) { return t > -INFINITY || x != x ? x * exp_under(t, most) : 0.0; };
-                double all = lane < parts ? part(top[m], sum[m]) : 0.0;
-                for (int p = lane + 64; p < parts; p += 64) all += part(b.top[at + p], b.sum[at + p]);
-                all = wave_sum(all);
-                l = (double)most + log(all);
-                if (!(fabs(l) < INFINITY)) k[m] = NONE;   // NaN or +inf among the logits, or nothing but -inf
-            }
-            if (lane == 0) {
-                lse[i] = l;
-                score[i] = (double)s[m];
-                weight[i] = w[m];
-                kind[i] = k[m];
-            }
+        total = over_row(total, [](double x, double y) { return x + y; });
+        const double l = k == LIVE ? (double)most + log(total) : 0.0;
+        // NaN or +inf among the logits, nothing but -inf, or a score or weight that is none
+        if (!(w > 0 && w < INFINITY) || !(fabsf(s) < INFINITY) || !(fabs(l) < INFINITY)) k = NONE;
+        if (l16 == 0) {
+            lse[i] = l;
+            score[i] = (double)s;
+            weight[i] = w;
+            kind[i] = k;
         }
     }
     __syncthreads();
@@ -422,9 +418,11 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
     int present = 0;
 #pragma unroll
     for (int m = 0; m < LPT; ++m) {
+        key[m] = 0u;
+        if (T * m >= items) continue;
         const int i = tid + T * m;
         Candidate &c = item[m];
-        const bool is = i < items && (all_entries ? complete(i / K, i % K, c) : complete(i, 0, c));
+        const bool is = i < items && complete(all ? i / K : i, all ? i % K : 0, c);
         key[m] = is ? key_high(c.rank) : 0u;
         if (is) {
             lo = min(lo, key[m]);
@@ -449,6 +447,7 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
     if (present < K) lo = 1;                           // all of them
     else {
         ++hi;
+#pragma unroll 1
         for (int step = 1; hi - lo > 1; ++step) {
             const uint32_t mid = lo + (hi - lo) / 2;
             int n = 0;
@@ -463,38 +462,43 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
             if (n >= K && n <= K + K / 2) break;
         }
     }
-    const auto note = [&](const Candidate &c, bool is) {   // all lanes of a wavefront
-        const unsigned long long on = __ballot(is);
-        if (on == 0) return;
-        int base = 0;
-        if (lane == 0) base = atomicAdd(&count, __popcll(on));
-        const int n = place_of(on, __builtin_amdgcn_readfirstlane(base));
-        if (!is || n >= ROOM) return;
+    const auto note = [&](const Candidate &c) {
+        const int n = atomicAdd(&count, 1);
+        if (n >= ROOM) return;
         crank[n] = c.rank;
         crow[n] = c.row;
         clogit[n] = c.logit;
         ccol[n] = c.col;
     };
-    if (all_entries) {
 #pragma unroll
-        for (int m = 0; m < LPT; ++m) note(item[m], key[m] >= lo);
-    } else {
-        // the lists whose heads reach the bound, each read by one wavefront, an entry to a lane
-#pragma unroll
-        for (int m = 0; m < LPT; ++m)
-            if (key[m] >= lo) sel[atomicAdd(&selected, 1)] = tid + T * m;
-        __syncthreads();
-        const int ns = selected;
-        for (int i0 = wave; i0 < ns; i0 += 8 * W) {
-            Candidate c[8];
-            bool is[8];
-#pragma unroll
-            for (int m = 0; m < 8; ++m) is[m] = i0 + m * W < ns && lane < K && entry(sel[min(i0 + m * W, ns - 1)], lane, c[m]);
-#pragma unroll
-            for (int m = 0; m < 8; ++m) note(c[m], is[m] && key_high(c[m].rank) >= lo);
-        }
+    for (int m = 0; m < LPT; ++m) {
+        if (key[m] < lo) continue;
+        if (all) note(item[m]);
+        else sel[atomicAdd(&selected, 1)] = tid + T * m;
     }
     __syncthreads();
+    if (!all) {
+        // the first entries of the lists whose heads reach the bound; where all of
+        // these do, the others
+        const int ns = selected;
+#pragma unroll 1
+        for (int i = tid; i < ns * NEAR; i += T) {
+            const int j = i % NEAR, list = sel[i / NEAR];
+            Candidate c;
+            if (j >= K || !entry(list, j, c) || key_high(c.rank) < lo) continue;
+            note(c);
+            if (j == NEAR - 1) rest[atomicAdd(&longer, 1)] = list;
+        }
+        __syncthreads();
+        const int nl = longer;
+#pragma unroll 1
+        for (int i = wave; i < nl; i += W) {
+            const int j = NEAR + lane;
+            Candidate c;
+            if (j < K && entry(rest[i], j, c) && key_high(c.rank) >= lo) note(c);
+        }
+        __syncthreads();
+    }
     const int n = count;
     const auto result = [&](int place, const Candidate &c, bool any) {
         const size_t o = (size_t)g * K + place;
@@ -509,28 +513,33 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         if (a.out_finished != nullptr) a.out_finished[o] = any && (kind[c.row] == DONE || c.col == a.end_token);
     };
     if (n <= ROOM) {
-        const int sub = n <= T / 16 ? 4 : n <= T / 8 ? 3 : n <= T / 4 ? 2 : 0;   // 2^sub threads count for one candidate
+        // 2^sub threads count for one candidate
+        const int sub = n <= T / 16 ? 4 : n <= T / 8 ? 3 : n <= T / 4 ? 2 : 0, mine = tid & ((1 << sub) - 1);
+#pragma unroll 1
         for (int i = tid >> sub; i < n; i += T >> sub) {
             const Candidate c{crank[i], crow[i], clogit[i], ccol[i]};
             int place = 0;
-#pragma unroll 4
-            for (int k = tid & ((1 << sub) - 1); k < n; k += 1 << sub) {
+#pragma unroll 2
+            for (int k = mine; k < n; k += 1 << sub) {
                 const double x = crank[k];
                 if (x > c.rank) ++place;
                 else if (x == c.rank) place += better({x, crow[k], clogit[k], ccol[k]}, c);
             }
             for (int o = 1; o < 1 << sub; o <<= 1) place += __shfl_xor(place, o, 64);
-            if (place < K && (tid & ((1 << sub) - 1)) == 0) result(place, c, true);
+            if (place < K && mine == 0) result(place, c, true);
         }
         for (int i = n + tid; i < K; i += T) result(i, {}, false);
         return;
     }
     // many equal ones: the best behind the last, K times, over all entries
     Candidate last{INFINITY, -1, INFINITY, -1};
+#pragma unroll 1
     for (int k = 0; k < K; ++k) {
         Candidate best{-INFINITY, INT32_MAX, 0.f, INT32_MAX};
+#pragma unroll 1
         for (int i = tid; i < lists; i += T) {
             Candidate c;
+#pragma unroll 1
             for (int j = 0; j < K && entry(i, j, c); ++j)
                 if (better(last, c)) {
                     if (better(c, best)) best = c;
