@@ -3,15 +3,17 @@
 // (corun_pages_compact).
 //
 // Nothing is kept between calls but the table and the slots' counts: which pages
-// are in use follows from them.  Four launches, none of which waits for the host:
+// are in use follows from them.  A plan is made, then carried out:
 //  1 clear    every page free
-//  2 mark     a wavefront to a slot checks what it takes, marks its pages, and
-//             stages its new row of the table (the old rows are still read)
+//  2 mark     what each slot takes is checked and its pages are marked; its new row
+//             of the table is staged (the old rows are still read)
 //  3 plan     one workgroup deals the free pages to the slots in order and lists
 //             the copies; it alone decides whether anything is written
 //  4 carry    rows of the table, and the copies, a (page, layer, k or v, kv head)
 //             to a workgroup
-// Marks are integer minima, so their order does not matter.
+// Where the marks of all pages fit in LDS and the table is small, 1 to 3 and the
+// table's rows are one workgroup's work, and a call is two launches.  Marks are
+// integer minima, so their order does not matter.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -251,38 +253,225 @@ __global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int
     }
 }
 
+// The whole plan, and the table, of a small pool: one workgroup, marks in LDS.
+constexpr int SMALL_PAGES = 8192, SMALL_SLOTS = 1024, SMALL_TABLE = 1 << 17;
+
+// The most of a value over the workgroup, whose threads all call.
+__device__ __forceinline__ int most_of(int v, int *lds)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) *lds = 0;
+    __syncthreads();
+    for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+    if ((threadIdx.x & 63) == 0) atomicMax(lds, v);
+    __syncthreads();
+    return *lds;
+}
+
+// Calls f(slot, i) for i < n, slot < slots, over the workgroup.
+template <class F>
+__device__ __forceinline__ void over_rows(int slots, int n, F &&f)
+{
+    if (n <= 0) return;
+    const int total = slots * n;                       // at most SMALL_TABLE
+#pragma unroll 4
+    for (int k = threadIdx.x; k < total; k += 1024) f((unsigned)k / (unsigned)n, (unsigned)k % (unsigned)n);
+}
+
+__global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32_t *__restrict__ table,
+                                                      int32_t *__restrict__ held, const int32_t *__restrict__ src,
+                                                      const int32_t *__restrict__ keep, const int32_t *__restrict__ hold,
+                                                      int32_t *status)
+{
+    extern __shared__ int mark[];                      // [pages]
+    __shared__ int from[SMALL_SLOTS], first[SMALL_SLOTS], taken[SMALL_SLOTS], total[SMALL_SLOTS], tail[SMALL_SLOTS],
+        fresh0[SMALL_SLOTS], lds[16], bad, most;
+    const int tid = threadIdx.x, r = tid;
+    const bool slot = r < s.slots;
+    // one thread to a slot
+    int n = 0, m = 0, take = 0;
+    bool wrong = false;
+    if (slot) {
+        const int f = src[r], n0 = keep[r], m0 = hold == nullptr ? n0 : hold[r];
+        wrong = f < -1 || f >= s.slots;
+        if (!wrong && f >= 0) {
+            const int has = held[f];
+            n = n0;
+            m = m0;
+            wrong = has < 0 || has > s.width || n < 0 || n > (long long)has * s.page_size || m < n ||
+                    m > (long long)s.width * s.page_size;
+        }
+        if (wrong) n = m = 0;
+        from[r] = f;
+        first[r] = n / s.page_size;
+        taken[r] = take = first[r] + (n > first[r] * s.page_size);
+        total[r] = (int)(((long long)m + s.page_size - 1) / s.page_size);
+        tail[r] = -1;
+    }
+    if (tid == 0) bad = 0;
+    for (int i = tid; i < s.pages; i += 1024) mark[i] = FREE;
+    const int span = most_of(take, &most);
+    if (wrong) bad = 1;
+    over_rows(s.slots, span, [&](int r, int i) {
+        if (i >= taken[r]) return;
+        const int page = table[(size_t)from[r] * s.width + i];
+        if ((unsigned)page >= (unsigned)s.pages) {
+            bad = 1;
+            return;
+        }
+        p.rows[(size_t)r * s.width + i] = page;
+        if (i < first[r]) atomicMin(&mark[page], WHOLE);
+        else {
+            atomicMin(&mark[page], r);
+            tail[r] = page;
+        }
+    });
+    __syncthreads();
+    if (bad) {
+        if (tid == 0) *status = p.head[STATUS] = -1;
+        return;
+    }
+    int fresh = 0, copy = 0, have = 0, t = -1, need, copies;
+    if (slot) {
+        t = tail[r];
+        const bool stays = t >= 0 && mark[t] == r;
+        copy = t >= 0 && !stays;
+        have = first[r] + stays;
+        fresh = total[r] - have;                       // the table's entries bound the sum
+    }
+    const int at = before(fresh, &need, lds), c = before(copy, &copies, lds);
+    int found = 0;
+    for (int i0 = 0; i0 < s.pages && found < need; i0 += 4096) {
+        const int i = i0 + 4 * tid;
+        bool free[4];
+        int mine = 0, all;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            free[e] = i + e < s.pages && mark[i + e] == FREE;
+            mine += free[e];
+        }
+        int k = found + before(mine, &all, lds);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (free[e]) p.list[k++] = i + e;
+        found += all;
+    }
+    const int left = need > found ? need - found : 0, longest = most_of(slot ? total[r] : 0, &most);
+    if (left == 0) {
+        if (slot) {
+            first[r] = have;
+            fresh0[r] = at;
+            held[r] = total[r];
+        }
+        if (copy) {
+            p.from[c] = t;
+            p.to[c] = p.list[at];
+            p.count[c] = (n % s.page_size + s.block - 1) / s.block;
+        }
+        __syncthreads();
+        over_rows(s.slots, longest, [&](int r, int i) {
+            if (i >= total[r]) return;
+            table[(size_t)r * s.width + i] = i < first[r] ? p.rows[(size_t)r * s.width + i] : p.list[fresh0[r] + i - first[r]];
+        });
+    }
+    if (tid == 0) {
+        *status = p.head[STATUS] = left;
+        p.head[COPIES] = copies;
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_pages_small_squeeze(PageShape s, Plan p, int32_t *__restrict__ table,
+                                                              const int32_t *__restrict__ held, int32_t *status)
+{
+    extern __shared__ int mark[];                      // [pages], then their new numbers
+    __shared__ int has[SMALL_SLOTS], lds[16], bad, most;
+    const int tid = threadIdx.x;
+    int h = tid < s.slots ? held[tid] : 0;
+    const bool wrong = h < 0 || h > s.width;
+    if (wrong) h = 0;
+    if (tid < s.slots) has[tid] = h;
+    if (tid == 0) bad = 0;
+    for (int i = tid; i < s.pages; i += 1024) mark[i] = FREE;
+    const int span = most_of(h, &most);
+    if (wrong) bad = 1;
+    over_rows(s.slots, span, [&](int r, int i) {
+        if (i >= has[r]) return;
+        const int page = table[(size_t)r * s.width + i];
+        if ((unsigned)page >= (unsigned)s.pages) bad = 1;
+        else mark[page] = WHOLE;
+    });
+    __syncthreads();
+    if (bad) {
+        if (tid == 0) *status = p.head[STATUS] = -1;
+        return;
+    }
+    int mine = 0, n;
+    for (int i = tid; i < s.pages; i += 1024) mine += mark[i] != FREE;
+    before(mine, &n, lds);
+    int high = 0, low = 0;
+    for (int i0 = 0; i0 < s.pages; i0 += 1024) {
+        const int i = i0 + tid;
+        const bool used = i < s.pages && mark[i] != FREE;
+        const int hole = i < n && !used, moves = i >= n && used;
+        int all;
+        const int at = before(hole | moves << 16, &all, lds);   // at most 1024 of each
+        if (hole) p.to[low + (at & 0xffff)] = i;
+        if (moves) p.from[high + (at >> 16)] = i;
+        low += all & 0xffff;
+        high += all >> 16;
+    }
+    __syncthreads();
+    for (int i = tid; i < s.pages; i += 1024) mark[i] = i;
+    __syncthreads();
+    for (int c = tid; c < high; c += 1024) {
+        mark[p.from[c]] = p.to[c];
+        p.count[c] = s.blocks;
+    }
+    __syncthreads();
+    over_rows(s.slots, span, [&](int r, int i) {
+        if (i >= has[r]) return;
+        const size_t at = (size_t)r * s.width + i;
+        table[at] = mark[table[at]];
+    });
+    if (tid == 0) {
+        p.head[COPIES] = high;
+        *status = n;
+        p.head[STATUS] = 0;
+    }
+}
+
 // Carries out the plan: the table's rows (ROWS 1: an assignment's, 2: a
-// compaction's, 0: none), and the copies of layers' pages.
+// compaction's, 0: none), and the copies of layers' pages: layer and k or v are the
+// workgroup's y, a copied page and kv head its x.
 template <int ROWS>
 __global__ __launch_bounds__(256) void k_pages_carry(PageShape s, Plan p, PageLayers layers, int32_t *__restrict__ table,
                                                      int32_t *__restrict__ held)
 {
     if (p.head[STATUS] != 0) return;
-    const int tid = threadIdx.x;
-    if (ROWS == 1)
+    const int tid = threadIdx.x, l = blockIdx.y >> 1, which = blockIdx.y & 1;
+    if (ROWS == 1 && blockIdx.y == 0)
         for (int r = blockIdx.x; r < s.slots; r += gridDim.x) {
             const int total = p.total[r], have = p.first[r], at = p.fresh0[r];
             for (int i = tid; i < total; i += 256)
                 table[(size_t)r * s.width + i] = i < have ? p.rows[(size_t)r * s.width + i] : p.list[at + i - have];
             if (tid == 0) held[r] = total;
         }
-    if (ROWS == 2)
+    if (ROWS == 2 && blockIdx.y == 0)
         for (int r = blockIdx.x; r < s.slots; r += gridDim.x)
             for (int i = tid; i < held[r]; i += 256) {
                 const int page = table[(size_t)r * s.width + i];
                 table[(size_t)r * s.width + i] = p.mark[page];
             }
-    const long long items = (long long)p.head[COPIES] * layers.n * 2 * s.nkv;
-    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const int h = (int)(it % s.nkv);
-        const long long rest = it / s.nkv;
-        const int which = (int)(rest & 1), l = (int)((rest >> 1) % layers.n), c = (int)((rest >> 1) / layers.n);
+    uint8_t *base = (uint8_t *)(which ? layers.v[l] : layers.k[l]);
+    const uint32_t nkv = s.nkv, items = (uint32_t)p.head[COPIES] * nkv;   // below 2^32: at most 2^20 copies, 4096 heads
+    for (unsigned long long it = blockIdx.x; it < items; it += gridDim.x) {
+        const uint32_t c = (uint32_t)it / nkv, h = (uint32_t)it % nkv;
         const int n = p.count[c];
-        const size_t a = (size_t)p.from[c] * s.nkv + h, b = (size_t)p.to[c] * s.nkv + h;
-        uint8_t *base = (uint8_t *)(which ? layers.v[l] : layers.k[l]);
+        const size_t a = (size_t)p.from[c] * nkv + h, b = (size_t)p.to[c] * nkv + h;
         const uint4 *from = (const uint4 *)(base + a * s.blocks * s.row);
         uint4 *to = (uint4 *)(base + b * s.blocks * s.row);
         const int units = (int)(n * s.row / 16);
+#pragma unroll 4
         for (int i = tid; i < units; i += 256) to[i] = from[i];
         if (s.scales) {
             uint8_t *sc = which ? layers.vs[l] : layers.ks[l];
@@ -305,21 +494,32 @@ hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const
 {
     const Plan p = plan_of(ws, s.slots, s.width, s.pages);
     const unsigned by4 = (unsigned)((s.slots + 3) / 4);
-    KLAUNCH(k_pages_clear, dim3(std::min((s.pages + 255) / 256, 1024)), dim3(256), 0, st, p, s.pages);
-    if (src != nullptr) {
-        KLAUNCH(k_pages_mark, dim3(by4), dim3(256), 0, st, s, p, table, held, src, keep, hold);
-        KLAUNCH(k_pages_plan, dim3(1), dim3(1024), 0, st, s, p, keep, status);
+    const bool assign = src != nullptr;
+    const bool small = s.pages <= SMALL_PAGES && s.slots <= SMALL_SLOTS && (long long)s.slots * s.width <= SMALL_TABLE;
+    const size_t marks = sizeof(int) * (size_t)s.pages;
+    if (small && assign) {
+        KLAUNCH(k_pages_small, dim3(1), dim3(1024), marks, st, s, p, table, held, src, keep, hold, status);
+    } else if (small) {
+        KLAUNCH(k_pages_small_squeeze, dim3(1), dim3(1024), marks, st, s, p, table, held, status);
     } else {
-        KLAUNCH(k_pages_held, dim3(by4), dim3(256), 0, st, s, p, table, held);
-        KLAUNCH(k_pages_squeeze, dim3(1), dim3(1024), 0, st, s, p, status);
+        KLAUNCH(k_pages_clear, dim3(std::min((s.pages + 255) / 256, 1024)), dim3(256), 0, st, p, s.pages);
+        if (assign) {
+            KLAUNCH(k_pages_mark, dim3(by4), dim3(256), 0, st, s, p, table, held, src, keep, hold);
+            KLAUNCH(k_pages_plan, dim3(1), dim3(1024), 0, st, s, p, keep, status);
+        } else {
+            KLAUNCH(k_pages_held, dim3(by4), dim3(256), 0, st, s, p, table, held);
+            KLAUNCH(k_pages_squeeze, dim3(1), dim3(1024), 0, st, s, p, status);
+        }
     }
     for (int l = 0; l < n_layers; l += COPY_LAYERS) {
         PageLayers pl;
         layers(of, l, &pl);
-        const long long most = (long long)(src != nullptr ? s.slots : (s.pages + 1) / 2) * pl.n * 2 * s.nkv;
-        const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>(most, 8192)));
-        if (l > 0) KLAUNCH((k_pages_carry<0>), grid, dim3(256), 0, st, s, p, pl, table, held);
-        else if (src != nullptr) KLAUNCH((k_pages_carry<1>), grid, dim3(256), 0, st, s, p, pl, table, held);
+        // workgroups of a layer's k or v: as many as it could have copies, up to a
+        // sixteenth of what the chip takes in a few rounds
+        const long long most = (long long)(assign ? s.slots : (s.pages + 1) / 2) * s.nkv;
+        const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>(most, 16384 / (2 * pl.n))), 2 * pl.n);
+        if (small || l > 0) KLAUNCH((k_pages_carry<0>), grid, dim3(256), 0, st, s, p, pl, table, held);
+        else if (assign) KLAUNCH((k_pages_carry<1>), grid, dim3(256), 0, st, s, p, pl, table, held);
         else KLAUNCH((k_pages_carry<2>), grid, dim3(256), 0, st, s, p, pl, table, held);
     }
     return hipGetLastError();

@@ -78,6 +78,8 @@ class Pool:
 SHAPES = [dict(), dict(blk=0), dict(blk=0, ps=48, d=128, nkv=1), dict(blk=64, ps=128, d=128, nkv=3, pages=50),
           dict(blk=16, ps=16, width=20, pages=90, layers=1), dict(blk=32, ps=64, layers=67, nkv=1, pages=30),
           dict(slots=70, width=3, pages=300, layers=1), dict(slots=1, width=1, pages=1, layers=1),
+          dict(pages=9000, ps=16, nkv=1, layers=1), dict(pages=8193, ps=32, blk=0, nkv=1, layers=1, width=40),
+          dict(pages=8192, ps=16, nkv=1, layers=1, width=300, slots=20), dict(slots=3, width=44000, pages=300, ps=16, layers=1, nkv=1),
           dict(slots=3, width=700, pages=2300, ps=16, layers=1, nkv=1), dict(slots=1100, width=2, pages=2600, ps=16, layers=1, nkv=1)]
 
 
@@ -103,9 +105,10 @@ def test_random_assignments(kw):
             p.compact()
 
 
-def test_a_beam_search():
+@pytest.mark.parametrize("pages", [24, 8300])
+def test_a_beam_search(pages):
     """Four beams of one prompt: forked, appended to token by token, reordered, cut short, freed."""
-    p = Pool(slots=5, width=8, pages=24, ps=16, blk=16)
+    p = Pool(slots=5, width=8, pages=pages, ps=16, blk=16, nkv=1)
     assert p.assign([0, -1, -1, -1, -1], [0] * 5, [37, 0, 0, 0, 0]) == 0
     assert p.assign([0, 0, 0, 0, -1], [37] * 5, [38] * 4 + [0]) == 0
     assert p.model.table[0][:2] == p.model.table[3][:2] and len({t[2] for t in p.model.table[:4]}) == 4
@@ -118,8 +121,9 @@ def test_a_beam_search():
     assert p.assign([-1] * 5, [0] * 5) == 0 and p.model.held == [0] * 5
 
 
-def test_too_few_pages_change_nothing():
-    p = Pool(slots=4, width=6, pages=10, ps=16)
+@pytest.mark.parametrize("width", [6, 40000])
+def test_too_few_pages_change_nothing(width):
+    p = Pool(slots=4, width=width, pages=10, ps=16)
     assert p.assign([0, -1, -1, -1], [0] * 4, [70, 0, 0, 0]) == 0                  # 5 pages
     before = [list(t) for t in p.model.table]
     assert p.assign([0, 0, 0, 0], [70] * 4, [96] * 4) == 2                         # 4 whole ones, 4 with 6 tokens, 4 behind them
@@ -136,7 +140,11 @@ def test_too_few_pages_change_nothing():
     dict(hold=[11, 0, 0, 0]), dict(hold=[12, 0, 129, 0]), dict(hold=[12, 0, 2**31 - 1, 0]), dict(src=[2**31 - 1, 1, 2, 3]),
     dict(keep=[2**31 - 1, 0, 0, 0], hold=[2**31 - 1, 0, 0, 0]), dict(src=[-2**31, 1, 2, 3])])
 def test_unsound_arguments_change_nothing(bad):
-    p = Pool(slots=4, width=8, pages=20, ps=16)
+    for pages in (20, 8200):
+        unsound(Pool(slots=4, width=8, pages=pages, ps=16, nkv=1, layers=1), bad)
+
+
+def unsound(p, bad):
     assert p.assign([0, -1, -1, -1], [0] * 4, [96, 0, 0, 0]) == 0
     args = dict(src=[0, 1, 2, 3], keep=[12, 0, 0, 0], hold=[12, 0, 0, 0])
     args.update(bad)
@@ -145,15 +153,16 @@ def test_unsound_arguments_change_nothing(bad):
     assert p.assign(**args) == -1
 
 
+@pytest.mark.parametrize("pages", [12, 8200])
 @pytest.mark.parametrize("what", ["held", "negative", "page", "page_low"])
-def test_unsound_tables_change_nothing(what):
-    p = Pool(slots=3, width=4, pages=12, ps=16)
+def test_unsound_tables_change_nothing(what, pages):
+    p = Pool(slots=3, width=4, pages=pages, ps=16, nkv=1, layers=1)
     assert p.assign([0, 1, 2], [0] * 3, [40, 20, 0]) == 0
     if what in ("held", "negative"):
         p.model.held[1] = 5 if what == "held" else -1
         p.held[1] = p.model.held[1]
     else:
-        p.model.table[1][1] = 12 if what == "page" else -1
+        p.model.table[1][1] = pages if what == "page" else -1
         p.table[1, 1] = p.model.table[1][1]
     assert p.compact() == -1
     assert p.assign([0, 1, 2], [40, 20, 0]) == -1
@@ -173,7 +182,7 @@ def test_compact(blk):
     assert p.compact() == 0
 
 
-@pytest.mark.parametrize("pages", [1023, 1024, 1025, 3000])
+@pytest.mark.parametrize("pages", [1023, 1024, 1025, 3000, 8192, 8193, 9300])
 def test_compact_from_the_top(pages):
     """Every held page above the count, and pools about the size of a workgroup's pass."""
     p = Pool(slots=2, width=600, pages=pages, ps=16, layers=1, nkv=1)
