@@ -9,8 +9,8 @@
 //             of the table is staged (the old rows are still read)
 //  3 plan     one workgroup deals the free pages to the slots in order and lists
 //             the copies; it alone decides whether anything is written
-//  4 carry    rows of the table, and the copies, a (page, layer, k or v, kv head)
-//             to a workgroup
+//  4 carry    rows of the table, and the copies, 16 KB of a page of a layer's k or
+//             v to a workgroup
 // Where the marks of all pages fit in LDS and the table is small, 1 to 3 and the
 // table's rows are one workgroup's work, and a call is two launches.  Marks are
 // integer minima, so their order does not matter.
@@ -442,7 +442,8 @@ __global__ __launch_bounds__(1024) void k_pages_small_squeeze(PageShape s, Plan 
 
 // Carries out the plan: the table's rows (ROWS 1: an assignment's, 2: a
 // compaction's, 0: none), and the copies of layers' pages: layer and k or v are the
-// workgroup's y, a copied page and kv head its x.
+// workgroup's y, pieces of 16 KB of the copied pages its x.
+constexpr int PIECE = 1024;                            // 16-byte units
 template <int ROWS>
 __global__ __launch_bounds__(256) void k_pages_carry(PageShape s, Plan p, PageLayers layers, int32_t *__restrict__ table,
                                                      int32_t *__restrict__ held)
@@ -463,20 +464,34 @@ __global__ __launch_bounds__(256) void k_pages_carry(PageShape s, Plan p, PageLa
                 table[(size_t)r * s.width + i] = p.mark[page];
             }
     uint8_t *base = (uint8_t *)(which ? layers.v[l] : layers.k[l]);
-    const uint32_t nkv = s.nkv, items = (uint32_t)p.head[COPIES] * nkv;   // below 2^32: at most 2^20 copies, 4096 heads
+    uint8_t *sc = s.scales ? (which ? layers.vs[l] : layers.ks[l]) : nullptr;
+    const size_t page = (size_t)s.nkv * s.blocks;      // blocks of a page
+    const uint32_t block_units = (uint32_t)(s.row / 16);
+    const uint32_t pieces = (uint32_t)((page * block_units + PIECE - 1) / PIECE);
+    const unsigned long long items = (unsigned long long)p.head[COPIES] * pieces;
     for (unsigned long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const uint32_t c = (uint32_t)it / nkv, h = (uint32_t)it % nkv;
-        const int n = p.count[c];
-        const size_t a = (size_t)p.from[c] * nkv + h, b = (size_t)p.to[c] * nkv + h;
-        const uint4 *from = (const uint4 *)(base + a * s.blocks * s.row);
-        uint4 *to = (uint4 *)(base + b * s.blocks * s.row);
-        const int units = (int)(n * s.row / 16);
-#pragma unroll 4
-        for (int i = tid; i < units; i += 256) to[i] = from[i];
-        if (s.scales) {
-            uint8_t *sc = which ? layers.vs[l] : layers.ks[l];
-            for (int i = tid; i < n; i += 256) sc[b * s.blocks + i] = sc[a * s.blocks + i];
+        const uint32_t c = (uint32_t)(it / pieces), piece = (uint32_t)(it - (unsigned long long)c * pieces);
+        const uint32_t n = p.count[c], head_units = n * block_units, units = s.nkv * head_units;
+        const size_t a = (size_t)p.from[c] * page, b = (size_t)p.to[c] * page;
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        const u32x4 *from = (const u32x4 *)(base + a * s.row);
+        u32x4 *to = (u32x4 *)(base + b * s.row);
+        u32x4 w[PIECE / 256];
+        uint32_t at[PIECE / 256];
+#pragma unroll
+        for (int k = 0; k < PIECE / 256; ++k) {        // all of a thread's loads, then its stores
+            const uint32_t i = min(piece * PIECE + 256 * k + tid, units - 1), h = i / head_units;
+            at[k] = h * s.blocks * block_units + (i - h * head_units);
+            w[k] = from[at[k]];
         }
+#pragma unroll
+        for (int k = 0; k < PIECE / 256; ++k)
+            if (piece * PIECE + 256 * k + tid < units) to[at[k]] = w[k];
+        if (sc != nullptr && piece == 0)
+            for (uint32_t i = tid; i < s.nkv * n; i += 256) {
+                const uint32_t o = i / n * s.blocks + i % n;
+                sc[b + o] = sc[a + o];
+            }
     }
 }
 
@@ -516,7 +531,8 @@ hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const
         layers(of, l, &pl);
         // workgroups of a layer's k or v: as many as it could have copies, up to a
         // sixteenth of what the chip takes in a few rounds
-        const long long most = (long long)(assign ? s.slots : (s.pages + 1) / 2) * s.nkv;
+        const long long pieces = ((long long)s.nkv * s.blocks * (s.row / 16) + PIECE - 1) / PIECE;
+        const long long most = (assign ? s.slots : (s.pages + 1) / 2) * pieces;
         const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>(most, 16384 / (2 * pl.n))), 2 * pl.n);
         if (small || l > 0) KLAUNCH((k_pages_carry<0>), grid, dim3(256), 0, st, s, p, pl, table, held);
         else if (assign) KLAUNCH((k_pages_carry<1>), grid, dim3(256), 0, st, s, p, pl, table, held);
