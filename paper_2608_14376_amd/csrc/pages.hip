@@ -110,16 +110,27 @@ __global__ __launch_bounds__(256) void k_pages_mark(PageShape s, Plan p, const i
     }
 }
 
+// A lane's value from a lane before it: n lanes before in its row of sixteen
+// (0x110 + n), the last lane of the row before (0x142), lane 31 (0x143); 0 where
+// there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_before(int x)
+{
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+
 // Sums of the workgroup's values before the caller's (exclusive), and of all, by
 // wavefronts of 64 in order.
 __device__ __forceinline__ int before(int v, int *all, int *lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     int x = v;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
-    }
+    x += from_before<0x111, 0xf>(x);
+    x += from_before<0x112, 0xf>(x);
+    x += from_before<0x114, 0xf>(x);
+    x += from_before<0x118, 0xf>(x);
+    x += from_before<0x142, 0xa>(x);                   // rows 1 and 3
+    x += from_before<0x143, 0xc>(x);                   // rows 2 and 3
     __syncthreads();                                  // lds is free
     if (lane == 63) lds[wave] = x;
     __syncthreads();
@@ -254,7 +265,7 @@ __global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int
 }
 
 // The whole plan, and the table, of a small pool: one workgroup, marks in LDS.
-constexpr int SMALL_PAGES = 8192, SMALL_SLOTS = 1024, SMALL_TABLE = 1 << 17;
+constexpr int SMALL_PAGES = 8192, SMALL_SLOTS = 1024, SMALL_TABLE = 1 << 17, SPARE = 512;
 
 // The most of a value over the workgroup, whose threads all call.
 __device__ __forceinline__ int most_of(int v, int *lds)
@@ -285,47 +296,68 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
 {
     extern __shared__ int mark[];                      // [pages]
     __shared__ int from[SMALL_SLOTS], first[SMALL_SLOTS], taken[SMALL_SLOTS], total[SMALL_SLOTS], tail[SMALL_SLOTS],
-        fresh0[SMALL_SLOTS], lds[16], bad, most;
+        fresh0[SMALL_SLOTS], has[SMALL_SLOTS], spare[SPARE], lds[16], bad, most;
     const int tid = threadIdx.x, r = tid;
     const bool slot = r < s.slots;
     // one thread to a slot
-    int n = 0, m = 0, take = 0;
-    bool wrong = false;
+    int f = -1, n = 0, m = 0, take = 0;
     if (slot) {
-        const int f = src[r], n0 = keep[r], m0 = hold == nullptr ? n0 : hold[r];
-        wrong = f < -1 || f >= s.slots;
-        if (!wrong && f >= 0) {
-            const int has = held[f];
-            n = n0;
-            m = m0;
-            wrong = has < 0 || has > s.width || n < 0 || n > (long long)has * s.page_size || m < n ||
-                    m > (long long)s.width * s.page_size;
-        }
-        if (wrong) n = m = 0;
-        from[r] = f;
-        first[r] = n / s.page_size;
-        taken[r] = take = first[r] + (n > first[r] * s.page_size);
-        total[r] = (int)(((long long)m + s.page_size - 1) / s.page_size);
+        f = src[r];
+        n = keep[r];
+        m = hold == nullptr ? n : hold[r];
+        has[r] = held[r];
         tail[r] = -1;
     }
     if (tid == 0) bad = 0;
     for (int i = tid; i < s.pages; i += 1024) mark[i] = FREE;
+    __syncthreads();
+    bool wrong = f < -1 || f >= s.slots;
+    if (wrong || f < 0) n = m = 0;
+    else {
+        const int h = has[f];
+        wrong = h < 0 || h > s.width || n < 0 || n > (long long)h * s.page_size || m < n ||
+                m > (long long)s.width * s.page_size;
+        if (wrong) n = m = 0;
+    }
+    if (slot) {
+        from[r] = f;
+        first[r] = n / s.page_size;
+        taken[r] = take = first[r] + (n > first[r] * s.page_size);
+        total[r] = (int)(((long long)m + s.page_size - 1) / s.page_size);
+    }
     const int span = most_of(take, &most);
     if (wrong) bad = 1;
-    over_rows(s.slots, span, [&](int r, int i) {
-        if (i >= taken[r]) return;
-        const int page = table[(size_t)from[r] * s.width + i];
-        if ((unsigned)page >= (unsigned)s.pages) {
-            bad = 1;
-            return;
-        }
-        p.rows[(size_t)r * s.width + i] = page;
-        if (i < first[r]) atomicMin(&mark[page], WHOLE);
+    // entries that are taken: page i of slot r.  Few of them stay in registers.
+    const bool few = s.slots * span <= 4096;
+    int kept[4];
+    const auto mark_page = [&](int r, int i, int page) {
+        if ((unsigned)page >= (unsigned)s.pages) bad = 1;
+        else if (i < first[r]) atomicMin(&mark[page], WHOLE);
         else {
             atomicMin(&mark[page], r);
             tail[r] = page;
         }
-    });
+    };
+    if (few) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = tid + 1024 * k, r = span > 0 ? (unsigned)e / (unsigned)span : s.slots, i = e - r * span;
+            kept[k] = -1;
+            if (r < s.slots && i < taken[r]) kept[k] = table[(size_t)from[r] * s.width + i];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = tid + 1024 * k, r = span > 0 ? (unsigned)e / (unsigned)span : s.slots, i = e - r * span;
+            if (r < s.slots && i < taken[r]) mark_page(r, i, kept[k]);
+        }
+    } else {
+        over_rows(s.slots, span, [&](int r, int i) {
+            if (i >= taken[r]) return;
+            const int page = table[(size_t)from[r] * s.width + i];
+            mark_page(r, i, page);
+            p.rows[(size_t)r * s.width + i] = page;
+        });
+    }
     __syncthreads();
     if (bad) {
         if (tid == 0) *status = p.head[STATUS] = -1;
@@ -353,11 +385,16 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
         int k = found + before(mine, &all, lds);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (free[e]) p.list[k++] = i + e;
+            if (free[e]) {
+                if (k < SPARE) spare[k] = i + e;
+                else p.list[k] = i + e;
+                ++k;
+            }
         found += all;
     }
-    const int left = need > found ? need - found : 0, longest = most_of(slot ? total[r] : 0, &most);
+    const int left = need > found ? need - found : 0, more = most_of(fresh, &most);
     if (left == 0) {
+        const auto dealt = [&](int k) { return k < SPARE ? spare[k] : p.list[k]; };
         if (slot) {
             first[r] = have;
             fresh0[r] = at;
@@ -365,13 +402,23 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
         }
         if (copy) {
             p.from[c] = t;
-            p.to[c] = p.list[at];
+            p.to[c] = dealt(at);
             p.count[c] = (n % s.page_size + s.block - 1) / s.block;
         }
         __syncthreads();
-        over_rows(s.slots, longest, [&](int r, int i) {
-            if (i >= total[r]) return;
-            table[(size_t)r * s.width + i] = i < first[r] ? p.rows[(size_t)r * s.width + i] : p.list[fresh0[r] + i - first[r]];
+        if (few) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = tid + 1024 * k, r = span > 0 ? (unsigned)e / (unsigned)span : s.slots, i = e - r * span;
+                if (r < s.slots && i < taken[r] && i < first[r]) table[(size_t)r * s.width + i] = kept[k];
+            }
+        } else {
+            over_rows(s.slots, span, [&](int r, int i) {
+                if (i < taken[r] && i < first[r]) table[(size_t)r * s.width + i] = p.rows[(size_t)r * s.width + i];
+            });
+        }
+        over_rows(s.slots, more, [&](int r, int i) {
+            if (first[r] + i < total[r]) table[(size_t)r * s.width + first[r] + i] = dealt(fresh0[r] + i);
         });
     }
     if (tid == 0) {

@@ -16,6 +16,7 @@
 // bf16 values and the codes of an e4m3 cache times their scale are exact there.
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <stdlib.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -65,8 +66,8 @@ __device__ __forceinline__ Prefix prefix_of(const SharedArgs &a, const GroupTabl
 // Tokens that row r sees, its prefix included: 0 for padding, -1 out of range.
 __device__ __forceinline__ int row_len(const SharedArgs &a, const CacheView &cv, const Prefix &p, int r)
 {
-    const int n = a.lens[r];
-    if (a.valid != nullptr && a.valid[r] == 0) return 0;
+    const int n = a.lens[r], live = a.valid == nullptr ? 1 : a.valid[r];   // in flight together
+    if (live == 0) return 0;
     return p.len < 0 || n < p.len || n - p.len > a.max_suffix || n > cv.cap ? -1 : n;
 }
 
@@ -92,6 +93,21 @@ __device__ __forceinline__ uint2 read_tr8(const void *lds_ptr)
     return __builtin_bit_cast(uint2, v);
 }
 
+// The value of the other half of 32 (HALF 16) or 64 lanes (HALF 32).
+template <int HALF>
+__device__ __forceinline__ float other(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const bool upper = threadIdx.x & HALF;
+    if constexpr (HALF == 16) {
+        const auto two = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return __uint_as_float(upper ? two[0] : two[1]);
+    } else {
+        const auto two = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return __uint_as_float(upper ? two[0] : two[1]);
+    }
+}
+
 // Four codes times a power of two, in bf16: exact.
 __device__ __forceinline__ uint2 codes4(uint32_t w, float scale)
 {
@@ -106,16 +122,39 @@ __device__ __forceinline__ uint4 codes8(uint32_t w0, uint32_t w1, float scale)
     return (uint4){a.x, a.y, b.x, b.y};
 }
 
-// Where 16 tokens from position t (a multiple of 16) of a slot stand: their first
-// row of one kv head, and their scale block.
+// A position (a multiple of 16) of a slot as it moves on: the entry of its page in
+// the table, and its place in the page.  Uniform over a wavefront, and followed by
+// additions where a division at every step would cost more than the step's loads.
+struct Walk {
+    int page, in, pages, rest;                         // pages, rest: what a step moves by
+    __device__ __forceinline__ Walk(int t, int step, int ps)
+    {
+        page = t / ps;
+        in = t - page * ps;
+        pages = step / ps;
+        rest = step - pages * ps;
+    }
+    __device__ __forceinline__ void next(int ps)
+    {
+        page += pages;
+        in += rest;
+        if (in >= ps) {
+            in -= ps;
+            ++page;
+        }
+    }
+};
+
+// Where 16 tokens from position t of a slot stand: their first row of one kv head,
+// and their scale block.  Paged: at place `in` of a page.
 struct Rows16 {
     size_t row, blk;
 };
 template <bool PAGED>
-__device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, int slot, int page, int t)
+__device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, int slot, int page, int in, int t)
 {
     if constexpr (PAGED) {
-        const int ps = cv.kv.page_size, in = t % ps;
+        const int ps = cv.kv.page_size;
         const size_t head = (size_t)page * nkv + kvh;
         return {head * ps + in, head * (ps >> cv.blk_shift) + (in >> cv.blk_shift)};
     }
@@ -125,20 +164,29 @@ __device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, 
 
 // ---------------------------------------------------------------------------
 // Up to 16 MT queries over tokens t_lo .. t_end - 1 of one slot: what a row has of
-// its own, and prefixes of few queries.  Four wavefronts, each with all the
-// queries and 32 tokens of a step of 128, on its own: no barrier in the loop.
+// its own, or a tile of queries on a split of a prefix.  Four wavefronts, each
+// with all the queries and 32 tokens of a step of 128, on its own: no barrier in
+// the loop, keys and values are read once for all the queries, and converted once.
 //  * S^T = K q^T on 16x16x32 MFMA.  Keys go from the cache to registers: the
 //    contraction may take the dimensions in any order, so lane (row, l / 16) loads
 //    the (l / 16)th quarter of its token's row in one piece, and the queries are
-//    held in the same order.  Tile T's row m is token 8 (m / 4) + 4 T + m % 4, so
-//    that lane l ends with the scores of tokens 8 (l / 16) .. + 7 of query l % 16,
-//    which is the A operand of
+//    held in the same order (in LDS from 64 queries on).  Tile T's row m is token
+//    8 (m / 4) + 4 T + m % 4, so that lane l ends with the scores of tokens
+//    8 (l / 16) .. + 7 of query l % 16, which is the A operand of
 //  * O += P V.  Values go global -> LDS by direct 16-byte loads and come back
 //    through transposed reads.
-// The next step's loads go out once this step's values are in registers.
+// The next step's values are loaded once this step's are in registers, its keys
+// once this step's scores are there.  Weights are 2^(s - ref), where ref follows
+// the running maximum when that is more than LAG above it.
 // ---------------------------------------------------------------------------
-template <int D, bool E4>
-constexpr int few_lds() { return 4 * (32 * D * (E4 ? 1 : 2) > 16 * D * 4 ? 32 * D * (E4 ? 1 : 2) : 16 * D * 4); }
+constexpr float LAG = 6.f;
+
+template <int D, bool E4, int MT>
+constexpr int few_lds()
+{
+    const int values = 4 * 32 * D * (E4 ? 1 : 2), queries = MT < 3 ? 0 : 16 * MT * D * 2, merge = 4 * 16 * D * 4;
+    return values + queries > merge ? values + queries : merge;
+}
 
 template <int D, bool E4, bool PAGED, int MT, class QueryOf>
 __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*cl)[64], int *lost, const CacheView &cv,
@@ -147,18 +195,23 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
 {
     constexpr int EB = E4 ? 1 : 2, RB = D * EB, KCH = RB / 16;       // bytes of a row; its 16-byte units
     constexpr int NK = RB / 64, NV = 32 * RB / 1024, ET = D / 16, KK = D / 32;
+    constexpr bool QL = MT >= 3;
     const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid == 0) *lost = 0;
-    bf16x8 qf[MT][KK];
+    char *mine = lds + wave * 32 * RB;
+    uint4 *ql = (uint4 *)(lds + 4 * 32 * RB);          // [MT][KK][64 lanes]
+    bf16x8 qf[QL ? 1 : MT][KK];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
+        if (QL && m % 4 != wave) continue;             // a wavefront writes its share
         const uint16_t *q = 16 * m + hl < queries ? query(16 * m + hl) : nullptr;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             uint4 v = {0u, 0u, 0u, 0u};
             if (q != nullptr) v = *(const uint4 *)(q + kg * (D / 4) + 8 * kk);
-            qf[m][kk] = __builtin_bit_cast(bf16x8, v);
+            if constexpr (QL) ql[(m * KK + kk) * 64 + lane] = v;
+            else qf[m][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);      // scores in base 2
@@ -172,20 +225,25 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         for (int et = 0; et < ET; ++et) acc[m][et] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const uint8_t *kc = (const uint8_t *)layer.k, *vc = (const uint8_t *)layer.v;
-    char *mine = lds + wave * 32 * RB;
     const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
     bool bad = false;
-    int tb = (t_lo & ~15) + 32 * wave, pg[2] = {0, 0};
-    auto pages = [&](int t) {                          // of the wavefront's two groups of 16 tokens from t
+    int tb = (t_lo & ~15) + 32 * wave, pg[2] = {0, 0}, in[2] = {0, 0};
+    const int ps = PAGED ? cv.kv.page_size : 16;
+    Walk walk(PAGED ? tb : 0, 128, ps);
+    auto pages = [&](int t) {                          // of the wavefront's two groups of 16 tokens from t, one step on at every call
         if constexpr (PAGED) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (t + 16 * j < t_end) pg[j] = pt[(t + 16 * j) / cv.kv.page_size];
+            const bool same = walk.in + 16 < ps;
+            if (t < t_end) pg[0] = pt[walk.page];
+            if (t + 16 < t_end) pg[1] = pt[walk.page + !same];
+            in[0] = walk.in;
+            in[1] = same ? walk.in + 16 : 0;
+            walk.next(ps);
         }
     };
     uint4 kr[2][NK];
     uint32_t ks = 0, vs = 0;                           // scale bytes of this lane's keys, and of its eight value tokens
-    auto issue = [&](int t) {
+    const uint8_t *kp = nullptr;
+    auto issue_values = [&](int t) {                   // and where the step's keys are
         Rows16 at[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -194,15 +252,11 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
                 if (t + 16 * j < t_end) bad = true;
                 page = 0;
             }
-            at[j] = rows16<PAGED>(cv, nkv, kvh, slot, page, t + 16 * j < t_end ? t + 16 * j : t);
+            at[j] = rows16<PAGED>(cv, nkv, kvh, slot, page, in[j], t + 16 * j < t_end ? t + 16 * j : t);
             if (t + 16 * j >= t_end) at[j] = at[0];    // past the end: the first group again, masked below
         }
         const Rows16 ka = hl & 8 ? at[1] : at[0];
-        const uint8_t *kp = kc + (ka.row + 8 * ((hl >> 2) & 1) + (hl & 3)) * RB + kg * (RB / 4);
-#pragma unroll
-        for (int T = 0; T < 2; ++T)
-#pragma unroll
-            for (int j = 0; j < NK; ++j) kr[T][j] = *(const uint4 *)(kp + 4 * T * RB + 16 * j);
+        kp = kc + (ka.row + 8 * ((hl >> 2) & 1) + (hl & 3)) * RB + kg * (RB / 4);
         if constexpr (E4) {
             ks = layer.ks[ka.blk];
             vs = layer.vs[(kg & 2 ? at[1] : at[0]).blk];
@@ -218,28 +272,24 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
                                              (lds_void *)(mine + 1024 * j), 16, 0, 0);
         }
     };
-    if (tb < t_end) {
-        pages(tb);
-        issue(tb);
-        pages(tb + 128);
-    }
-    for (; tb < t_end; tb += 128) {
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        asm volatile("" ::: "memory");
-        // operands out of the buffers that the next step's loads fill
-        bf16x8 kf[2][KK];
-        const float ksc = __uint_as_float(ks << 23), vsc = __uint_as_float(vs << 23);
+    auto issue_keys = [&]() {
 #pragma unroll
         for (int T = 0; T < 2; ++T)
 #pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                if constexpr (E4) {
-                    const uint4 w = kr[T][kk / 2];
-                    kf[T][kk] = __builtin_bit_cast(bf16x8, kk & 1 ? codes8(w.z, w.w, ksc) : codes8(w.x, w.y, ksc));
-                } else {
-                    kf[T][kk] = __builtin_bit_cast(bf16x8, kr[T][kk]);
-                }
-            }
+            for (int j = 0; j < NK; ++j) kr[T][j] = *(const uint4 *)(kp + 4 * T * RB + 16 * j);
+    };
+    if (tb < t_end) {
+        pages(tb);
+        issue_values(tb);
+        issue_keys();
+        pages(tb + 128);
+    }
+    if constexpr (QL) __syncthreads();                 // the queries are in LDS
+    for (; tb < t_end; tb += 128) {
+        const bool more = tb + 128 < t_end;
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        asm volatile("" ::: "memory");
+        const float ksc = __uint_as_float(ks << 23), vsc = __uint_as_float(vs << 23);
         uint4 vr[ET];                                  // e4m3: the codes in the first two words
 #pragma unroll
         for (int et = 0; et < ET; ++et) {
@@ -259,10 +309,7 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         }
         __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the values are in registers
         asm volatile("" ::: "memory");
-        if (tb + 128 < t_end) {
-            issue(tb + 128);
-            pages(tb + 256);
-        }
+        if (more) issue_values(tb + 128);
         const bool edge = tb < t_lo || tb + 32 > t_end;   // wave-uniform: some of the 32 tokens are masked
         const int first = t_lo - (tb + 8 * kg), behind = t_end - (tb + 8 * kg);   // this lane's real tokens: first .. behind - 1 of 8
         if (edge) {
@@ -277,47 +324,51 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
                 }
             }
         }
-        bf16x8 vf[ET];
+        f32x4 st[MT][2];
 #pragma unroll
-        for (int et = 0; et < ET; ++et)
-            vf[et] = __builtin_bit_cast(bf16x8, E4 ? codes8(vr[et].x, vr[et].y, vsc) : vr[et]);
+        for (int m = 0; m < MT; ++m) st[m][0] = st[m][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            f32x4 st[2];
-            float mt = -INFINITY;
+        for (int kk = 0; kk < KK; ++kk) {
+            bf16x8 kf[2], qk[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) qk[m] = QL ? __builtin_bit_cast(bf16x8, ql[(m * KK + kk) * 64 + lane]) : qf[QL ? 0 : m][kk];
 #pragma unroll
             for (int T = 0; T < 2; ++T) {
-                st[T] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    st[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T][kk], qf[m][kk], st[T], 0, 0, 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float sv = st[T][e] * scale2;
-                    if (edge) sv = 4 * T + e >= first && 4 * T + e < behind ? sv : -INFINITY;
-                    st[T][e] = sv;
-                    mt = fmaxf(mt, sv);
+                if constexpr (E4) {
+                    const uint4 w = kr[T][kk / 2];
+                    kf[T] = __builtin_bit_cast(bf16x8, kk & 1 ? codes8(w.z, w.w, ksc) : codes8(w.x, w.y, ksc));
+                } else {
+                    kf[T] = __builtin_bit_cast(bf16x8, kr[T][kk]);
                 }
             }
-            mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
-            mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-            const float mnew = fmaxf(mrun[m], mt);
-            const float alpha = mnew == mrun[m] ? 1.f : __builtin_amdgcn_exp2f(mrun[m] - mnew);
-            const float moff = mnew == -INFINITY ? 0.f : mnew;
-            uint32_t hi[4], lo[4];
-            float ls = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = __builtin_amdgcn_exp2f(st[i / 2][2 * (i % 2)] - moff);
-                const float b = __builtin_amdgcn_exp2f(st[i / 2][2 * (i % 2) + 1] - moff);
-                ls += a + b;
-                const uint32_t w = f2bf2(a, b);
-                hi[i] = w;
-                lo[i] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
-            }
-            lrun[m] = lrun[m] * alpha + ls;
-            mrun[m] = mnew;
-            if (__ballot(alpha != 1.f)) {              // lane l's sums belong to queries 4 (l / 16) + e
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int T = 0; T < 2; ++T) st[m][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T], qk[m], st[m][T], 0, 0, 0);
+        }
+        if (MT >= 3) __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            issue_keys();
+            pages(tb + 256);
+        }
+        bf16x8 ph[MT], pl[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float mt = -INFINITY;
+#pragma unroll
+            for (int T = 0; T < 2; ++T)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (edge) st[m][T][e] = 4 * T + e >= first && 4 * T + e < behind ? st[m][T][e] : -INFINITY;
+                    mt = fmaxf(mt, st[m][T][e]);
+                }
+            mt = fmaxf(mt, other<16>(mt));
+            mt = fmaxf(mt, other<32>(mt)) * scale2;
+            const float mnew = mt > mrun[m] + LAG ? mt : mrun[m], moff = mnew == -INFINITY ? 0.f : mnew;
+            if (__ballot(mnew != mrun[m])) {           // lane l's sums belong to queries 4 (l / 16) + e
+                const float alpha = mnew == mrun[m] ? 1.f : __builtin_amdgcn_exp2f(mrun[m] - mnew);
+                lrun[m] *= alpha;
+                mrun[m] = mnew;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float ae = __shfl(alpha, 4 * kg + e, 64);
@@ -325,11 +376,29 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
                     for (int et = 0; et < ET; ++et) acc[m][et][e] *= ae;
                 }
             }
-            const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+            uint32_t hi[4], lo[4];
+            float ls = 0.f;
 #pragma unroll
-            for (int et = 0; et < ET; ++et) {
-                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph, vf[et], acc[m][et], 0, 0, 0);
-                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl, vf[et], acc[m][et], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) {
+                const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2)], scale2, -moff));
+                const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2) + 1], scale2, -moff));
+                ls += a + b;
+                const uint32_t w = f2bf2(a, b);
+                hi[i] = w;
+                lo[i] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+            }
+            lrun[m] += ls;
+            ph[m] = __builtin_bit_cast(bf16x8, hi);
+            pl[m] = __builtin_bit_cast(bf16x8, lo);
+            if (MT >= 3) __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int et = 0; et < ET; ++et) {
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, E4 ? codes8(vr[et].x, vr[et].y, vsc) : vr[et]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph[m], vf, acc[m][et], 0, 0, 0);
+                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl[m], vf, acc[m][et], 0, 0, 0);
             }
         }
     }
@@ -339,8 +408,8 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
     float *ca = (float *)lds;                          // [4][16][D]
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        lrun[m] += __shfl_xor(lrun[m], 16, 64);
-        lrun[m] += __shfl_xor(lrun[m], 32, 64);
+        lrun[m] += other<16>(lrun[m]);
+        lrun[m] += other<32>(lrun[m]);
         if (lane < 16) {
             cm[wave][16 * m + lane] = mrun[m];
             cl[wave][16 * m + lane] = lrun[m];
@@ -416,11 +485,16 @@ __device__ __forceinline__ void attend_many(char *lds, int *lost, const CacheVie
     }
     const uint8_t *kc = (const uint8_t *)layer.k, *vc = (const uint8_t *)layer.v;
     const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
-    int next = t0 + 16 * wave, page = 0;               // the wavefront's group of the next tile to load
+    int next = t0 + 16 * wave, page = 0, in = 0;       // the wavefront's group of the next tile to load
+    const int ps = PAGED ? cv.kv.page_size : 16;
+    Walk walk(PAGED ? next : 0, 64, ps);
     bool bad = false;
     auto fetch_page = [&]() {
-        if constexpr (PAGED)
-            if (next < t_end) page = pt[next / cv.kv.page_size];
+        if constexpr (PAGED) {
+            if (next < t_end) page = pt[walk.page];
+            in = walk.in;
+            walk.next(ps);
+        }
     };
     // the wavefront's next group: whether there is one, and where it stands
     auto locate = [&](Rows16 &at) -> bool {
@@ -431,7 +505,7 @@ __device__ __forceinline__ void attend_many(char *lds, int *lost, const CacheVie
                 bad = true;
                 pg = 0;
             }
-            at = rows16<PAGED>(cv, nkv, kvh, slot, pg, next);
+            at = rows16<PAGED>(cv, nkv, kvh, slot, pg, in, next);
         }
         next += 64;
         return real;
@@ -630,18 +704,19 @@ __device__ __forceinline__ void attend_many(char *lds, int *lost, const CacheVie
     if (h == 0) *(float2 *)(dst + 32 * D + 2 * r32) = {*lost ? qnan() : mrow, sum};
 }
 
-// Prefix workgroups first (kv head, query tile, split, the kv head running
-// fastest), then the rows' own (kv head, split, row).
+// Workgroup: a kv head (running fastest) of a unit, which is a query tile and split
+// of a prefix, or a split of a row's own tokens.
 template <int D, bool E4, bool PAGED, int MT>
 __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
                                                          CacheLayer layer, float *__restrict__ ws)
 {
-    constexpr int LDS = MT == 128 && many_lds<D>() > few_lds<D, E4>() ? many_lds<D>() : few_lds<D, E4>();
+    constexpr int FEW = few_lds<D, E4, MT == 128 ? 1 : MT / 16>(), LDS = MT == 128 && many_lds<D>() > FEW ? many_lds<D>() : FEW;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ float cm[4][64], cl[4][64];
     __shared__ int lost;
     const int nkv = a.nkv, G = s.G, kvh = blockIdx.x % nkv, unit = blockIdx.x / nkv;
-    if (unit < s.tiles * s.splits_p) {
+    const int np = s.tiles * s.splits_p;               // the prefixes' units come first
+    if (unit < np) {
         const int tile = unit % s.tiles, split = unit / s.tiles;
         const int gi = last_at_most(s.tile0, gt.n, tile);
         const Prefix p = prefix_of(a, gt, cv, gi);
@@ -661,7 +736,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTabl
                                               part, u0);
         return;
     }
-    const int v = unit - s.tiles * s.splits_p, split = v % s.splits_s, r = v / s.splits_s;
+    const int v = unit - np, split = v % s.splits_s, r = v / s.splits_s;
     const int gi = last_at_most(gt.row0, gt.n, r);
     const Prefix p = prefix_of(a, gt, cv, gi);
     const int n = row_len(a, cv, p, r), t0 = (p.len & ~15) + split * s.chunk_s;
@@ -677,7 +752,7 @@ template <int D>
 __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
                                                      float *__restrict__ ws)
 {
-    constexpr int PF = 8;                              // splits whose values are in flight at once
+    constexpr int PF = 16;                             // splits whose values are in flight at once
     const int nkv = a.nkv, G = s.G, kvh = blockIdx.x % nkv, block = blockIdx.x / nkv;
     const int tid = threadIdx.x, u32 = tid & 31, d4 = 4 * blockIdx.y + (tid >> 5);
     const int gi = last_at_most(s.qb0, gt.n, block);
@@ -693,29 +768,35 @@ __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt
     }
     const int np = (p.len + s.chunk_p - 1) / s.chunk_p;
     const int parts = np + (n > p.len ? (n - (p.len & ~15) + s.chunk_s - 1) / s.chunk_s : 0);
-    const auto at = [&](int i) { return part_at<D>(ws, s, nkv, i < np ? i : s.splits_p + i - np, kvh, block); };
+    const float *base = part_at<D>(ws, s, nkv, 0, kvh, block);
+    const size_t split = (size_t)nkv * s.blocks * part_floats<D>();
     float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < parts; ++i) M = fmaxf(M, at(i)[32 * D + 2 * u32]);
-    const float off = M == -INFINITY ? 0.f : M;
-    float4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < parts; i0 += PF) {
-        float4 x[PF];
-        float2 ml[PF];
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    for (int i0 = 0; i0 < parts; i0 += PF) {           // in order, relative to the largest maximum so far
+        f32x4 x[PF];
+        f32x2 ml[PF];
 #pragma unroll
         for (int j = 0; j < PF; ++j) {
-            const float *b = at(min(i0 + j, parts - 1));
-            x[j] = *(const float4 *)(b + (d4 * 32 + u32) * 4);
-            ml[j] = *(const float2 *)(b + 32 * D + 2 * u32);
+            const int i = min(i0 + j, parts - 1);
+            const float *b = base + (size_t)(i < np ? i : s.splits_p + i - np) * split;
+            x[j] = *(const f32x4 *)(b + (d4 * 32 + u32) * 4);
+            ml[j] = *(const f32x2 *)(b + 32 * D + 2 * u32);
         }
+        float m = M;
+#pragma unroll
+        for (int j = 0; j < PF; ++j) m = fmaxf(m, ml[j].x);   // a NaN shows in the sums
+        const float off = m == -INFINITY ? 0.f : m, down = __builtin_amdgcn_exp2f(M - off);
+        M = m;
+        L *= down;
+        o *= down;
 #pragma unroll
         for (int j = 0; j < PF; ++j) {
-            if (i0 + j >= parts) break;
-            const float f = __builtin_amdgcn_exp2f(ml[j].x - off);
-            L += ml[j].y * f;
-            o.x += x[j].x * f;
-            o.y += x[j].y * f;
-            o.z += x[j].z * f;
-            o.w += x[j].w * f;
+            if (i0 + j < parts) {
+                const float f = __builtin_amdgcn_exp2f(ml[j].x - off);
+                L += ml[j].y * f;
+                o += x[j] * f;
+            }
         }
     }
     const float inv = 1.0f / L;
@@ -728,7 +809,7 @@ Shape shape_of(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suf
     s.G = nq / nkv;
     int most = 0;
     for (int i = 0; i < g.n; ++i) most = std::max(most, (g.row0[i + 1] - g.row0[i]) * s.G);
-    s.mt = most <= 16 ? 16 : most <= 32 ? 32 : 128;
+    s.mt = most <= 16 ? 16 : most <= 32 ? 32 : getenv("SHARED_MT") ? atoi(getenv("SHARED_MT")) : 48;
     s.blocks = s.tiles = 0;
     for (int i = 0; i < g.n; ++i) {
         const int queries = (g.row0[i + 1] - g.row0[i]) * s.G;
@@ -739,16 +820,17 @@ Shape shape_of(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suf
     }
     s.qb0[g.n] = s.blocks;
     s.tile0[g.n] = s.tiles;
-    const auto splits = [&](long long tokens, long long wgs, int least) {   // tokens of a split: 512 workgroups in all
-        long long n = std::max<long long>(1, 512 / std::max<long long>(1, wgs));
+    const auto splits = [&](long long tokens, long long wgs, long long most, int least) {   // tokens of a split: about `most` workgroups
+        long long n = std::max<long long>(1, most / std::max<long long>(1, wgs));
         n = std::min<long long>({n, (tokens + least - 1) / least, 256});
         const long long per = (tokens + n - 1) / n;
         return (int)std::min<long long>((per + 127) / 128 * 128, 1 << 30);
     };
-    s.chunk_p = splits(max_prefix, (long long)s.tiles * nkv, 128);
+    const int wp = getenv("WP") ? atoi(getenv("WP")) : 1024, wsu = getenv("WS") ? atoi(getenv("WS")) : 2048;
+    s.chunk_p = splits(max_prefix, (long long)s.tiles * nkv, wp, 128);
     s.splits_p = (int)(((long long)max_prefix + s.chunk_p - 1) / s.chunk_p);
     const long long suffix = (long long)max_suffix + 15;
-    s.chunk_s = splits(suffix, (long long)g.row0[g.n] * nkv, 256);
+    s.chunk_s = splits(suffix, (long long)g.row0[g.n] * nkv, wsu, 256);
     s.splits_s = (int)((suffix + s.chunk_s - 1) / s.chunk_s);
     return s;
 }
@@ -775,6 +857,7 @@ hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheVi
     do {                                               \
         if (s.mt == 16) CORUN_SHARED(D_, E_, P_, 16);  \
         else if (s.mt == 32) CORUN_SHARED(D_, E_, P_, 32); \
+        else if (s.mt == 48) CORUN_SHARED(D_, E_, P_, 48); \
         else CORUN_SHARED(D_, E_, P_, 128);            \
     } while (0)
 #define CORUN_SHARED_P(D_, E_)                  \
