@@ -658,7 +658,7 @@ def shared_attention(cache, layer, q, group_rows, lens, prefix_lens, out, ws, pr
     overlap.  Does not wait."""
     rows, nq, ldq, ldo = _attention_rows(cache, q, out)
     gr = _np(group_rows, np.int32)
-    if gr.ndim != 1 or int(gr.sum(dtype=np.int64)) != rows:
+    if gr.ndim != 1 or sum(gr.tolist()) != rows:
         raise ValueError(f"group_rows: rows of each group, {rows} in all")
     ln = _vec(cache, lens, _torch.ints, rows, "lens")
     pl = _vec(cache, prefix_lens, _torch.ints, gr.size, "prefix_lens")

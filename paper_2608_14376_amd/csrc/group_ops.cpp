@@ -158,18 +158,18 @@ corun_status shared_call(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads
 {
     TRY(check_heads(kv, n_heads, n_kv_heads, head_dim));
     if (!group_rows) return set_error(CORUN_E_INVAL, "null group_rows");
-    static_assert(CORUN_MAX_GROUPS + 1 == sizeof(GroupTable::row0) / sizeof(int), "a call's groups fit the table");
+    static_assert(CORUN_MAX_GROUPS == MOST_GROUPS, "a call's groups fit the table");
     if (n_groups < 1 || n_groups > CORUN_MAX_GROUPS)
         return set_errorf(CORUN_E_INVAL, "n_groups %d outside [1, %d]", n_groups, CORUN_MAX_GROUPS);
     g->n = n_groups;
     long long rows = 0;
     for (int i = 0; i < n_groups; ++i) {
         if (group_rows[i] < 1) return set_errorf(CORUN_E_INVAL, "group_rows[%d] = %d", i, group_rows[i]);
-        g->row0[i] = (int)rows;
+        g->row0[i] = (uint16_t)rows;
         rows += group_rows[i];
         if (rows > 65535) return set_error(CORUN_E_SHAPE, "more than 65535 rows");
     }
-    g->row0[n_groups] = (int)rows;
+    g->row0[n_groups] = (uint16_t)rows;
     if (rows > kv->n_slots)
         return set_errorf(CORUN_E_CAPACITY, "KV cache has %d slots < %lld rows", kv->n_slots, rows);
     const int cap = cache_view(kv).cap;
@@ -189,7 +189,7 @@ extern "C" int64_t corun_shared_attention_workspace(const corun_kv *kv, int32_t 
     GroupTable g;
     int most[2];
     TRY(shared_call(kv, n_heads, n_kv_heads, head_dim, n_groups, group_rows, max_prefix, max_suffix, &g, most));
-    return (int64_t)shared_ws(g, n_heads, n_kv_heads, head_dim, most[0], most[1]);
+    return (int64_t)shared_ws(shared_shape(g, n_heads, n_kv_heads, most[0], most[1]), n_kv_heads, head_dim);
 }
 
 extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
@@ -207,7 +207,6 @@ extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * head_dim));
     TRY(check_rows("out", out, ld_out, (int64_t)n_heads * head_dim));
     if (!lens || !prefix_lens) return set_error(CORUN_E_INVAL, "null argument");
-    TRY(check_ws(ws, ws_bytes, (int64_t)shared_ws(g, n_heads, n_kv_heads, head_dim, most[0], most[1])));
     SharedArgs a;
     a.q = (const uint16_t *)q;
     a.ldq = ld_q;
@@ -222,5 +221,7 @@ extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer
     a.d = head_dim;
     a.max_prefix = most[0];
     a.max_suffix = most[1];
-    return launched(launch_shared(a, g, cache_view(kv), cl, (float *)ws, (hipStream_t)stream));
+    const SharedShape shape = shared_shape(g, n_heads, n_kv_heads, most[0], most[1]);
+    TRY(check_ws(ws, ws_bytes, (int64_t)shared_ws(shape, n_kv_heads, head_dim)));
+    return launched(launch_shared(a, g, shape, cache_view(kv), cl, (float *)ws, (hipStream_t)stream));
 }

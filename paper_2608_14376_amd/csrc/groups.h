@@ -45,11 +45,12 @@ hipError_t launch_pages(const PageShape &s, int32_t *table, int32_t *held, const
                         const int32_t *hold, int32_t *status, int n_layers, LayersOf layers, const void *of, void *ws,
                         hipStream_t st);
 
-// Groups of rows, by value: group g owns rows row0[g] .. row0[g + 1] - 1.
+// Groups of rows, by value: group g owns rows row0[g] .. row0[g + 1] - 1, of at
+// most 65535.
 constexpr int MOST_GROUPS = 256;
 struct GroupTable {
     int n;
-    int row0[MOST_GROUPS + 1];
+    uint16_t row0[MOST_GROUPS + 1];
 };
 struct SharedArgs {
     const uint16_t *q;
@@ -60,8 +61,18 @@ struct SharedArgs {
     const int32_t *lens, *prefix_slots, *prefix_lens;
     int nq, nkv, d, max_prefix, max_suffix;
 };
-size_t shared_ws(const GroupTable &g, int nq, int nkv, int d, int max_prefix, int max_suffix);
-hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheView &cv, const CacheLayer &cl, float *ws,
-                         hipStream_t st);
+// A call's launch: where each group's 32-query blocks (of one kv head) and query
+// tiles start, and the splits; by value.
+struct SharedShape {
+    int G, mt;                                         // query heads to a kv head; queries of a prefix tile
+    int blocks;                                        // 32-query blocks of a kv head, all groups
+    int chunk_p, splits_p, chunk_s, splits_s;          // tokens of a split, splits
+    int tiles;                                         // query tiles of all groups
+    uint16_t qb0[MOST_GROUPS + 1], tile0[MOST_GROUPS + 1];
+};
+SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix);
+size_t shared_ws(const SharedShape &s, int nkv, int d);
+hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const SharedShape &s, const CacheView &cv,
+                         const CacheLayer &cl, float *ws, hipStream_t st);
 
 }  // namespace corun

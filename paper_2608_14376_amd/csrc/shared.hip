@@ -16,7 +16,6 @@
 // bf16 values and the codes of an e4m3 cache times their scale are exact there.
 #include <hip/hip_runtime.h>
 #include <math.h>
-#include <stdlib.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -33,7 +32,7 @@ __device__ __forceinline__ float qnan() { return __uint_as_float(0x7fc00000u); }
 
 // The last of n entries of a rising table that is at most u: a load and a count
 // for 64 entries, where a search would wait for one after another.
-__device__ __forceinline__ int last_at_most(const int *t, int n, int u)
+__device__ __forceinline__ int last_at_most(const uint16_t *t, int n, int u)
 {
     const int lane = threadIdx.x & 63;
     int count = 0;
@@ -43,15 +42,7 @@ __device__ __forceinline__ int last_at_most(const int *t, int n, int u)
     return __builtin_amdgcn_readfirstlane(count - 1);
 }
 
-// A call's launch: where each group's 32-query blocks (of one kv head) and query
-// tiles start, and the splits.
-struct Shape {
-    int G, mt;                                         // query heads to a kv head; queries of a prefix tile
-    int blocks;                                        // 32-query blocks of a kv head, all groups
-    int chunk_p, splits_p, chunk_s, splits_s;          // tokens of a split, splits
-    int tiles;                                         // query tiles of all groups
-    int qb0[MOST_GROUPS + 1], tile0[MOST_GROUPS + 1];
-};
+using Shape = SharedShape;
 
 // A group's prefix.  len < 0: out of the launch's range.
 struct Prefix {
@@ -170,7 +161,7 @@ __device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, 
 //  * S^T = K q^T on 16x16x32 MFMA.  Keys go from the cache to registers: the
 //    contraction may take the dimensions in any order, so lane (row, l / 16) loads
 //    the (l / 16)th quarter of its token's row in one piece, and the queries are
-//    held in the same order (in LDS from 64 queries on).  Tile T's row m is token
+//    held in the same order.  Tile T's row m is token
 //    8 (m / 4) + 4 T + m % 4, so that lane l ends with the scores of tokens
 //    8 (l / 16) .. + 7 of query l % 16, which is the A operand of
 //  * O += P V.  Values go global -> LDS by direct 16-byte loads and come back
@@ -181,12 +172,8 @@ __device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, 
 // ---------------------------------------------------------------------------
 constexpr float LAG = 6.f;
 
-template <int D, bool E4, int MT>
-constexpr int few_lds()
-{
-    const int values = 4 * 32 * D * (E4 ? 1 : 2), queries = MT < 3 ? 0 : 16 * MT * D * 2, merge = 4 * 16 * D * 4;
-    return values + queries > merge ? values + queries : merge;
-}
+template <int D, bool E4>
+constexpr int few_lds() { return 4 * (32 * D * (E4 ? 1 : 2) > 16 * D * 4 ? 32 * D * (E4 ? 1 : 2) : 16 * D * 4); }
 
 template <int D, bool E4, bool PAGED, int MT, class QueryOf>
 __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*cl)[64], int *lost, const CacheView &cv,
@@ -195,23 +182,19 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
 {
     constexpr int EB = E4 ? 1 : 2, RB = D * EB, KCH = RB / 16;       // bytes of a row; its 16-byte units
     constexpr int NK = RB / 64, NV = 32 * RB / 1024, ET = D / 16, KK = D / 32;
-    constexpr bool QL = MT >= 3;
     const int tid = threadIdx.x, lane = tid & 63, hl = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (tid == 0) *lost = 0;
     char *mine = lds + wave * 32 * RB;
-    uint4 *ql = (uint4 *)(lds + 4 * 32 * RB);          // [MT][KK][64 lanes]
-    bf16x8 qf[QL ? 1 : MT][KK];
+    bf16x8 qf[MT][KK];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        if (QL && m % 4 != wave) continue;             // a wavefront writes its share
         const uint16_t *q = 16 * m + hl < queries ? query(16 * m + hl) : nullptr;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             uint4 v = {0u, 0u, 0u, 0u};
             if (q != nullptr) v = *(const uint4 *)(q + kg * (D / 4) + 8 * kk);
-            if constexpr (QL) ql[(m * KK + kk) * 64 + lane] = v;
-            else qf[m][kk] = __builtin_bit_cast(bf16x8, v);
+            qf[m][kk] = __builtin_bit_cast(bf16x8, v);
         }
     }
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);      // scores in base 2
@@ -284,7 +267,6 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         issue_keys();
         pages(tb + 128);
     }
-    if constexpr (QL) __syncthreads();                 // the queries are in LDS
     for (; tb < t_end; tb += 128) {
         const bool more = tb + 128 < t_end;
         __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -329,9 +311,7 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         for (int m = 0; m < MT; ++m) st[m][0] = st[m][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            bf16x8 kf[2], qk[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) qk[m] = QL ? __builtin_bit_cast(bf16x8, ql[(m * KK + kk) * 64 + lane]) : qf[QL ? 0 : m][kk];
+            bf16x8 kf[2];
 #pragma unroll
             for (int T = 0; T < 2; ++T) {
                 if constexpr (E4) {
@@ -344,9 +324,8 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int T = 0; T < 2; ++T) st[m][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T], qk[m], st[m][T], 0, 0, 0);
+                for (int T = 0; T < 2; ++T) st[m][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T], qf[m][kk], st[m][T], 0, 0, 0);
         }
-        if (MT >= 3) __builtin_amdgcn_sched_barrier(0);
         if (more) {
             issue_keys();
             pages(tb + 256);
@@ -390,7 +369,6 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
             lrun[m] += ls;
             ph[m] = __builtin_bit_cast(bf16x8, hi);
             pl[m] = __builtin_bit_cast(bf16x8, lo);
-            if (MT >= 3) __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int et = 0; et < ET; ++et) {
@@ -710,7 +688,7 @@ template <int D, bool E4, bool PAGED, int MT>
 __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
                                                          CacheLayer layer, float *__restrict__ ws)
 {
-    constexpr int FEW = few_lds<D, E4, MT == 128 ? 1 : MT / 16>(), LDS = MT == 128 && many_lds<D>() > FEW ? many_lds<D>() : FEW;
+    constexpr int FEW = few_lds<D, E4>(), LDS = MT == 128 && many_lds<D>() > FEW ? many_lds<D>() : FEW;
     __shared__ __attribute__((aligned(16))) char lds[LDS];
     __shared__ float cm[4][64], cl[4][64];
     __shared__ int lost;
@@ -803,51 +781,55 @@ __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt
     *(uint2 *)out = {f2bf2(o.x * inv, o.y * inv), f2bf2(o.z * inv, o.w * inv)};
 }
 
-Shape shape_of(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix)
+}  // namespace
+
+SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix)
 {
-    Shape s;
+    SharedShape s;
     s.G = nq / nkv;
     int most = 0;
     for (int i = 0; i < g.n; ++i) most = std::max(most, (g.row0[i + 1] - g.row0[i]) * s.G);
-    s.mt = most <= 16 ? 16 : most <= 32 ? 32 : getenv("SHARED_MT") ? atoi(getenv("SHARED_MT")) : 48;
+    s.mt = most <= 16 ? 16 : most <= 32 ? 32 : 128;
     s.blocks = s.tiles = 0;
     for (int i = 0; i < g.n; ++i) {
         const int queries = (g.row0[i + 1] - g.row0[i]) * s.G;
-        s.qb0[i] = s.blocks;
-        s.tile0[i] = s.tiles;
+        s.qb0[i] = (uint16_t)s.blocks;
+        s.tile0[i] = (uint16_t)s.tiles;
         s.blocks += (queries + 31) / 32;
         s.tiles += (queries + s.mt - 1) / s.mt;
     }
-    s.qb0[g.n] = s.blocks;
-    s.tile0[g.n] = s.tiles;
-    const auto splits = [&](long long tokens, long long wgs, long long most, int least) {   // tokens of a split: about `most` workgroups
-        long long n = std::max<long long>(1, most / std::max<long long>(1, wgs));
-        n = std::min<long long>({n, (tokens + least - 1) / least, 256});
+    s.qb0[g.n] = (uint16_t)s.blocks;
+    s.tile0[g.n] = (uint16_t)s.tiles;   // rows bound all of them
+    // Tokens of a split: about `wgs` workgroups in all, splits of at least 256 tokens
+    // and of at most `longest`, 256 splits at most.
+    const auto chunk = [](long long tokens, long long units, long long wgs, long long longest) {
+        long long n = std::max<long long>(1, wgs / std::max<long long>(1, units));
+        n = std::min<long long>(std::max(std::min(n, (tokens + 255) / 256), (tokens + longest - 1) / longest), 256);
         const long long per = (tokens + n - 1) / n;
         return (int)std::min<long long>((per + 127) / 128 * 128, 1 << 30);
     };
-    const int wp = getenv("WP") ? atoi(getenv("WP")) : 1024, wsu = getenv("WS") ? atoi(getenv("WS")) : 2048;
-    s.chunk_p = splits(max_prefix, (long long)s.tiles * nkv, wp, 128);
+    // One group: a workgroup to each CU (8000 tokens in bf16 for 128 rows of 8 kv heads
+    // and 32: 53 us, 59 with 512 workgroups, 81 with 128; 64 rows 35, 40, 47).  Of
+    // several, some may be shorter than the longest, and workgroups of many tokens then
+    // end late (four of 11 to 30 thousand tokens: 159 us with splits of 1664, 238 of
+    // 7424; eight of 500 to 8000: 60 of 1024, 71 of 2048).
+    s.chunk_p = chunk(max_prefix, (long long)s.tiles * nkv, 256, g.n == 1 ? 1 << 30 : std::max(1024, max_prefix / 16));
     s.splits_p = (int)(((long long)max_prefix + s.chunk_p - 1) / s.chunk_p);
     const long long suffix = (long long)max_suffix + 15;
-    s.chunk_s = splits(suffix, (long long)g.row0[g.n] * nkv, wsu, 256);
+    s.chunk_s = chunk(suffix, (long long)g.row0[g.n] * nkv, 2048, 1 << 30);
     s.splits_s = (int)((suffix + s.chunk_s - 1) / s.chunk_s);
     return s;
 }
 
-}  // namespace
-
-size_t shared_ws(const GroupTable &g, int nq, int nkv, int d, int max_prefix, int max_suffix)
+size_t shared_ws(const SharedShape &s, int nkv, int d)
 {
-    const Shape s = shape_of(g, nq, nkv, max_prefix, max_suffix);
     return (size_t)(s.splits_p + s.splits_s) * nkv * s.blocks * (d == 128 ? part_floats<128>() : part_floats<64>()) *
            sizeof(float);
 }
 
-hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheView &cv, const CacheLayer &cl, float *ws,
-                         hipStream_t st)
+hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const SharedShape &s, const CacheView &cv,
+                         const CacheLayer &cl, float *ws, hipStream_t st)
 {
-    const Shape s = shape_of(g, a.nq, a.nkv, a.max_prefix, a.max_suffix);
     const long long wgs = ((long long)s.tiles * s.splits_p + (long long)g.row0[g.n] * s.splits_s) * a.nkv;
     if (wgs > (1 << 24) - 1) return hipErrorInvalidValue;
     const bool paged = cv.kv.layout == 1;
@@ -857,7 +839,6 @@ hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const CacheVi
     do {                                               \
         if (s.mt == 16) CORUN_SHARED(D_, E_, P_, 16);  \
         else if (s.mt == 32) CORUN_SHARED(D_, E_, P_, 32); \
-        else if (s.mt == 48) CORUN_SHARED(D_, E_, P_, 48); \
         else CORUN_SHARED(D_, E_, P_, 128);            \
     } while (0)
 #define CORUN_SHARED_P(D_, E_)                  \
