@@ -513,7 +513,8 @@ int64_t corun_pages_workspace(const corun_kv *kv);
  * slot r: out = softmax(q k / sqrt(head_dim)) v over all of them, sums in fp32.
  * A prefix of 0 tokens leaves the attention of an ordinary decode step.
  *  group_rows  host int32 [n_groups], each >= 1; their sum, the rows, at most
- *              n_slots
+ *              n_slots and 65535 (CORUN_E_SHAPE also where rows, kv heads and
+ *              splits make more than 2^24 - 1 workgroups)
  *  valid       uint8 [rows], or NULL: all rows are live
  *  lens        int32 [rows], the prefix included
  *  prefix_slots  int32 [n_groups], or NULL: the slot of each group's first row

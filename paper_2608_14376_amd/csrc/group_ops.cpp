@@ -152,9 +152,10 @@ extern "C" corun_status corun_pages_compact(const corun_kv *kv, int32_t n_layers
 
 namespace {
 
-// The call's groups and, in `most`, the longest prefix and suffix that it covers.
+// The call's groups, the longest prefix and suffix that it covers, and its launch.
 corun_status shared_call(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_groups,
-                         const int32_t *group_rows, int32_t max_prefix, int32_t max_suffix, GroupTable *g, int *most)
+                         const int32_t *group_rows, int32_t max_prefix, int32_t max_suffix, GroupTable *g, int *most,
+                         SharedShape *shape)
 {
     TRY(check_heads(kv, n_heads, n_kv_heads, head_dim));
     if (!group_rows) return set_error(CORUN_E_INVAL, "null group_rows");
@@ -177,6 +178,10 @@ corun_status shared_call(const corun_kv *kv, int32_t n_heads, int32_t n_kv_heads
         return set_errorf(CORUN_E_CAPACITY, "max_prefix %d or max_suffix %d outside [0, %d]", max_prefix, max_suffix, cap);
     most[0] = max_prefix == 0 ? cap : max_prefix;
     most[1] = max_suffix == 0 ? cap : max_suffix;
+    *shape = shared_shape(*g, n_heads, n_kv_heads, most[0], most[1]);
+    if (shared_workgroups(*g, *shape, n_kv_heads) >= 1 << 24)
+        return set_errorf(CORUN_E_SHAPE, "%lld rows of %d kv heads and their splits: at most 2^24 - 1 workgroups", rows,
+                          n_kv_heads);
     return CORUN_OK;
 }
 
@@ -187,9 +192,10 @@ extern "C" int64_t corun_shared_attention_workspace(const corun_kv *kv, int32_t 
                                                     int32_t max_prefix, int32_t max_suffix)
 {
     GroupTable g;
+    SharedShape shape;
     int most[2];
-    TRY(shared_call(kv, n_heads, n_kv_heads, head_dim, n_groups, group_rows, max_prefix, max_suffix, &g, most));
-    return (int64_t)shared_ws(shared_shape(g, n_heads, n_kv_heads, most[0], most[1]), n_kv_heads, head_dim);
+    TRY(shared_call(kv, n_heads, n_kv_heads, head_dim, n_groups, group_rows, max_prefix, max_suffix, &g, most, &shape));
+    return (int64_t)shared_ws(shape, n_kv_heads, head_dim);
 }
 
 extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
@@ -200,8 +206,9 @@ extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer
                                                void *ws, int64_t ws_bytes, void *stream)
 {
     GroupTable g;
+    SharedShape shape;
     int most[2];
-    TRY(shared_call(kv, n_heads, n_kv_heads, head_dim, n_groups, group_rows, max_prefix, max_suffix, &g, most));
+    TRY(shared_call(kv, n_heads, n_kv_heads, head_dim, n_groups, group_rows, max_prefix, max_suffix, &g, most, &shape));
     CacheLayer cl;
     TRY(layer_of(kv, layer, &cl));
     TRY(check_rows("q", q, ld_q, (int64_t)n_heads * head_dim));
@@ -221,7 +228,6 @@ extern "C" corun_status corun_shared_attention(const corun_kv *kv, int32_t layer
     a.d = head_dim;
     a.max_prefix = most[0];
     a.max_suffix = most[1];
-    const SharedShape shape = shared_shape(g, n_heads, n_kv_heads, most[0], most[1]);
     TRY(check_ws(ws, ws_bytes, (int64_t)shared_ws(shape, n_kv_heads, head_dim)));
     return launched(launch_shared(a, g, shape, cache_view(kv), cl, (float *)ws, (hipStream_t)stream));
 }

@@ -64,6 +64,7 @@ struct SharedArgs {
 // A call's launch: where each group's 32-query blocks (of one kv head) and query
 // tiles start, and the splits; by value.
 struct SharedShape {
+    bool alone;                                        // one launch, no splits: the rest is not looked at
     int G, mt;                                         // query heads to a kv head; queries of a prefix tile
     int blocks;                                        // 32-query blocks of a kv head, all groups
     int chunk_p, splits_p, chunk_s, splits_s;          // tokens of a split, splits
@@ -71,6 +72,7 @@ struct SharedShape {
     uint16_t qb0[MOST_GROUPS + 1], tile0[MOST_GROUPS + 1];
 };
 SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix);
+long long shared_workgroups(const GroupTable &g, const SharedShape &s, int nkv);   // of its largest launch
 size_t shared_ws(const SharedShape &s, int nkv, int d);
 hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const SharedShape &s, const CacheView &cv,
                          const CacheLayer &cl, float *ws, hipStream_t st);

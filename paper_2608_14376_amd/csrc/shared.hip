@@ -175,10 +175,14 @@ constexpr float LAG = 6.f;
 template <int D, bool E4>
 constexpr int few_lds() { return 4 * (32 * D * (E4 ? 1 : 2) > 16 * D * 4 ? 32 * D * (E4 ? 1 : 2) : 16 * D * 4); }
 
-template <int D, bool E4, bool PAGED, int MT, class QueryOf>
+struct Span {
+    int slot, t_lo, t_end;
+};
+
+template <int D, bool E4, bool PAGED, int MT, int SPANS, class QueryOf, class Emit>
 __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*cl)[64], int *lost, const CacheView &cv,
-                                           const CacheLayer &layer, int nkv, int kvh, int slot, int t_lo, int t_end,
-                                           int queries, QueryOf &&query, float *part, int u0)
+                                           const CacheLayer &layer, int nkv, int kvh, const Span (&spans)[SPANS],
+                                           int queries, QueryOf &&query, Emit &&emit)
 {
     constexpr int EB = E4 ? 1 : 2, RB = D * EB, KCH = RB / 16;       // bytes of a row; its 16-byte units
     constexpr int NK = RB / 64, NV = 32 * RB / 1024, ET = D / 16, KK = D / 32;
@@ -208,175 +212,180 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         for (int et = 0; et < ET; ++et) acc[m][et] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const uint8_t *kc = (const uint8_t *)layer.k, *vc = (const uint8_t *)layer.v;
-    const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
     bool bad = false;
-    int tb = (t_lo & ~15) + 32 * wave, pg[2] = {0, 0}, in[2] = {0, 0};
-    const int ps = PAGED ? cv.kv.page_size : 16;
-    Walk walk(PAGED ? tb : 0, 128, ps);
-    auto pages = [&](int t) {                          // of the wavefront's two groups of 16 tokens from t, one step on at every call
-        if constexpr (PAGED) {
-            const bool same = walk.in + 16 < ps;
-            if (t < t_end) pg[0] = pt[walk.page];
-            if (t + 16 < t_end) pg[1] = pt[walk.page + !same];
-            in[0] = walk.in;
-            in[1] = same ? walk.in + 16 : 0;
-            walk.next(ps);
-        }
-    };
-    uint4 kr[2][NK];
-    uint32_t ks = 0, vs = 0;                           // scale bytes of this lane's keys, and of its eight value tokens
-    const uint8_t *kp = nullptr;
-    auto issue_values = [&](int t) {                   // and where the step's keys are
-        Rows16 at[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            int page = __builtin_amdgcn_readfirstlane(pg[j]);
-            if (PAGED && (unsigned)page >= (unsigned)cv.num_pages) {
-                if (t + 16 * j < t_end) bad = true;
-                page = 0;
+    for (int sp = 0; sp < SPANS; ++sp) {
+        const int slot = spans[sp].slot, t_lo = spans[sp].t_lo, t_end = spans[sp].t_end;
+        if (t_lo >= t_end) continue;
+        const int32_t *pt = PAGED ? cv.kv.page_table + (size_t)slot * cv.kv.max_pages_per_seq : nullptr;
+        int tb = (t_lo & ~15) + 32 * wave, pg[2] = {0, 0}, in[2] = {0, 0};
+        const int ps = PAGED ? cv.kv.page_size : 16;
+        Walk walk(PAGED ? tb : 0, 128, ps);
+        auto pages = [&](int t) {                          // of the wavefront's two groups of 16 tokens from t, one step on at every call
+            if constexpr (PAGED) {
+                const bool same = walk.in + 16 < ps;
+                if (t < t_end) pg[0] = pt[walk.page];
+                if (t + 16 < t_end) pg[1] = pt[walk.page + !same];
+                in[0] = walk.in;
+                in[1] = same ? walk.in + 16 : 0;
+                walk.next(ps);
             }
-            at[j] = rows16<PAGED>(cv, nkv, kvh, slot, page, in[j], t + 16 * j < t_end ? t + 16 * j : t);
-            if (t + 16 * j >= t_end) at[j] = at[0];    // past the end: the first group again, masked below
-        }
-        const Rows16 ka = hl & 8 ? at[1] : at[0];
-        kp = kc + (ka.row + 8 * ((hl >> 2) & 1) + (hl & 3)) * RB + kg * (RB / 4);
-        if constexpr (E4) {
-            ks = layer.ks[ka.blk];
-            vs = layer.vs[(kg & 2 ? at[1] : at[0]).blk];
-        }
+        };
+        uint4 kr[2][NK];
+        uint32_t ks = 0, vs = 0;                           // scale bytes of this lane's keys, and of its eight value tokens
+        const uint8_t *kp = nullptr;
+        auto issue_values = [&](int t) {                   // and where the step's keys are
+            Rows16 at[2];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int tk = (j * 64 + lane) / KCH, p = (j * 64 + lane) % KCH;
-            int c;
-            if constexpr (E4) c = p ^ (KCH == 8 ? (tk >> 1) & 7 : (tk >> 2) & 3);
-            else c = p ^ vtile_swz<KCH>(tk);
-            const size_t row = (j * 64 / KCH >= 16 ? at[1] : at[0]).row;
-            __builtin_amdgcn_global_load_lds((const void *)(vc + row * RB + (tk & 15) * RB + 16 * c),
-                                             (lds_void *)(mine + 1024 * j), 16, 0, 0);
-        }
-    };
-    auto issue_keys = [&]() {
-#pragma unroll
-        for (int T = 0; T < 2; ++T)
-#pragma unroll
-            for (int j = 0; j < NK; ++j) kr[T][j] = *(const uint4 *)(kp + 4 * T * RB + 16 * j);
-    };
-    if (tb < t_end) {
-        pages(tb);
-        issue_values(tb);
-        issue_keys();
-        pages(tb + 128);
-    }
-    for (; tb < t_end; tb += 128) {
-        const bool more = tb + 128 < t_end;
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        asm volatile("" ::: "memory");
-        const float ksc = __uint_as_float(ks << 23), vsc = __uint_as_float(vs << 23);
-        uint4 vr[ET];                                  // e4m3: the codes in the first two words
-#pragma unroll
-        for (int et = 0; et < ET; ++et) {
+            for (int j = 0; j < 2; ++j) {
+                int page = __builtin_amdgcn_readfirstlane(pg[j]);
+                if (PAGED && (unsigned)page >= (unsigned)cv.num_pages) {
+                    if (t + 16 * j < t_end) bad = true;
+                    page = 0;
+                }
+                at[j] = rows16<PAGED>(cv, nkv, kvh, slot, page, in[j], t + 16 * j < t_end ? t + 16 * j : t);
+                if (t + 16 * j >= t_end) at[j] = at[0];    // past the end: the first group again, masked below
+            }
+            const Rows16 ka = hl & 8 ? at[1] : at[0];
+            kp = kc + (ka.row + 8 * ((hl >> 2) & 1) + (hl & 3)) * RB + kg * (RB / 4);
             if constexpr (E4) {
-                const int t = 8 * kg + (hl >> 1), swz = KCH == 8 ? (t >> 1) & 7 : (t >> 2) & 3;
-                const uint2 w = read_tr8(mine + 16 * (t * KCH + (et ^ swz)) + 8 * (hl & 1));
-                vr[et] = (uint4){w.x, w.y, 0u, 0u};
-            } else {
-                uint2 w[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int t = 8 * kg + 4 * r + (hl >> 2), c = 2 * et + ((hl & 3) >> 1);
-                    w[r] = lds_read_tr16(mine + 16 * (t * KCH + (c ^ vtile_swz<KCH>(t))) + 8 * (hl & 1));
-                }
-                vr[et] = (uint4){w[0].x, w[0].y, w[1].x, w[1].y};
-            }
-        }
-        __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the values are in registers
-        asm volatile("" ::: "memory");
-        if (more) issue_values(tb + 128);
-        const bool edge = tb < t_lo || tb + 32 > t_end;   // wave-uniform: some of the 32 tokens are masked
-        const int first = t_lo - (tb + 8 * kg), behind = t_end - (tb + 8 * kg);   // this lane's real tokens: first .. behind - 1 of 8
-        if (edge) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool off = e < first || e >= behind;
-#pragma unroll
-                for (int et = 0; et < ET; ++et) {
-                    uint32_t *w = (uint32_t *)&vr[et];
-                    if constexpr (E4) w[e / 4] &= off ? ~(0xffu << (8 * (e % 4))) : ~0u;
-                    else w[e / 2] &= off ? ~(0xffffu << (16 * (e % 2))) : ~0u;
-                }
-            }
-        }
-        f32x4 st[MT][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) st[m][0] = st[m][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            bf16x8 kf[2];
-#pragma unroll
-            for (int T = 0; T < 2; ++T) {
-                if constexpr (E4) {
-                    const uint4 w = kr[T][kk / 2];
-                    kf[T] = __builtin_bit_cast(bf16x8, kk & 1 ? codes8(w.z, w.w, ksc) : codes8(w.x, w.y, ksc));
-                } else {
-                    kf[T] = __builtin_bit_cast(bf16x8, kr[T][kk]);
-                }
+                ks = layer.ks[ka.blk];
+                vs = layer.vs[(kg & 2 ? at[1] : at[0]).blk];
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int T = 0; T < 2; ++T) st[m][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T], qf[m][kk], st[m][T], 0, 0, 0);
-        }
-        if (more) {
-            issue_keys();
-            pages(tb + 256);
-        }
-        bf16x8 ph[MT], pl[MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            float mt = -INFINITY;
+            for (int j = 0; j < NV; ++j) {
+                const int tk = (j * 64 + lane) / KCH, p = (j * 64 + lane) % KCH;
+                int c;
+                if constexpr (E4) c = p ^ (KCH == 8 ? (tk >> 1) & 7 : (tk >> 2) & 3);
+                else c = p ^ vtile_swz<KCH>(tk);
+                const size_t row = (j * 64 / KCH >= 16 ? at[1] : at[0]).row;
+                __builtin_amdgcn_global_load_lds((const void *)(vc + row * RB + (tk & 15) * RB + 16 * c),
+                                                 (lds_void *)(mine + 1024 * j), 16, 0, 0);
+            }
+        };
+        auto issue_keys = [&]() {
 #pragma unroll
             for (int T = 0; T < 2; ++T)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (edge) st[m][T][e] = 4 * T + e >= first && 4 * T + e < behind ? st[m][T][e] : -INFINITY;
-                    mt = fmaxf(mt, st[m][T][e]);
-                }
-            mt = fmaxf(mt, other<16>(mt));
-            mt = fmaxf(mt, other<32>(mt)) * scale2;
-            const float mnew = mt > mrun[m] + LAG ? mt : mrun[m], moff = mnew == -INFINITY ? 0.f : mnew;
-            if (__ballot(mnew != mrun[m])) {           // lane l's sums belong to queries 4 (l / 16) + e
-                const float alpha = mnew == mrun[m] ? 1.f : __builtin_amdgcn_exp2f(mrun[m] - mnew);
-                lrun[m] *= alpha;
-                mrun[m] = mnew;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float ae = __shfl(alpha, 4 * kg + e, 64);
-#pragma unroll
-                    for (int et = 0; et < ET; ++et) acc[m][et][e] *= ae;
-                }
-            }
-            uint32_t hi[4], lo[4];
-            float ls = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2)], scale2, -moff));
-                const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2) + 1], scale2, -moff));
-                ls += a + b;
-                const uint32_t w = f2bf2(a, b);
-                hi[i] = w;
-                lo[i] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
-            }
-            lrun[m] += ls;
-            ph[m] = __builtin_bit_cast(bf16x8, hi);
-            pl[m] = __builtin_bit_cast(bf16x8, lo);
+                for (int j = 0; j < NK; ++j) kr[T][j] = *(const uint4 *)(kp + 4 * T * RB + 16 * j);
+        };
+        if (tb < t_end) {
+            pages(tb);
+            issue_values(tb);
+            issue_keys();
+            pages(tb + 128);
         }
+        for (; tb < t_end; tb += 128) {
+            const bool more = tb + 128 < t_end;
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+            asm volatile("" ::: "memory");
+            const float ksc = __uint_as_float(ks << 23), vsc = __uint_as_float(vs << 23);
+            uint4 vr[ET];                                  // e4m3: the codes in the first two words
 #pragma unroll
-        for (int et = 0; et < ET; ++et) {
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, E4 ? codes8(vr[et].x, vr[et].y, vsc) : vr[et]);
+            for (int et = 0; et < ET; ++et) {
+                if constexpr (E4) {
+                    const int t = 8 * kg + (hl >> 1), swz = KCH == 8 ? (t >> 1) & 7 : (t >> 2) & 3;
+                    const uint2 w = read_tr8(mine + 16 * (t * KCH + (et ^ swz)) + 8 * (hl & 1));
+                    vr[et] = (uint4){w.x, w.y, 0u, 0u};
+                } else {
+                    uint2 w[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int t = 8 * kg + 4 * r + (hl >> 2), c = 2 * et + ((hl & 3) >> 1);
+                        w[r] = lds_read_tr16(mine + 16 * (t * KCH + (c ^ vtile_swz<KCH>(t))) + 8 * (hl & 1));
+                    }
+                    vr[et] = (uint4){w[0].x, w[0].y, w[1].x, w[1].y};
+                }
+            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): the values are in registers
+            asm volatile("" ::: "memory");
+            if (more) issue_values(tb + 128);
+            const bool edge = tb < t_lo || tb + 32 > t_end;   // wave-uniform: some of the 32 tokens are masked
+            const int first = t_lo - (tb + 8 * kg), behind = t_end - (tb + 8 * kg);   // this lane's real tokens: first .. behind - 1 of 8
+            if (edge) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool off = e < first || e >= behind;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et) {
+                        uint32_t *w = (uint32_t *)&vr[et];
+                        if constexpr (E4) w[e / 4] &= off ? ~(0xffu << (8 * (e % 4))) : ~0u;
+                        else w[e / 2] &= off ? ~(0xffffu << (16 * (e % 2))) : ~0u;
+                    }
+                }
+            }
+            f32x4 st[MT][2];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) st[m][0] = st[m][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                bf16x8 kf[2];
+#pragma unroll
+                for (int T = 0; T < 2; ++T) {
+                    if constexpr (E4) {
+                        const uint4 w = kr[T][kk / 2];
+                        kf[T] = __builtin_bit_cast(bf16x8, kk & 1 ? codes8(w.z, w.w, ksc) : codes8(w.x, w.y, ksc));
+                    } else {
+                        kf[T] = __builtin_bit_cast(bf16x8, kr[T][kk]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int T = 0; T < 2; ++T) st[m][T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[T], qf[m][kk], st[m][T], 0, 0, 0);
+            }
+            if (more) {
+                issue_keys();
+                pages(tb + 256);
+            }
+            bf16x8 ph[MT], pl[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph[m], vf, acc[m][et], 0, 0, 0);
-                acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl[m], vf, acc[m][et], 0, 0, 0);
+                float mt = -INFINITY;
+#pragma unroll
+                for (int T = 0; T < 2; ++T)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (edge) st[m][T][e] = 4 * T + e >= first && 4 * T + e < behind ? st[m][T][e] : -INFINITY;
+                        mt = fmaxf(mt, st[m][T][e]);
+                    }
+                mt = fmaxf(mt, other<16>(mt));
+                mt = fmaxf(mt, other<32>(mt)) * scale2;
+                const float mnew = mt > mrun[m] + LAG ? mt : mrun[m], moff = mnew == -INFINITY ? 0.f : mnew;
+                if (__ballot(mnew != mrun[m])) {           // lane l's sums belong to queries 4 (l / 16) + e
+                    const float alpha = mnew == mrun[m] ? 1.f : __builtin_amdgcn_exp2f(mrun[m] - mnew);
+                    lrun[m] *= alpha;
+                    mrun[m] = mnew;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ae = __shfl(alpha, 4 * kg + e, 64);
+#pragma unroll
+                        for (int et = 0; et < ET; ++et) acc[m][et][e] *= ae;
+                    }
+                }
+                uint32_t hi[4], lo[4];
+                float ls = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2)], scale2, -moff));
+                    const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(st[m][i / 2][2 * (i % 2) + 1], scale2, -moff));
+                    ls += a + b;
+                    const uint32_t w = f2bf2(a, b);
+                    hi[i] = w;
+                    lo[i] = f2bf2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+                }
+                lrun[m] += ls;
+                ph[m] = __builtin_bit_cast(bf16x8, hi);
+                pl[m] = __builtin_bit_cast(bf16x8, lo);
+            }
+#pragma unroll
+            for (int et = 0; et < ET; ++et) {
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, E4 ? codes8(vr[et].x, vr[et].y, vsc) : vr[et]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ph[m], vf, acc[m][et], 0, 0, 0);
+                    acc[m][et] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pl[m], vf, acc[m][et], 0, 0, 0);
+                }
             }
         }
     }
@@ -399,7 +408,7 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
         __syncthreads();
         const int here = min(16, queries - 16 * m);
         for (int i = tid; i < here * (D / 4); i += 256) {
-            const int g = i / (D / 4), d4 = i % (D / 4), u = u0 + 16 * m + g;
+            const int g = i / (D / 4), d4 = i % (D / 4);
             float M = -INFINITY, L = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) M = fmaxf(M, cm[w][16 * m + g]);
@@ -415,12 +424,19 @@ __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*c
                 o.z += x.z * f;
                 o.w += x.w * f;
             }
-            float *dst = part + (u / 32) * part_floats<D>();
-            *(float4 *)(dst + (d4 * 32 + u % 32) * 4) = o;
-            if (d4 == 0) *(float2 *)(dst + 32 * D + 2 * (u % 32)) = {*lost ? qnan() : M, L};
+            emit(16 * m + g, d4, o, *lost ? qnan() : M, L);
         }
         __syncthreads();
     }
+}
+
+// Query u's result of a split, to the workspace.
+template <int D>
+__device__ __forceinline__ void emit_part(float *part, int u, int d4, const float4 &o, float m, float l)
+{
+    float *dst = part + (u / 32) * part_floats<D>();
+    *(float4 *)(dst + (d4 * 32 + u % 32) * 4) = o;
+    if (d4 == 0) *(float2 *)(dst + 32 * D + 2 * (u % 32)) = {m, l};
 }
 
 // ---------------------------------------------------------------------------
@@ -710,8 +726,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTabl
             attend_many<D, E4, PAGED>(lds, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
                                       part + (u0 / 32) * part_floats<D>());
         else
-            attend_few<D, E4, PAGED, MT / 16>(lds, cm, cl, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
-                                              part, u0);
+            attend_few<D, E4, PAGED, MT / 16, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, {{p.slot, t0, t_end}}, queries, query,
+                                                 [&](int u, int d4, const float4 &o, float m, float l) {
+                                                     emit_part<D>(part, u0 + u, d4, o, m, l);
+                                                 });
         return;
     }
     const int v = unit - np, split = v % s.splits_s, r = v / s.splits_s;
@@ -720,8 +738,38 @@ __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTabl
     const int n = row_len(a, cv, p, r), t0 = (p.len & ~15) + split * s.chunk_s;
     if (n <= p.len || t0 >= n) return;
     const auto query = [&](int m) { return a.q + (size_t)r * a.ldq + (size_t)(kvh * G + m) * D; };
-    attend_few<D, E4, PAGED, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, r, max(t0, p.len), min(n, t0 + s.chunk_s), G, query,
-                                part_at<D>(ws, s, nkv, s.splits_p + split, kvh, s.qb0[gi]), (r - gt.row0[gi]) * G);
+    float *part = part_at<D>(ws, s, nkv, s.splits_p + split, kvh, s.qb0[gi]);
+    const int u0 = (r - gt.row0[gi]) * G;
+    attend_few<D, E4, PAGED, 1, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, {{r, max(t0, p.len), min(n, t0 + s.chunk_s)}}, G,
+                                   query, [&](int u, int d4, const float4 &o, float m, float l) {
+                                       emit_part<D>(part, u0 + u, d4, o, m, l);
+                                   });
+}
+
+// The smallest calls in one launch: a workgroup to a row and kv head, which goes
+// over the prefix and the row's own tokens by itself.
+template <int D, bool E4, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_shared_alone(SharedArgs a, GroupTable gt, CacheView cv, CacheLayer layer)
+{
+    __shared__ __attribute__((aligned(16))) char lds[few_lds<D, E4>()];
+    __shared__ float cm[4][64], cl[4][64];
+    __shared__ int lost;
+    const int nkv = a.nkv, G = a.nq / nkv, kvh = blockIdx.x % nkv, r = blockIdx.x / nkv;
+    const int gi = last_at_most(gt.row0, gt.n, r);
+    const Prefix p = prefix_of(a, gt, cv, gi);
+    const int n = row_len(a, cv, p, r);
+    uint16_t *out = a.out + (size_t)r * a.ldo + (size_t)kvh * G * D;
+    if (n <= 0) {
+        for (int i = threadIdx.x; i < G * D; i += 256) out[i] = n < 0 ? (uint16_t)0x7fc0 : (uint16_t)0;
+        return;
+    }
+    const auto query = [&](int m) { return a.q + (size_t)r * a.ldq + (size_t)(kvh * G + m) * D; };
+    attend_few<D, E4, PAGED, 1, 2>(lds, cm, cl, &lost, cv, layer, nkv, kvh, {{p.slot, 0, p.len}, {r, p.len, n}}, G, query,
+                                   [&](int u, int d4, const float4 &o, float m, float l) {
+                                       const float inv = (m != m ? m : 1.0f) / l;
+                                       *(uint2 *)(out + (size_t)u * D + 4 * d4) = {f2bf2(o.x * inv, o.y * inv),
+                                                                                  f2bf2(o.z * inv, o.w * inv)};
+                                   });
 }
 
 // Joins the splits: a workgroup takes four dimension fours (y) of a 32-query block
@@ -783,9 +831,17 @@ __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt
 
 }  // namespace
 
+// Whether a call is one launch of a workgroup to a row and kv head: few enough that
+// all run at once, and not over four steps of 128 tokens.
+static bool alone(const GroupTable &g, int nkv, int max_prefix, int max_suffix)
+{
+    return (long long)max_prefix + max_suffix <= 512 && (long long)g.row0[g.n] * nkv <= 512;
+}
+
 SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, int max_suffix)
 {
     SharedShape s;
+    s.alone = alone(g, nkv, max_prefix, max_suffix);
     s.G = nq / nkv;
     int most = 0;
     for (int i = 0; i < g.n; ++i) most = std::max(most, (g.row0[i + 1] - g.row0[i]) * s.G);
@@ -821,8 +877,15 @@ SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, i
     return s;
 }
 
+long long shared_workgroups(const GroupTable &g, const SharedShape &s, int nkv)
+{
+    if (s.alone) return (long long)g.row0[g.n] * nkv;
+    return std::max(((long long)s.tiles * s.splits_p + (long long)g.row0[g.n] * s.splits_s) * nkv, (long long)s.blocks * nkv);
+}
+
 size_t shared_ws(const SharedShape &s, int nkv, int d)
 {
+    if (s.alone) return 0;
     return (size_t)(s.splits_p + s.splits_s) * nkv * s.blocks * (d == 128 ? part_floats<128>() : part_floats<64>()) *
            sizeof(float);
 }
@@ -830,9 +893,20 @@ size_t shared_ws(const SharedShape &s, int nkv, int d)
 hipError_t launch_shared(const SharedArgs &a, const GroupTable &g, const SharedShape &s, const CacheView &cv,
                          const CacheLayer &cl, float *ws, hipStream_t st)
 {
-    const long long wgs = ((long long)s.tiles * s.splits_p + (long long)g.row0[g.n] * s.splits_s) * a.nkv;
-    if (wgs > (1 << 24) - 1) return hipErrorInvalidValue;
+    const long long wgs = shared_workgroups(g, s, a.nkv);
     const bool paged = cv.kv.layout == 1;
+    if (s.alone) {
+        const dim3 grid((unsigned)g.row0[g.n] * a.nkv);
+#define CORUN_ALONE(D_, E_) \
+    if (a.d == D_ && cv.e4m3 == E_ && paged) KLAUNCH((k_shared_alone<D_, E_, true>), grid, dim3(256), 0, st, a, g, cv, cl); \
+    if (a.d == D_ && cv.e4m3 == E_ && !paged) KLAUNCH((k_shared_alone<D_, E_, false>), grid, dim3(256), 0, st, a, g, cv, cl)
+        CORUN_ALONE(128, 1);
+        CORUN_ALONE(128, 0);
+        CORUN_ALONE(64, 1);
+        CORUN_ALONE(64, 0);
+#undef CORUN_ALONE
+        return hipGetLastError();
+    }
 #define CORUN_SHARED(D_, E_, P_, M_) \
     KLAUNCH((k_shared_parts<D_, E_, P_, M_>), dim3((unsigned)wgs), dim3(256), 0, st, a, g, s, cv, cl, ws)
 #define CORUN_SHARED_M(D_, E_, P_)                     \

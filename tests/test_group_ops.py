@@ -96,6 +96,13 @@ def test_shared_attention_refusals(dtype, kw, status):
     assert shared(_kv(dtype=dtype), **kw) == status and corun.last_error()
 
 
+def test_shared_attention_refuses_too_many_workgroups():
+    kv = _kv(n_slots=60000, max_seq_len=1024)
+    rows = (60000,)
+    assert shared(kv, nq=4096, nkv=4096, d=64, groups=rows, ldq=1 << 18, ldo=1 << 18) == corun.E_SHAPE
+    assert corun.load().corun_shared_attention_workspace(C.addressof(kv), 4096, 4096, 64, 1, _i32(*rows), 0, 0) == corun.E_SHAPE
+
+
 def test_shared_attention_refuses_caches():
     assert shared(None) == corun.E_INVAL
     assert shared(_kv(ptr=None)) == shared(_kv(scales=None)) == shared(_kv(layout=3)) == corun.E_INVAL
