@@ -553,7 +553,7 @@ def _need(n):
 
 
 def _beam(t, dtypes, shape, index, name):
-    if t.dtype not in dtypes or t.get_device() != index or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype not in dtypes or t.shape != shape or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous {dtypes[0]} {list(shape)} on cuda:{index}")
     return t.data_ptr()
 
@@ -576,29 +576,26 @@ def beam_select(logits, scores, beams, tokens, parents, out_scores, ws, valid=No
     may overlap.  Does not wait."""
     global _torch
     _torch = _torch or _Torch()
-    index, shape = logits.get_device(), logits.shape
-    if logits.dtype is not _torch.fp32[0] or index < 0 or len(shape) != 2 or (shape[1] > 1 and logits.stride(1) != 1) or \
-            shape[1] < 1:
+    index, shape, fp32, flags = logits.get_device(), logits.shape, _torch.fp32, _torch.flags
+    if logits.dtype is not fp32[0] or index < 0 or len(shape) != 2 or shape[1] < 1 or (shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits: fp32 [groups beams, vocab] on the GPU, the elements of a row contiguous")
     rows, vocab = shape
     if beams < 1 or rows < 1 or rows % beams:
         raise ValueError(f"logits: {rows} rows are not groups of {beams}")
     if tokens.dim() != 2:
         raise ValueError("tokens: int32 [groups, n_keep]")
-    groups, keep = rows // beams, tokens.shape[1]
-    flat, out = (rows,), (groups, keep)
-    opt = lambda t, dtypes, name, shape=flat: None if t is None else _beam(t, dtypes, shape, index, name)
     if index != _torch.device():
         raise ValueError(f"logits are on cuda:{index}, the current device is cuda:{_torch.device()}")
-    size = ws.numel()
+    flat, out, size = (rows,), (rows // beams, tokens.shape[1]), ws.numel()
     _check(load().corun_beam_select(
-        logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, groups, beams,
-        _beam(scores, _torch.fp32, flat, index, "scores"), opt(valid, _torch.flags, "valid"),
-        opt(finished, _torch.flags, "finished"), opt(weights, _torch.fp32, "weights"), end_token, keep,
+        logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, out[0], beams,
+        _beam(scores, fp32, flat, index, "scores"), None if valid is None else _beam(valid, flags, flat, index, "valid"),
+        None if finished is None else _beam(finished, flags, flat, index, "finished"),
+        None if weights is None else _beam(weights, fp32, flat, index, "weights"), end_token, out[1],
         _beam(tokens, _torch.ints, out, index, "tokens"), _beam(parents, _torch.ints, out, index, "parents"),
-        _beam(out_scores, _torch.fp32, out, index, "out_scores"), opt(out_finished, _torch.flags, "out_finished", out),
-        _beam(ws, _torch.flags[:1], (size,), index, "ws"), size,
-        _torch.stream(index) if stream is None else stream.cuda_stream))
+        _beam(out_scores, fp32, out, index, "out_scores"),
+        None if out_finished is None else _beam(out_finished, flags, out, index, "out_finished"),
+        _beam(ws, flags[:1], (size,), index, "ws"), size, _torch.stream(index) if stream is None else stream.cuda_stream))
 
 
 def pages_workspace(cache) -> int:

@@ -3,7 +3,9 @@ layouts, caches, groups, prefixes and suffixes from nothing to long, padding,
 what must not be seen, and calls out of range.
 
 Tolerances: cache_reference.attention_bound with weights of at least 16 bits
-(2^-14 leaves room for both halves' roundings)."""
+(2^-14 leaves room for both halves' roundings), or, where a group has over 32
+queries of a kv head on an e4m3 cache, of fp16: off by at most half a step, 2^-11,
+and as much again as the others for what is far below the largest."""
 import numpy as np
 import pytest
 import torch
@@ -17,6 +19,11 @@ from tests.test_gpu_cache_ops import rows_of, same
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 U_WEIGHT = 2.0**-14
+
+
+def u_weight(hc, q, groups):
+    queries = max(groups) * (q.shape[1] // hc.d // hc.nkv)
+    return U_WEIGHT + (2.0**-11 if hc.ks is not None and queries > 32 else 0.0)
 
 
 def i32(x):
@@ -46,7 +53,7 @@ def check(hc, q, out, groups, lens, prefix, slots, valid=None, rows=None):
             assert (got == 0).all()
             continue
         want, pv, size = gref.shared_attention(hc, q[r].double().view(-1, d), r, slots[of[r]], prefix[of[r]], lens[r])
-        tol = ref.attention_bound(want, pv, size, d, max(lens[r], 1), U_WEIGHT)
+        tol = ref.attention_bound(want, pv, size, d, max(lens[r], 1), u_weight(hc, q, groups))
         err = (got - want).abs()
         assert (err <= tol).all(), (r, float((err / tol.clamp(min=1e-30)).max()), lens[r], prefix[of[r]])
 
@@ -229,6 +236,35 @@ def test_scores_and_values_of_any_size(dtype, rows):
     q[1] = 0
     q[2] *= 1000
     lens = [P + 7 * (r % 9) for r in range(rows)]
+    out = run(hc.device_cache(corun), q.to(DEV), [rows], lens, [P], [rows])
+    check(hc, q, out, [rows], lens, [P], [rows])
+
+
+@pytest.mark.parametrize("d,page", [(128, 0), (64, 32)])
+@pytest.mark.parametrize("spread", [8, 24, 25, 60])
+def test_scales_apart(d, page, spread):
+    """Value scales of a prefix that are as far apart as one fp16 product takes, farther in one block of one split, and far
+    apart everywhere; the weight goes to tokens of small scales, to those of large ones, and to all."""
+    nq, nkv, rows, P, blk = 8, 2, 30, 1700, 16
+    cap = -(-(P + 64) // 96) * 96 if page else 1792
+    hc = HostCache(nkv, d, rows + 1, cap, blk, page, seed=30, dtype="e4m3")
+    hc.vs[:] = 120
+    at = [hc.at(rows, t) for t in range(0, P, blk)]
+    rng = np.random.default_rng(spread)
+    for i, (pg, t) in enumerate(at):
+        near = min(spread, 24) if spread < 60 else 60
+        up = 0 if i == 0 else int(rng.integers(-near, near + 1))
+        if spread == 25 and i == 40:
+            up = 25
+        hc.vs[pg, :, t // blk] = 120 + up
+    for i in (20, 41):                                 # keys that some queries meet
+        pg, t = at[i]
+        hc.ks[pg, :, t // blk] += 3
+        hc.vs[pg, :, t // blk] = 120 + (8 if i == 20 else -8)
+    q, _ = rows_of(rows, nq, d, 31)
+    q[1] *= 8
+    q[2] = 0
+    lens = [P + r % 5 for r in range(rows)]
     out = run(hc.device_cache(corun), q.to(DEV), [rows], lens, [P], [rows])
     check(hc, q, out, [rows], lens, [P], [rows])
 
