@@ -13,6 +13,15 @@
 // lists' heads), some one to two times `keep` candidates reach it, and each finds
 // its place by counting those before it.  Sums and places are in a fixed order,
 // whatever the order in which candidates were noted.
+//
+// k_beam_part: 195 live rows of 151936 logits, 118 MB, in 36 us, 3.3 TB/s (a copy
+// reaches 5.1).  Its vector arithmetic alone is 24 us, most of it the exponentials
+// in 64 bits (18 instructions for each logit); the rest is waiting for loads and for
+// the part's other wavefronts.  Parts of 4096 columns came out the same (39 us), a
+// workgroup that loads its next part while it works on this one slower (58 us for
+// the whole call, 47 so): its registers leave fewer wavefronts.
+// k_beam_pick: 7 us for 64 groups of 4 rows and 4 results, 12 for 4 groups of 32 rows
+// and 64 results: a chain of dependent loads and barriers.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

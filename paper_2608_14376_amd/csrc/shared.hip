@@ -12,8 +12,15 @@
 // call's sizes and a row's lengths alone, and a query's arithmetic does not depend
 // on its place in a tile, so rows stay position-invariant.
 //
-// Weights enter the matrix units as two bf16 halves, hi + lo (about 16 bits);
-// bf16 values and the codes of an e4m3 cache times their scale are exact there.
+// Weights enter the matrix units as two bf16 halves, hi + lo (about 16 bits), or, over
+// many queries of an e4m3 cache, as fp16; bf16 values and the codes of an e4m3
+// cache times their scale are exact there.
+//
+// The rows' own tokens are bound by reading (228 rows of 1024 bf16 tokens of 8 kv
+// heads of 128: 5.1 TB/s, a large copy's rate), the prefixes by the products and
+// the softmax of a wavefront in turn (below).  Prefixes' workgroups come first in
+// the launch: mixed among the others they were spread unevenly over the CUs (128
+// rows of 64 heads behind 32768 tokens: 313 us, 233 so).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -171,7 +178,13 @@ __device__ __forceinline__ Rows16 rows16(const CacheView &cv, int nkv, int kvh, 
 //    through transposed reads.
 // The next step's values are loaded once this step's are in registers, its keys
 // once this step's scores are there.  Weights are 2^(s - ref), where ref follows
-// the running maximum when that is more than LAG above it.
+// the running maximum when that is more than LAG above it: most steps rescale
+// nothing.
+//
+// For few queries this is bound by loads: a step is 16 KB (e4m3) or 32 KB for 16 or
+// 32 queries.  48 and 64 queries in the same way were slower than the shared tiles
+// below, from 33 queries on (128 rows of 4 heads to a kv head behind 8000 e4m3 tokens:
+// 58 us, 49; 10 rows 31, 25): every wavefront then waits for loads of its own.
 // ---------------------------------------------------------------------------
 constexpr float LAG = 6.f;
 
@@ -459,8 +472,14 @@ __device__ __forceinline__ void emit_part(float *part, int u, int d4, const floa
 // maximum of s + b.  They keep 11 bits down to 2^-22 of the largest, what is below
 // 2^-32 of it becomes zero, and the sum, of the weights before they are rounded,
 // takes the scales out again.  A split with a scale more than 2^NEAR from its
-// first, where 32 bits may not hold that sum, is left to attend_few.  (Four documents of 11 to 30 thousand tokens with 11 to 29 rows of 64 heads:
-// HALF_FIGURES.)
+// first, where 32 bits may not hold that sum, is left to attend_few.  (Four documents
+// of 11 to 30 thousand tokens, 80 rows of 64 heads: 139 us, 156 with two halves.)
+//
+// Bound by a wavefront's products and softmax in turn: 128 rows of 64 heads behind
+// 32768 tokens take 203 us (e4m3, 0.68 PFLOP/s) or 250 (bf16, 0.55; its second
+// product is done twice).  A SIMD's two wavefronts hardly overlap the two: with two
+// products, of the time that a CU was busy the matrix units took 43% and the vector
+// units 55%.  Raising a wavefront's priority around its products changed nothing.
 // ---------------------------------------------------------------------------
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -551,7 +570,6 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
     auto store = [&](int k0, int b) {
         uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
         const float ksc = __uint_as_float(__builtin_amdgcn_readfirstlane(ks8) << 23);
-        const float vsc = __uint_as_float(__builtin_amdgcn_readfirstlane(vs8) << 23);
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
             const int u = 64 * j + lane, row = 16 * wave + u / RU, c = u % RU;
@@ -562,10 +580,10 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
             }
             K[pf_swz<KCH>(row, 2 * c)] = codes8(kraw[j].x, kraw[j].y, ksc);
             K[pf_swz<KCH>(row, 2 * c + 1)] = codes8(kraw[j].z, kraw[j].w, ksc);
-            V[row * KCH + ((2 * c) ^ val16_swz<KCH>(row))] = HALF ? codes8_half(w.x, w.y) : codes8(w.x, w.y, vsc);
-            V[row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row))] = HALF ? codes8_half(w.z, w.w) : codes8(w.z, w.w, vsc);
+            V[row * KCH + ((2 * c) ^ val16_swz<KCH>(row))] = codes8_half(w.x, w.y);
+            V[row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row))] = codes8_half(w.z, w.w);
         }
-        if (HALF && lane == 0) scales[b][wave] = k0 + 16 * wave < t_end ? (int)vs8 : -1;
+        if (lane == 0) scales[b][wave] = k0 + 16 * wave < t_end ? (int)vs8 : -1;
     };
     // bf16: straight to buffer b; values past the end are cleared once they have landed
     auto direct = [&](int b) {
@@ -847,7 +865,9 @@ __global__ __launch_bounds__(256, 2) void k_shared_alone(SharedArgs a, GroupTabl
 }
 
 // Joins the splits: a workgroup takes four dimension fours (y) of a 32-query block
-// of a kv head (x); thread (four, query).
+// of a kv head (x); thread (four, query).  Sixteen splits' loads are in flight at
+// once: latency, 6.5 us for 32 queries of 13 splits (11.4 with eight, after a pass over
+// the maxima), 8 to 10 for 1024.
 template <int D>
 __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
                                                      float *__restrict__ ws)
