@@ -485,7 +485,8 @@ int64_t corun_beam_select_workspace(int32_t vocab, int32_t groups, int32_t beams
  *             [keep, capacity], held or a held page outside the table or cache.
  *             Unless 0, nothing else is written.
  *  ws         at least corun_pages_workspace bytes
- * n_slots and num_pages at most 2^20, n_slots max_pages_per_seq at most 2^28. */
+ * n_slots and num_pages at most 2^20, n_slots max_pages_per_seq at most 2^28, a
+ * page's keys of one layer at most 2^35 bytes. */
 corun_status corun_pages_assign(const corun_kv *kv, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
                                 int32_t *page_table, int32_t *held, const int32_t *src, const int32_t *keep,
                                 const int32_t *hold, int32_t *status, void *ws, int64_t ws_bytes, void *stream);

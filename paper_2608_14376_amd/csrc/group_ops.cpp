@@ -100,6 +100,8 @@ corun_status pages_call(const corun_kv *kv, int32_t n_layers, int32_t n_kv_heads
 {
     TRY(check_pages(kv));
     TRY(check_heads(kv, n_kv_heads, n_kv_heads, head_dim));
+    const int64_t page_bytes = (int64_t)n_kv_heads * kv->page_size * head_dim * (kv->dtype == CORUN_KV_E4M3 ? 1 : 2);
+    if (page_bytes > 1ll << 35) return set_error(CORUN_E_SHAPE, "a page above 2^35 bytes of a layer's keys");
     if (n_layers < 1) return set_errorf(CORUN_E_INVAL, "n_layers %d", n_layers);
     for (int l = 0; l < n_layers; ++l) {
         CacheLayer cl;

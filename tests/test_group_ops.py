@@ -58,7 +58,7 @@ def compact(kv, layers=1, nkv=2, d=128, table=P, held=P, status=P, ws=P, ws_byte
     (dict(scales=None), {}, corun.E_INVAL), (dict(table=None), dict(table=None), corun.E_INVAL),
     ({}, dict(table=P + 64), corun.E_INVAL), ({}, dict(table=None), corun.E_INVAL), ({}, dict(held=None), corun.E_INVAL),
     ({}, dict(status=None), corun.E_INVAL), ({}, dict(layers=0), corun.E_INVAL), ({}, dict(d=96), corun.E_SHAPE),
-    ({}, dict(nkv=0), corun.E_SHAPE), ({}, dict(ws=None), corun.E_INVAL), ({}, dict(ws=P + 8), corun.E_INVAL),
+    ({}, dict(nkv=0), corun.E_SHAPE), (dict(page_size=1 << 20), dict(nkv=512), corun.E_SHAPE), ({}, dict(ws=None), corun.E_INVAL), ({}, dict(ws=P + 8), corun.E_INVAL),
     ({}, dict(ws_bytes=16), corun.E_CAPACITY),
 ])
 def test_pages_refusals(kv, kw, status):
