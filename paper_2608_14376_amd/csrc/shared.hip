@@ -900,10 +900,14 @@ __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt
         f32x2 ml[PF];
 #pragma unroll
         for (int j = 0; j < PF; ++j) {
-            const int i = min(i0 + j, parts - 1);
-            const float *b = base + (size_t)(i < np ? i : s.splits_p + i - np) * split;
-            x[j] = *(const f32x4 *)(b + (d4 * 32 + u32) * 4);
-            ml[j] = *(const f32x2 *)(b + 32 * D + 2 * u32);
+            const int i = i0 + j;
+            x[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            ml[j] = (f32x2){-INFINITY, 0.f};
+            if (i < parts) {
+                const float *b = base + (size_t)(i < np ? i : s.splits_p + i - np) * split;
+                x[j] = *(const f32x4 *)(b + (d4 * 32 + u32) * 4);
+                ml[j] = *(const f32x2 *)(b + 32 * D + 2 * u32);
+            }
         }
         float m = M;
 #pragma unroll
@@ -914,11 +918,9 @@ __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt
         o *= down;
 #pragma unroll
         for (int j = 0; j < PF; ++j) {
-            if (i0 + j < parts) {
-                const float f = __builtin_amdgcn_exp2f(ml[j].x - off);
-                L += ml[j].y * f;
-                o += x[j] * f;
-            }
+            const float f = __builtin_amdgcn_exp2f(ml[j].x - off);   // 0 past the last split
+            L += ml[j].y * f;
+            o += x[j] * f;
         }
     }
     const float inv = 1.0f / L;
@@ -965,7 +967,7 @@ SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, i
     // several, some may be shorter than the longest, and workgroups of many tokens then
     // end late (four of 11 to 30 thousand tokens: 159 us with splits of 1664, 238 of
     // 7424; eight of 500 to 8000: 60 of 1024, 71 of 2048).
-    s.chunk_p = chunk(max_prefix, (long long)s.tiles * nkv, 256, g.n == 1 ? 1 << 30 : std::max(1024, max_prefix / 16));
+    s.chunk_p = chunk(max_prefix, (long long)s.tiles * nkv, 256, g.n == 1 ? 1 << 30 : std::max(1024, max_prefix / 15));
     s.splits_p = (int)(((long long)max_prefix + s.chunk_p - 1) / s.chunk_p);
     const long long suffix = (long long)max_suffix + 15;
     s.chunk_s = chunk(suffix, (long long)g.row0[g.n] * nkv, 2048, 1 << 30);

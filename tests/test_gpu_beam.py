@@ -137,6 +137,25 @@ def test_wide_groups_of_equal_logits(V, beams):
     check(select(x, s, beams, 64), gref.beam_select(x, s, beams, 64))
 
 
+def test_the_most_rows():
+    rows, V = 65535, 5
+    x = torch.randn((rows, V), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    tok, par = (torch.empty((rows, 2), dtype=torch.int32, device=DEV) for _ in range(2))
+    sc = torch.empty((rows, 2), device=DEV)
+    ws = torch.empty(corun.beam_select_workspace(V, rows, 1, 2), dtype=torch.uint8, device=DEV)
+    corun.beam_select(x, torch.zeros(rows, device=DEV), 1, tok, par, sc, ws)
+    top = x.topk(2, 1)
+    lp = torch.log_softmax(x.double(), 1).gather(1, top.indices)
+    assert torch.equal(tok.long(), top.indices) and torch.equal(par[:, 0], torch.arange(rows, dtype=torch.int32, device=DEV))
+    assert ((sc.double() - lp).abs() <= 2.0**-24 * lp.abs() * (1 + 1e-6)).all()
+
+
+def test_the_widest_vocabulary_and_group():
+    V, beams = 1 << 19, 64
+    x, s = logits_of(beams, V, 12)
+    check(select(x, s, beams, 64), gref.beam_select(x, s, beams, 64))
+
+
 def test_logits_of_any_size():
     rng = np.random.default_rng(4)
     x = rng.standard_normal((6, 12000)).astype(np.float32)

@@ -128,6 +128,45 @@ def test_long_prefixes(dtype, blk, page, groups, prefix, suffix):
         assert not torch.isnan(out).any()
 
 
+@pytest.mark.parametrize("dtype,nq,P,S,rows", [("bf16", 4, 70000, 50000, 2), ("e4m3", 8, 3, 100000, 1), ("e4m3", 16, 90000, 100, 8)])
+def test_very_long(dtype, nq, P, S, rows):
+    """More tokens than 256 splits of the shortest chunk hold, of prefixes and of a row's own."""
+    d, nkv = 64, 1
+    cap = -(-(P + S) // 16) * 16
+    hc = HostCache(nkv, d, rows + 1, cap, 16, 0, seed=6, dtype=dtype)
+    q, qd = rows_of(rows, nq, d, 14)
+    lens = [P + S - 3 * r for r in range(rows)]
+    out = run(hc.device_cache(corun), qd, [rows], lens, [P], [rows])
+    check(hc, q, out, [rows], lens, [P], [rows], rows=sorted({0, rows - 1}))
+
+
+@pytest.mark.parametrize("nq", [2, 16])
+def test_the_most_rows_and_groups(nq):
+    """65535 rows in 256 groups, of one query head to a kv head and of sixteen: every row against torch in fp32 (its sums of
+    32 terms are off by under 2^-18 of the weighted sizes, beside the result's own rounding)."""
+    nkv, d = (2, 64) if nq == 2 else (1, 64)
+    groups = [256] * 255 + [255]
+    rows = sum(groups)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn((rows, nkv, 32, d), generator=g, device=DEV).bfloat16() for _ in range(2))
+    cache = corun.KvCache([k], [v])
+    q = torch.randn((rows, nq * d), generator=g, device=DEV).bfloat16()
+    lens = torch.randint(16, 33, (rows,), generator=g, device=DEV, dtype=torch.int32)
+    first = torch.arange(256, device=DEV, dtype=torch.int32) * 256
+    ws = torch.empty(corun.shared_attention_workspace(cache, groups, nq), dtype=torch.uint8, device=DEV)
+    out = torch.zeros_like(q)
+    corun.shared_attention(cache, 0, q, groups, lens, torch.full_like(first, 16), out, ws, prefix_slots=first.flip(0).contiguous())
+    of = torch.arange(rows, device=DEV) // 256
+    at = first.flip(0).long()[of]
+    kk, vv = (torch.cat([t[at][:, :, :16], t[:, :, 16:]], 2).float() for t in (k, v))
+    s = (q.float().view(rows, nkv, nq // nkv, d) @ kk.transpose(2, 3).contiguous()) / 8.0
+    s = s.masked_fill((torch.arange(32, device=DEV)[None, :] >= lens[:, None])[:, None, None], -float("inf"))
+    p = torch.softmax(s, -1)
+    want, pv = (p @ vv).view(rows, -1), (p @ vv.abs()).view(rows, -1)
+    tol = ref.U_BF16 * (want.abs() + 2.0**-13 * pv) + (2.0**-13 + 2.0**-18) * pv
+    assert ((out.float() - want).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_prefix_in_the_first_rows_slot(dtype):
     groups, prefix = [3, 2], [90, 33]
