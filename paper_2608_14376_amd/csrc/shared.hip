@@ -473,7 +473,7 @@ __device__ __forceinline__ void emit_part(float *part, int u, int d4, const floa
 // 2^-32 of it becomes zero, and the sum, of the weights before they are rounded,
 // takes the scales out again.  A split with a scale more than 2^NEAR from its
 // first, where 32 bits may not hold that sum, is left to attend_few.  (Four documents
-// of 11 to 30 thousand tokens, 80 rows of 64 heads: 139 us, 156 with two halves.)
+// of 11 to 30 thousand tokens, 80 rows of 64 heads: 134 us, 17 more with two halves.)
 //
 // Bound by a wavefront's products and softmax in turn: 128 rows of 64 heads behind
 // 32768 tokens take 203 us (e4m3, 0.68 PFLOP/s) or 250 (bf16, 0.55; its second
