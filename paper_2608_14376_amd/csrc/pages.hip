@@ -124,11 +124,12 @@ __device__ __forceinline__ int from_before(int x)
     return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
 
-// Sums of the workgroup's values before the caller's (exclusive), and of all, by
-// wavefronts of 64 in order.
+// Sums of the workgroup's values before the caller's (exclusive), and of all, by its
+// sixteen wavefronts in order.  One barrier: calls take two lds in turn, so that
+// whoever still reads one has not reached the barrier before it is written again.
 __device__ __forceinline__ int before(int v, int *all, int *lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int x = v;
     x += from_before<0x111, 0xf>(x);
     x += from_before<0x112, 0xf>(x);
@@ -136,11 +137,11 @@ __device__ __forceinline__ int before(int v, int *all, int *lds)
     x += from_before<0x118, 0xf>(x);
     x += from_before<0x142, 0xa>(x);                   // rows 1 and 3
     x += from_before<0x143, 0xc>(x);                   // rows 2 and 3
-    __syncthreads();                                  // lds is free
     if (lane == 63) lds[wave] = x;
     __syncthreads();
     int sum = 0, mine = 0;
-    for (int w = 0; w < waves; ++w) {
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
         mine += w < wave ? lds[w] : 0;
         sum += lds[w];
     }
@@ -148,11 +149,31 @@ __device__ __forceinline__ int before(int v, int *all, int *lds)
     return mine + x - v;
 }
 
+// The most of values >= 0 over the workgroup's sixteen wavefronts: noted, and read
+// after a barrier.
+__device__ __forceinline__ void note_most(int v, int *lds)
+{
+    v = max(v, from_before<0x111, 0xf>(v));
+    v = max(v, from_before<0x112, 0xf>(v));
+    v = max(v, from_before<0x114, 0xf>(v));
+    v = max(v, from_before<0x118, 0xf>(v));
+    v = max(v, from_before<0x142, 0xa>(v));
+    v = max(v, from_before<0x143, 0xc>(v));
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
+}
+__device__ __forceinline__ int most_of(const int *lds)
+{
+    int v = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) v = max(v, lds[w]);
+    return v;
+}
+
 // Assignment: deals the free pages.  One workgroup.
 __global__ __launch_bounds__(1024) void k_pages_plan(PageShape s, Plan p, const int32_t *__restrict__ keep,
                                                      int32_t *status)
 {
-    __shared__ int lds[16];
+    __shared__ int lds[2][16];
     const int tid = threadIdx.x;
     if (p.head[BAD]) {
         if (tid == 0) *status = p.head[STATUS] = -1;
@@ -171,9 +192,9 @@ __global__ __launch_bounds__(1024) void k_pages_plan(PageShape s, Plan p, const 
             fresh = p.total[r] - have;
         }
         int all;
-        const long long at = need + before(fresh, &all, lds);
+        const long long at = need + before(fresh, &all, lds[0]);
         need += all;
-        const int c = copies + before(copy, &all, lds);
+        const int c = copies + before(copy, &all, lds[1]);
         copies += all;
         if (r < s.slots) {
             p.fresh0[r] = (int)(at < INT_MAX ? at : INT_MAX);
@@ -187,11 +208,11 @@ __global__ __launch_bounds__(1024) void k_pages_plan(PageShape s, Plan p, const 
         }
     }
     long long found = 0;
-    for (int i0 = 0; i0 < s.pages && found < need; i0 += 1024) {
+    for (int i0 = 0, b = 0; i0 < s.pages && found < need; i0 += 1024, b ^= 1) {
         const int i = i0 + tid;
         const int free = i < s.pages && p.mark[i] == FREE;
         int all;
-        const int at = (int)found + before(free, &all, lds);
+        const int at = (int)found + before(free, &all, lds[b]);
         if (free) p.list[at] = i;
         found += all;
     }
@@ -228,7 +249,7 @@ __global__ __launch_bounds__(256) void k_pages_held(PageShape s, Plan p, const i
 // order.  One workgroup.
 __global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int32_t *status)
 {
-    __shared__ int lds[16];
+    __shared__ int lds[3][16];
     const int tid = threadIdx.x;
     if (p.head[BAD]) {
         if (tid == 0) *status = p.head[STATUS] = -1;
@@ -236,21 +257,21 @@ __global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int
     }
     int mine = 0, n;
     for (int i = tid; i < s.pages; i += 1024) mine += p.mark[i] != FREE;
-    before(mine, &n, lds);
-    int high = 0, low = 0;
+    before(mine, &n, lds[2]);
+    int high = 0, low = 0, b = 0;
     for (int i0 = 0; i0 < s.pages; i0 += 1024) {
         const int i = i0 + tid;
         const bool used = i < s.pages && p.mark[i] != FREE;
         int all;
         if (i0 < n) {
             const bool hole = i < n && !used;
-            const int at = low + before(hole, &all, lds);
+            const int at = low + before(hole, &all, lds[b ^= 1]);
             if (hole) p.to[at] = i;
             low += all;
         }
         if (i0 + 1024 > n) {
             const bool moves = i >= n && used;
-            const int at = high + before(moves, &all, lds);
+            const int at = high + before(moves, &all, lds[b ^= 1]);
             if (moves) p.from[at] = i;
             high += all;
         }
@@ -272,18 +293,6 @@ __global__ __launch_bounds__(1024) void k_pages_squeeze(PageShape s, Plan p, int
 // The whole plan, and the table, of a small pool: one workgroup, marks in LDS.
 constexpr int SMALL_PAGES = 8192, SMALL_SLOTS = 1024, SMALL_TABLE = 1 << 17, SPARE = 512;
 
-// The most of a value over the workgroup, whose threads all call.
-__device__ __forceinline__ int most_of(int v, int *lds)
-{
-    __syncthreads();
-    if (threadIdx.x == 0) *lds = 0;
-    __syncthreads();
-    for (int o = 32; o; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-    if ((threadIdx.x & 63) == 0) atomicMax(lds, v);
-    __syncthreads();
-    return *lds;
-}
-
 // Calls f(slot, i) for i < n, slot < slots, over the workgroup.
 template <class F>
 __device__ __forceinline__ void over_rows(int slots, int n, F &&f)
@@ -301,7 +310,7 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
 {
     extern __shared__ int mark[];                      // [pages]
     __shared__ int from[SMALL_SLOTS], first[SMALL_SLOTS], taken[SMALL_SLOTS], total[SMALL_SLOTS], tail[SMALL_SLOTS],
-        fresh0[SMALL_SLOTS], has[SMALL_SLOTS], spare[SPARE], lds[16], bad, most;
+        fresh0[SMALL_SLOTS], has[SMALL_SLOTS], spare[SPARE], lds[2][16], most[2][16], bad;
     const int tid = threadIdx.x, r = tid;
     const bool slot = r < s.slots;
     // one thread to a slot
@@ -330,8 +339,10 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
         taken[r] = take = first[r] + (n > first[r] * s.page_size);
         total[r] = (int)(((long long)m + s.page_size - 1) / s.page_size);
     }
-    const int span = most_of(take, &most);
     if (wrong) bad = 1;
+    note_most(take, most[0]);
+    __syncthreads();
+    const int span = most_of(most[0]);
     // entries that are taken: page i of slot r.  Few of them stay in registers.
     const bool few = s.slots * span <= 4096;
     int kept[4];
@@ -376,9 +387,17 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
         have = first[r] + stays;
         fresh = total[r] - have;                       // the table's entries bound the sum
     }
-    const int at = before(fresh, &need, lds), c = before(copy, &copies, lds);
+    note_most(fresh, most[1]);
+    static_assert(SMALL_TABLE < 1 << 18 && SMALL_SLOTS < 1 << 13, "both counts in one word");
+    const int both = before(fresh | copy << 18, &need, lds[0]), at = both & 0x3ffff, c = both >> 18;
+    copies = need >> 18;
+    need &= 0x3ffff;
+    if (slot) {
+        first[r] = have;
+        fresh0[r] = at;
+    }
     int found = 0;
-    for (int i0 = 0; i0 < s.pages && found < need; i0 += 4096) {
+    for (int i0 = 0, b = 1; i0 < s.pages && found < need; i0 += 4096, b ^= 1) {
         const int i = i0 + 4 * tid;
         bool free[4];
         int mine = 0, all;
@@ -387,7 +406,7 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
             free[e] = i + e < s.pages && mark[i + e] == FREE;
             mine += free[e];
         }
-        int k = found + before(mine, &all, lds);
+        int k = found + before(mine, &all, lds[b]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (free[e]) {
@@ -397,20 +416,16 @@ __global__ __launch_bounds__(1024) void k_pages_small(PageShape s, Plan p, int32
             }
         found += all;
     }
-    const int left = need > found ? need - found : 0, more = most_of(fresh, &most);
+    __syncthreads();
+    const int left = need > found ? need - found : 0, more = most_of(most[1]);
     if (left == 0) {
         const auto dealt = [&](int k) { return k < SPARE ? spare[k] : p.list[k]; };
-        if (slot) {
-            first[r] = have;
-            fresh0[r] = at;
-            held[r] = total[r];
-        }
+        if (slot) held[r] = total[r];
         if (copy) {
             p.from[c] = t;
             p.to[c] = dealt(at);
             p.count[c] = (n % s.page_size + s.block - 1) / s.block;
         }
-        __syncthreads();
         if (few) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -436,16 +451,21 @@ __global__ __launch_bounds__(1024) void k_pages_small_squeeze(PageShape s, Plan 
                                                               const int32_t *__restrict__ held, int32_t *status)
 {
     extern __shared__ int mark[];                      // [pages], then their new numbers
-    __shared__ int has[SMALL_SLOTS], lds[16], bad, most;
+    __shared__ int has[SMALL_SLOTS], lds[3][16], most[16], bad;
     const int tid = threadIdx.x;
     int h = tid < s.slots ? held[tid] : 0;
     const bool wrong = h < 0 || h > s.width;
     if (wrong) h = 0;
     if (tid < s.slots) has[tid] = h;
-    if (tid == 0) bad = 0;
     for (int i = tid; i < s.pages; i += 1024) mark[i] = FREE;
-    const int span = most_of(h, &most);
-    if (wrong) bad = 1;
+    note_most(wrong ? s.width + 1 : h, most);
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    const int span = most_of(most);
+    if (span > s.width) {                              // a count outside the table, the same for all threads
+        if (tid == 0) *status = p.head[STATUS] = -1;
+        return;
+    }
     over_rows(s.slots, span, [&](int r, int i) {
         if (i >= has[r]) return;
         const int page = table[(size_t)r * s.width + i];
@@ -459,14 +479,14 @@ __global__ __launch_bounds__(1024) void k_pages_small_squeeze(PageShape s, Plan 
     }
     int mine = 0, n;
     for (int i = tid; i < s.pages; i += 1024) mine += mark[i] != FREE;
-    before(mine, &n, lds);
+    before(mine, &n, lds[2]);
     int high = 0, low = 0;
-    for (int i0 = 0; i0 < s.pages; i0 += 1024) {
+    for (int i0 = 0, b = 0; i0 < s.pages; i0 += 1024, b ^= 1) {
         const int i = i0 + tid;
         const bool used = i < s.pages && mark[i] != FREE;
         const int hole = i < n && !used, moves = i >= n && used;
         int all;
-        const int at = before(hole | moves << 16, &all, lds);   // at most 1024 of each
+        const int at = before(hole | moves << 16, &all, lds[b]);   // at most 1024 of each
         if (hole) p.to[low + (at & 0xffff)] = i;
         if (moves) p.from[high + (at >> 16)] = i;
         low += all & 0xffff;
