@@ -349,7 +349,7 @@ __device__ __forceinline__ bool better(const Candidate &x, const Candidate &y)
 template <int T>
 __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
 {
-    constexpr int W = T / 64, LPT = 4, ROOM = MOST, NEAR = 8;
+    constexpr int W = T / 64, LPT = 4, ROOM = MOST, NEAR = 8, HELD = 5;
     __shared__ double lse[MOST_BEAMS], score[MOST_BEAMS], weight[MOST_BEAMS];
     __shared__ int kind[MOST_BEAMS], wn[2][W], wi[W], count, selected, longer;
     __shared__ uint32_t wlo[W], whi[W];
@@ -378,12 +378,28 @@ __global__ __launch_bounds__(T) void k_beam_pick(BeamArgs a, Best b, int parts)
         int k = row_kind(a, r);
         const double w = a.weights == nullptr ? 1.0 : (double)a.weights[r];
         const float s = a.scores[r];
-        float most = -INFINITY;
-        for (int p = l16; p < parts; p += 16) most = fmaxf(most, top[p]);
+        float most = -INFINITY, t0[HELD];
+        double x0[HELD];
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            const int p = l16 + 16 * j;
+            t0[j] = -INFINITY;
+            x0[j] = 0;
+            if (p < parts) {
+                t0[j] = top[p];
+                x0[j] = sum[p];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) most = fmaxf(most, t0[j]);
+        for (int p = l16 + 16 * HELD; p < parts; p += 16) most = fmaxf(most, top[p]);
         most = over_row(most, [](float x, float y) { return x > y ? x : y; });
         double total = 0;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j)
+            if (16 * j < parts) total += t0[j] > -INFINITY || x0[j] != x0[j] ? x0[j] * exp_under(t0[j], most) : 0.0;
 #pragma unroll 2
-        for (int p = l16; p < parts; p += 16) {
+        for (int p = l16 + 16 * HELD; p < parts; p += 16) {
             const float t = top[p];
             const double x = sum[p];
             total += t > -INFINITY || x != x ? x * exp_under(t, most) : 0.0;
