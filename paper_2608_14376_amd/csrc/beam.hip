@@ -20,8 +20,9 @@
 // the part's other wavefronts.  Parts of 4096 columns came out the same (39 us), a
 // workgroup that loads its next part while it works on this one slower (58 us for
 // the whole call, 47 so): its registers leave fewer wavefronts.
-// k_beam_pick: 7 us for 64 groups of 4 rows and 4 results, 12 for 4 groups of 32 rows
-// and 64 results: a chain of dependent loads and barriers.
+// k_beam_pick: 7 us for 64 groups of 4 rows and 4 results, 11 for 4 groups of 32 rows
+// and 64 results: a chain of dependent loads and barriers.  A lane's first five parts
+// are read at once (75 parts to a row: 6.5 us, 8.1 with two at a time).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -868,8 +868,8 @@ __global__ __launch_bounds__(256, 2) void k_shared_alone(SharedArgs a, GroupTabl
 
 // Joins the splits: a workgroup takes four dimension fours (y) of a 32-query block
 // of a kv head (x); thread (four, query).  Sixteen splits' loads are in flight at
-// once: latency, 6.5 us for 32 queries of 13 splits (11.4 with eight, after a pass over
-// the maxima), 8 to 10 for 1024.
+// once: latency, 4.5 us for 32 queries of 13 splits, 8 to 10 for 1024 (with eight, after a
+// pass over the maxima, 11.4 for the 32).
 template <int D>
 __global__ __launch_bounds__(128) void k_shared_join(SharedArgs a, GroupTable gt, Shape s, CacheView cv,
                                                      float *__restrict__ ws)
@@ -955,7 +955,8 @@ SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, i
     s.qb0[g.n] = (uint16_t)s.blocks;
     s.tile0[g.n] = (uint16_t)s.tiles;   // rows bound all of them
     // Tokens of a split: about `wgs` workgroups in all, splits of at least 256 tokens
-    // and of at most `longest`, 256 splits at most.
+    // (8 rows behind 4000 in bf16: 17 us, 18.6 with 128) and of at most `longest`, 256
+    // splits at most.
     const auto chunk = [](long long tokens, long long units, long long wgs, long long longest) {
         long long n = std::max<long long>(1, wgs / std::max<long long>(1, units));
         n = std::min<long long>(std::max(std::min(n, (tokens + 255) / 256), (tokens + longest - 1) / longest), 256);

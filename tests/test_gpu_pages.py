@@ -80,7 +80,8 @@ SHAPES = [dict(), dict(blk=0), dict(blk=0, ps=48, d=128, nkv=1), dict(blk=64, ps
           dict(slots=70, width=3, pages=300, layers=1), dict(slots=1, width=1, pages=1, layers=1),
           dict(pages=9000, ps=16, nkv=1, layers=1), dict(pages=8193, ps=32, blk=0, nkv=1, layers=1, width=40),
           dict(pages=8192, ps=16, nkv=1, layers=1, width=300, slots=20), dict(slots=3, width=44000, pages=300, ps=16, layers=1, nkv=1),
-          dict(slots=1500, width=40, pages=12000, ps=16, layers=1, nkv=1, blk=0), dict(slots=3, width=700, pages=2300, ps=16, layers=1, nkv=1), dict(slots=1100, width=2, pages=2600, ps=16, layers=1, nkv=1)]
+          dict(slots=1500, width=40, pages=12000, ps=16, layers=1, nkv=1, blk=0),
+          dict(slots=3, width=700, pages=2300, ps=16, layers=1, nkv=1), dict(slots=1100, width=2, pages=2600, ps=16, layers=1, nkv=1)]
 
 
 @pytest.mark.parametrize("kw", SHAPES)
