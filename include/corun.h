@@ -530,10 +530,7 @@ int64_t corun_pages_workspace(const corun_kv *kv);
  * lens[r] outside [prefix_lens[g], prefix_lens[g] + max_suffix] or above the
  * capacity, or where a page that the row sees is outside [0, num_pages).  A value of
  * a bf16 cache that is infinite makes the results that see it infinite or NaN.
- * Weights have about 16 bits; over prefixes of e4m3 caches, where a group has more
- * than 32 query heads to a kv head, 11, and one whose product with its value's
- * scale is below 2^-32 of the row's largest there counts for the softmax's sum
- * alone. */
+ * Weights have about 16 bits. */
 corun_status corun_shared_attention(const corun_kv *kv, int32_t layer, int32_t n_heads, int32_t n_kv_heads,
                                     int32_t head_dim, int32_t n_groups, const int32_t *group_rows, const void *q,
                                     int64_t ld_q, const uint8_t *valid, const int32_t *lens,

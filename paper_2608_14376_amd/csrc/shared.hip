@@ -12,9 +12,9 @@
 // call's sizes and a row's lengths alone, and a query's arithmetic does not depend
 // on its place in a tile, so rows stay position-invariant.
 //
-// Weights enter the matrix units as two bf16 halves, hi + lo (about 16 bits), or, over
-// many queries of an e4m3 cache, as fp16; bf16 values and the codes of an e4m3
-// cache times their scale are exact there.
+// Weights enter the matrix units as two bf16 halves, hi + lo: about 16 bits, however
+// small a weight is, for a value may be met by small ones alone.  bf16 values and the
+// codes of an e4m3 cache times their scale are exact there.
 //
 // The rows' own tokens are bound by reading (228 rows of 1024 bf16 tokens of 8 kv
 // heads of 128: 5.1 TB/s, a large copy's rate), the prefixes by the products and
@@ -26,7 +26,6 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "device.h"
 #include "groups.h"
@@ -465,52 +464,28 @@ __device__ __forceinline__ void emit_part(float *part, int u, int d4, const floa
 //    each step s of 16 keys: the operand P^T of
 //  * O^T += V^T P^T, V^T by transposed reads.
 //
-// HALF, e4m3 caches: the second product in fp16, one instead of two.  The values
-// are the bare codes, and a weight carries the scale of its 16 tokens, whose
-// exponent costs nothing where the score's is added to it: 2^(s + b - ref + UP), b
-// the scale's exponent less that of the split's first, and ref following the
-// maximum of s + b.  They keep 11 bits down to 2^-22 of the largest, what is below
-// 2^-32 of it becomes zero, and the sum, of the weights before they are rounded,
-// takes the scales out again.  A split with a scale more than 2^NEAR from its
-// first, where 32 bits may not hold that sum, is left to attend_few.  (Four documents
-// of 11 to 30 thousand tokens, 80 rows of 64 heads: 134 us, 17 more with two halves.)
-//
-// Bound by a wavefront's products and softmax in turn: 128 rows of 64 heads behind
-// 32768 tokens take 203 us (e4m3, 0.68 PFLOP/s) or 250 (bf16, 0.55; its second
-// product is done twice).  A SIMD's two wavefronts hardly overlap the two: with two
-// products, of the time that a CU was busy the matrix units took 43% and the vector
-// units 55%.  Raising a wavefront's priority around its products changed nothing;
-// tiles of 32 tokens, whose registers and LDS let three workgroups on a CU, took 231
-// and 279 us.
+// Bound by a wavefront's products and softmax in turn: a call of 128 rows of 64
+// heads behind 32768 tokens takes 273 us (e4m3, 0.50 PFLOP/s; its conversions come on
+// top) or 259 (bf16, 0.53); the second product is done twice, for the weights' halves.
+// A SIMD's two wavefronts hardly overlap products and softmax: of the time that a CU
+// was busy the matrix units took 43% and the vector units 55%.  One fp16 product over
+// e4m3 values was 70 us faster there and is not used: a weight far below the largest
+// lost its bits, and with them values that the largest ones do not meet.  Raising a
+// wavefront's priority around its products changed nothing; tiles of 32 tokens, whose
+// registers and LDS let three workgroups on a CU, took 279 us for bf16 where this took
+// 250.
 // ---------------------------------------------------------------------------
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-constexpr int UP = 8, NEAR = 24;
-
-// Eight codes in fp16: exact.
-__device__ __forceinline__ uint4 codes8_half(uint32_t w0, uint32_t w1)
-{
-    uint4 o;
-    o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, false));
-    o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, true));
-    o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, false));
-    o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, true));
-    return o;
-}
-
 template <int KCH>
 __device__ __forceinline__ int val16_swz(int t) { return vtile_swz<KCH>(t) ^ (t & 1); }
 
 template <int D>
 constexpr int many_lds() { return 4 * 64 * D * 2; }
 
-// False: the scales are too far apart for HALF, and nothing has been written.
 template <int D, bool E4, bool PAGED, class QueryOf>
-__device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lost, const CacheView &cv,
-                                            const CacheLayer &layer, int nkv, int kvh, int slot, int t0, int t_end,
-                                            int queries, QueryOf &&query, float *part)
+__device__ __forceinline__ void attend_many(char *lds, int *lost, const CacheView &cv, const CacheLayer &layer, int nkv,
+                                            int kvh, int slot, int t0, int t_end, int queries, QueryOf &&query,
+                                            float *part)
 {
-    constexpr bool HALF = E4;
     constexpr int EB = E4 ? 1 : 2, RB = D * EB, RU = RB / 16;        // a row's bytes and 16-byte units in the cache
     constexpr int NR = 16 * RB / 1024, KCH = D / 8, UNITS = 64 * KCH, DT = D / 32, KS = D / 16;
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, h = lane >> 5;
@@ -572,6 +547,7 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
     auto store = [&](int k0, int b) {
         uint4 *K = ring + b * UNITS, *V = ring + (2 + b) * UNITS;
         const float ksc = __uint_as_float(__builtin_amdgcn_readfirstlane(ks8) << 23);
+        const float vsc = __uint_as_float(__builtin_amdgcn_readfirstlane(vs8) << 23);
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
             const int u = 64 * j + lane, row = 16 * wave + u / RU, c = u % RU;
@@ -582,10 +558,9 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
             }
             K[pf_swz<KCH>(row, 2 * c)] = codes8(kraw[j].x, kraw[j].y, ksc);
             K[pf_swz<KCH>(row, 2 * c + 1)] = codes8(kraw[j].z, kraw[j].w, ksc);
-            V[row * KCH + ((2 * c) ^ val16_swz<KCH>(row))] = codes8_half(w.x, w.y);
-            V[row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row))] = codes8_half(w.z, w.w);
+            V[row * KCH + ((2 * c) ^ val16_swz<KCH>(row))] = codes8(w.x, w.y, vsc);
+            V[row * KCH + ((2 * c + 1) ^ val16_swz<KCH>(row))] = codes8(w.z, w.w, vsc);
         }
-        if (lane == 0) scales[b][wave] = k0 + 16 * wave < t_end ? (int)vs8 : -1;
     };
     // bf16: straight to buffer b; values past the end are cleared once they have landed
     auto direct = [&](int b) {
@@ -612,7 +587,6 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[dt][j] = 0.f;
     float mrow = -INFINITY, lpart = 0.f;
-    int byte0 = -1;                                    // HALF: the split's first scale
     const float scale2 = 1.4426950408889634f / sqrtf((float)D);
     const int krow = pf_key_of_row(r32), a4 = lane & 3, qv = (lane >> 2) & 3, half16 = (lane >> 4) & 1;
 
@@ -642,21 +616,6 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
                 direct(b ^ 1);
             }
             fetch_page();
-        }
-        float be[4];                                   // HALF: exponents of the groups' scales, less byte0's
-        if constexpr (HALF) {
-            if (byte0 < 0) byte0 = scales[b][0];
-            bool near = true;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int x = scales[b][g], e = x < 0 ? 0 : x - byte0;
-                near &= e >= -NEAR && e <= NEAR;
-                be[g] = (float)e;
-            }
-            if (__ballot(!near)) {                     // the same for all wavefronts
-                __syncthreads();
-                return false;
-            }
         }
         if (!active) continue;
         const uint4 *Kt = ring + b * UNITS, *Vt = ring + (2 + b) * UNITS;
@@ -695,15 +654,12 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
         }
         float mt = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            float mg = -INFINITY;
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) mg = fmaxf(mg, st[g / 2][8 * (g % 2) + j]);
-            mt = fmaxf(mt, HALF ? __builtin_fmaf(mg, scale2, be[g]) : mg * scale2);
-        }
+            for (int j = 0; j < 16; ++j) mt = fmaxf(mt, st[kt][j]);
         const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(mt), __float_as_uint(mt), false, false);
-        mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1]));   // both halves of the query's keys
-        const float mnew = mt > mrow + LAG ? mt : mrow, moff = (mnew == -INFINITY ? 0.f : mnew) - (HALF ? UP : 0);
+        mt = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * scale2;   // both halves of the query's keys
+        const float mnew = mt > mrow + LAG ? mt : mrow, moff = mnew == -INFINITY ? 0.f : mnew;
         if (__ballot(mnew != mrow)) {
             const float alpha = mnew == mrow ? 1.f : __builtin_amdgcn_exp2f(mrow - mnew);
             lpart *= alpha;
@@ -713,34 +669,27 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
                 for (int j = 0; j < 16; ++j) acc[dt][j] *= alpha;
             mrow = mnew;
         }
-        uint4 ph[4], pl[HALF ? 1 : 4];
+        bf16x8 ph[4], pl[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             uint32_t hi[4], lo[4];
             float ls = 0.f;
-            const float at = HALF ? be[s] - moff : -moff;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e], scale2, at));
-                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e + 1], scale2, at));
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e], scale2, -moff));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s / 2][8 * (s % 2) + 2 * e + 1], scale2, -moff));
                 ls += x + y;
-                if constexpr (HALF) {
-                    typedef float f32x2_t __attribute__((ext_vector_type(2)));
-                    hi[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){x, y}, f16x2));
-                } else {
-                    const uint32_t w = f2bf2(x, y);
-                    hi[e] = w;
-                    lo[e] = f2bf2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
-                }
+                const uint32_t w = f2bf2(x, y);
+                hi[e] = w;
+                lo[e] = f2bf2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
             }
-            ph[s] = (uint4){hi[0], hi[1], hi[2], hi[3]};
-            if constexpr (!HALF) pl[s] = (uint4){lo[0], lo[1], lo[2], lo[3]};
-            // the scale out of the sum again: times 2^-be
-            lpart = HALF ? __builtin_fmaf(ls, __uint_as_float((uint32_t)(127 - (int)be[s]) << 23), lpart) : lpart + ls;
+            ph[s] = __builtin_bit_cast(bf16x8, hi);
+            pl[s] = __builtin_bit_cast(bf16x8, lo);
+            lpart += ls;
         }
         // operand f: step f / DT of 16 keys, dimensions 32 (f % DT) + l % 32
         constexpr int VD = 3;
-        uint4 vf[VD + 1];
+        bf16x8 vf[VD + 1];
         auto vread = [&](int f) {
             uint2 w[2];
 #pragma unroll
@@ -748,7 +697,7 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
                 const int key = 16 * (f / DT) + 8 * h + 4 * r + qv, c = 4 * (f % DT) + 2 * half16 + (a4 >> 1);
                 w[r] = lds_read_tr16((const char *)(Vt + key * KCH + (c ^ val16_swz<KCH>(key))) + 8 * (a4 & 1));
             }
-            vf[f % (VD + 1)] = (uint4){w[0].x, w[0].y, w[1].x, w[1].y};
+            vf[f % (VD + 1)] = __builtin_bit_cast(bf16x8, (uint4){w[0].x, w[0].y, w[1].x, w[1].y});
         };
 #pragma unroll
         for (int f = 0; f < VD; ++f) vread(f);
@@ -756,33 +705,24 @@ __device__ __forceinline__ bool attend_many(char *lds, int (*scales)[4], int *lo
         for (int f = 0; f < 4 * DT; ++f) {
             if (f + VD < 4 * DT) vread(f + VD);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (HALF) {
-                acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vf[f % (VD + 1)]),
-                                                                     __builtin_bit_cast(f16x8, ph[f / DT]), acc[f % DT], 0, 0, 0);
-            } else {
-                const bf16x8 v = __builtin_bit_cast(bf16x8, vf[f % (VD + 1)]);
-                acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, ph[f / DT]), acc[f % DT], 0, 0, 0);
-                acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pl[f / DT]), acc[f % DT], 0, 0, 0);
-            }
+            acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % (VD + 1)], ph[f / DT], acc[f % DT], 0, 0, 0);
+            acc[f % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % (VD + 1)], pl[f / DT], acc[f % DT], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (bad) *lost = 1;
     __syncthreads();
-    if (!active) return true;
+    if (!active) return;
     // lane: O^T[32 dt + 8 (j / 4) + 4 h + j % 4][query l % 32]
     const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(lpart), __float_as_uint(lpart), false, false);
     const float sum = __uint_as_float(two[0]) + __uint_as_float(two[1]);
     float *dst = part + wave * part_floats<D>();
-    const float unit = HALF ? __uint_as_float((uint32_t)byte0 << 23) : 1.f;   // of the values
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
-            *(float4 *)(dst + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = {acc[dt][j] * unit, acc[dt][j + 1] * unit,
-                                                                        acc[dt][j + 2] * unit, acc[dt][j + 3] * unit};
-    if (h == 0) *(float2 *)(dst + 32 * D + 2 * r32) = {*lost ? qnan() : mrow - (HALF ? UP : 0), sum};
-    return true;
+            *(float4 *)(dst + 4 * ((8 * dt + j / 2 + h) * 32 + r32)) = {acc[dt][j], acc[dt][j + 1], acc[dt][j + 2], acc[dt][j + 3]};
+    if (h == 0) *(float2 *)(dst + 32 * D + 2 * r32) = {*lost ? qnan() : mrow, sum};
 }
 
 // Workgroup: a kv head (running fastest) of a unit, which is a query tile and split
@@ -809,21 +749,13 @@ __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTabl
             return a.q + (size_t)(row0 + (u0 + m) / G) * a.ldq + (size_t)(kvh * G + (u0 + m) % G) * D;
         };
         float *part = part_at<D>(ws, s, nkv, split, kvh, s.qb0[gi]);
-        const auto few = [&](auto tiles, int first) {  // 16 tiles queries from `first` on
-            attend_few<D, E4, PAGED, tiles.value, 1>(
-                lds, cm, cl, &lost, cv, layer, nkv, kvh, {{p.slot, t0, t_end}}, min(16 * tiles.value, queries - first),
-                [&](int m) { return query(first + m); },
-                [&](int u, int d4, const float4 &o, float m, float l) { emit_part<D>(part, u0 + first + u, d4, o, m, l); });
-        };
-        if constexpr (MT == 128) {
-            __shared__ int scales[2][4];
-            const bool done = attend_many<D, E4, PAGED>(lds, scales, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
-                                                        part + (u0 / 32) * part_floats<D>());
-            if constexpr (E4)
-                for (int first = 0; !done && first < queries; first += 32) few(std::integral_constant<int, 2>(), first);
-        } else {
-            few(std::integral_constant<int, MT / 16>(), 0);
-        }
+        if constexpr (MT == 128)
+            attend_many<D, E4, PAGED>(lds, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
+                                      part + (u0 / 32) * part_floats<D>());
+        else
+            attend_few<D, E4, PAGED, MT / 16, 1>(
+                lds, cm, cl, &lost, cv, layer, nkv, kvh, {{p.slot, t0, t_end}}, queries, query,
+                [&](int u, int d4, const float4 &o, float m, float l) { emit_part<D>(part, u0 + u, d4, o, m, l); });
         return;
     }
     const int v = unit - np, split = v % s.splits_s, r = v / s.splits_s;
