@@ -61,6 +61,38 @@ struct SharedArgs {
     const int32_t *lens, *prefix_slots, *prefix_lens;
     int nq, nkv, d, max_prefix, max_suffix;
 };
+// What a call's lengths and slots, which only the device sees, leave to read; plain
+// functions of numbers, so that a host program can go over all of them.
+// A group's prefix.  len < 0: out of the launch's range.
+struct Prefix {
+    int len, slot;
+};
+__host__ __device__ inline Prefix prefix_within(int len, int slot, int max_prefix, int n_slots)
+{
+    return {len < 0 || len > max_prefix || (unsigned)slot >= (unsigned)n_slots ? -1 : len, slot};
+}
+// Tokens that a row sees, its prefix included: 0 for padding, -1 out of range.
+__host__ __device__ inline int tokens_within(const Prefix &p, int len, int live, int max_suffix, int cap)
+{
+    if (live == 0) return 0;
+    return p.len < 0 || len < p.len || len - p.len > max_suffix || len > cap ? -1 : len;
+}
+// Tokens t_lo .. t_end - 1 of a slot: a split of a prefix, or of what row r has of its
+// own behind it (n of tokens_within).  Nothing: t_lo >= t_end.
+struct Span {
+    int slot, t_lo, t_end;
+};
+__host__ __device__ inline Span prefix_span(const Prefix &p, int chunk, int split)
+{
+    const int t0 = split * chunk;
+    return {p.slot, t0, p.len - t0 < chunk ? p.len : t0 + chunk};
+}
+__host__ __device__ inline Span own_span(const Prefix &p, int r, int n, int chunk, int split)
+{
+    if (p.len < 0 || n <= p.len) return {r, 0, 0};     // a padding row's n is 0, its prefix may be any
+    const int t0 = (p.len & ~15) + split * chunk;
+    return {r, t0 > p.len ? t0 : p.len, n - t0 < chunk ? n : t0 + chunk};
+}
 // A call's launch: where each group's 32-query blocks (of one kv head) and query
 // tiles start, and the splits; by value.
 struct SharedShape {

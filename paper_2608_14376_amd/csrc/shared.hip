@@ -51,24 +51,17 @@ __device__ __forceinline__ int last_at_most(const uint16_t *t, int n, int u)
 
 using Shape = SharedShape;
 
-// A group's prefix.  len < 0: out of the launch's range.
-struct Prefix {
-    int len, slot;
-};
 __device__ __forceinline__ Prefix prefix_of(const SharedArgs &a, const GroupTable &gt, const CacheView &cv, int gi)
 {
     // gi is the same for a wavefront, and so are these: told so, addresses from them stay scalar
     const int p = __builtin_amdgcn_readfirstlane(a.prefix_lens[gi]);
     const int slot = __builtin_amdgcn_readfirstlane(a.prefix_slots == nullptr ? gt.row0[gi] : a.prefix_slots[gi]);
-    const bool bad = p < 0 || p > a.max_prefix || (unsigned)slot >= (unsigned)cv.n_slots;
-    return {bad ? -1 : p, slot};
+    return prefix_within(p, slot, a.max_prefix, cv.n_slots);
 }
-// Tokens that row r sees, its prefix included: 0 for padding, -1 out of range.
 __device__ __forceinline__ int row_len(const SharedArgs &a, const CacheView &cv, const Prefix &p, int r)
 {
     const int n = a.lens[r], live = a.valid == nullptr ? 1 : a.valid[r];   // in flight together
-    if (live == 0) return 0;
-    return p.len < 0 || n < p.len || n - p.len > a.max_suffix || n > cv.cap ? -1 : n;
+    return tokens_within(p, n, live, a.max_suffix, cv.cap);
 }
 
 // What a split leaves of a 32-query block: values [D / 4][32][4], then (maximum in
@@ -189,10 +182,6 @@ constexpr float LAG = 6.f;
 
 template <int D, bool E4>
 constexpr int few_lds() { return 4 * (32 * D * (E4 ? 1 : 2) > 16 * D * 4 ? 32 * D * (E4 ? 1 : 2) : 16 * D * 4); }
-
-struct Span {
-    int slot, t_lo, t_end;
-};
 
 template <int D, bool E4, bool PAGED, int MT, int SPANS, class QueryOf, class Emit>
 __device__ __forceinline__ void attend_few(char *lds, float (*cm)[64], float (*cl)[64], int *lost, const CacheView &cv,
@@ -741,33 +730,33 @@ __global__ __launch_bounds__(256, 2) void k_shared_parts(SharedArgs a, GroupTabl
         const int tile = unit % s.tiles, split = unit / s.tiles;
         const int gi = last_at_most(s.tile0, gt.n, tile);
         const Prefix p = prefix_of(a, gt, cv, gi);
-        const int t0 = split * s.chunk_p;
-        if (t0 >= p.len) return;
-        const int t_end = min(p.len, t0 + s.chunk_p), u0 = (tile - s.tile0[gi]) * MT, row0 = gt.row0[gi];
+        const Span span = prefix_span(p, s.chunk_p, split);
+        if (span.t_lo >= span.t_end) return;
+        const int u0 = (tile - s.tile0[gi]) * MT, row0 = gt.row0[gi];
         const int queries = min(MT, (gt.row0[gi + 1] - row0) * G - u0);
         const auto query = [&](int m) {
             return a.q + (size_t)(row0 + (u0 + m) / G) * a.ldq + (size_t)(kvh * G + (u0 + m) % G) * D;
         };
         float *part = part_at<D>(ws, s, nkv, split, kvh, s.qb0[gi]);
         if constexpr (MT == 128)
-            attend_many<D, E4, PAGED>(lds, &lost, cv, layer, nkv, kvh, p.slot, t0, t_end, queries, query,
+            attend_many<D, E4, PAGED>(lds, &lost, cv, layer, nkv, kvh, span.slot, span.t_lo, span.t_end, queries, query,
                                       part + (u0 / 32) * part_floats<D>());
         else
             attend_few<D, E4, PAGED, MT / 16, 1>(
-                lds, cm, cl, &lost, cv, layer, nkv, kvh, {{p.slot, t0, t_end}}, queries, query,
+                lds, cm, cl, &lost, cv, layer, nkv, kvh, {span}, queries, query,
                 [&](int u, int d4, const float4 &o, float m, float l) { emit_part<D>(part, u0 + u, d4, o, m, l); });
         return;
     }
     const int v = unit - np, split = v % s.splits_s, r = v / s.splits_s;
     const int gi = last_at_most(gt.row0, gt.n, r);
     const Prefix p = prefix_of(a, gt, cv, gi);
-    const int n = row_len(a, cv, p, r), t0 = (p.len & ~15) + split * s.chunk_s;
-    if (n <= p.len || t0 >= n) return;
+    const Span span = own_span(p, r, row_len(a, cv, p, r), s.chunk_s, split);
+    if (span.t_lo >= span.t_end) return;
     const auto query = [&](int m) { return a.q + (size_t)r * a.ldq + (size_t)(kvh * G + m) * D; };
     float *part = part_at<D>(ws, s, nkv, s.splits_p + split, kvh, s.qb0[gi]);
     const int u0 = (r - gt.row0[gi]) * G;
-    attend_few<D, E4, PAGED, 1, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, {{r, max(t0, p.len), min(n, t0 + s.chunk_s)}}, G,
-                                   query, [&](int u, int d4, const float4 &o, float m, float l) {
+    attend_few<D, E4, PAGED, 1, 1>(lds, cm, cl, &lost, cv, layer, nkv, kvh, {span}, G, query,
+                                   [&](int u, int d4, const float4 &o, float m, float l) {
                                        emit_part<D>(part, u0 + u, d4, o, m, l);
                                    });
 }

@@ -90,3 +90,30 @@ def test_scales_apart_at_the_weights(heavy):
     lens = [P + r % 5 for r in range(rows)]
     out = run(hc.device_cache(corun), q.to(DEV), [rows], lens, [P], [rows])
     check(hc, q, out, range(rows), P, lens, rows)
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 0), ("bf16", 16), ("bf16", 48), ("e4m3", 0), ("e4m3", 16), ("e4m3", 48)])
+@pytest.mark.parametrize("many", [1, 20])
+@pytest.mark.parametrize("cap", [192, 1536])
+def test_padding_rows_of_prefixes_out_of_range(dtype, page, many, cap):
+    """Groups whose prefix has no length or no slot, that of row 0 among them: zeros for their padding rows, NaN for live
+    ones, whether the call is one launch (cap 192, few rows) or split; rows of good groups beside them are right."""
+    nq, nkv, d = 8, 2, 128
+    groups = [2 * many, 2 * many, 2 * many, 2 * many, 2 * many, 2]
+    rows = sum(groups)
+    prefix, slots = [-1, cap + 1, 100, 33, 90, 100], [rows, rows, rows + 1, -5, -1, rows]
+    hc = HostCache(nkv, d, rows + 1, cap, 16, page, seed=45, dtype=dtype)
+    if page:
+        hc.table[:5, 0] = 0                            # where reading before a page 0 would leave the cache
+    of = [g for g, n in enumerate(groups) for _ in range(n)]
+    valid = [int(r % 2) for r in range(rows)]
+    lens = [[120, -1, 0, 150][(r // 2) % 4] if r < rows - 2 else 110 for r in range(rows)]
+    valid[-2:] = 1, 1
+    q, qd = rows_of(rows, nq, d, 46)
+    out = torch.full((rows, nq * d), 5.0, dtype=torch.bfloat16, device=DEV)
+    cache = hc.device_cache(corun)
+    ws = torch.full((corun.shared_attention_workspace(cache, groups, nq),), 0xFF, dtype=torch.uint8, device=DEV)
+    out = run(cache, qd, groups, lens, prefix, slots, valid, out=out, ws=ws)
+    for r in range(rows - 2):
+        assert (out[r] == 0).all() if not valid[r] else torch.isnan(out[r]).all(), (r, of[r])
+    check(hc, q, out, [rows - 2, rows - 1], 100, lens, rows)
