@@ -888,7 +888,9 @@ SharedShape shared_shape(const GroupTable &g, int nq, int nkv, int max_prefix, i
     // and 32: 53 us, 59 with 512 workgroups, 81 with 128; 64 rows 35, 40, 47).  Of
     // several, some may be shorter than the longest, and workgroups of many tokens then
     // end late (four of 11 to 30 thousand tokens: 159 us with splits of 1664, 238 of
-    // 7424; eight of 500 to 8000: 60 of 1024, 71 of 2048).
+    // 7424; eight of 500 to 8000: 60 of 1024, 71 of 2048).  Prefixes of up to 15 K tokens
+    // take splits of 1024, longer ones fifteen or sixteen splits: a fifteenth rounded
+    // down, since rounded up the documents' 1920 became 2048 (145 us, 175 so).
     s.chunk_p = chunk(max_prefix, (long long)s.tiles * nkv, 256, g.n == 1 ? 1 << 30 : std::max(1024, max_prefix / 15));
     s.splits_p = (int)(((long long)max_prefix + s.chunk_p - 1) / s.chunk_p);
     const long long suffix = (long long)max_suffix + 15;

@@ -8,7 +8,8 @@ import subprocess
 import numpy as np
 import pytest
 
-from paper_2608_14376_amd import build
+from paper_2608_14376_amd import build, corun
+from tests.test_cache_ops import _i32, _kv
 
 SOURCE = """#include "groups.h"
 using namespace corun;
@@ -92,3 +93,16 @@ def test_spans_of_the_farthest_tokens(spans):
     base = (x[:, 2] & ~15) + t0
     want = np.where(n < 0, 0, np.clip(np.minimum(x[:, 1], base + x[:, 8]) - np.maximum(base, x[:, 2]), 0, None))
     assert np.array_equal(np.where(ra < rb, rb - ra, 0), want)
+
+
+@pytest.mark.parametrize("groups", [(8, 16, 24, 32), (50, 60)])
+@pytest.mark.parametrize("most", [15361, 16000, 20000, 29672, 32768, 65536, 100001, 1 << 20])
+def test_prefixes_of_several_groups_take_sixteen_splits_at_most(groups, most):
+    """The longest split of a prefix beside others is a fifteenth of it, rounded down: read off the workspace, whose parts
+    are [splits][kv heads][blocks of 32 queries][32 (d + 2)] floats, one split of them for 16 tokens of a row's own."""
+    nq, nkv, d = 64, 8, 128
+    kv = _kv(n_slots=sum(groups), max_seq_len=1 << 20)
+    size = corun.load().corun_shared_attention_workspace(ctypes.addressof(kv), nq, nkv, d, len(groups), _i32(*groups), most, 1)
+    blocks = sum(-(-n * (nq // nkv) // 32) for n in groups)
+    splits, rest = divmod(size, nkv * blocks * 32 * (d + 2) * 4)
+    assert rest == 0 and 12 <= splits - 1 <= 16
