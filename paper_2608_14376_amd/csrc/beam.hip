@@ -16,7 +16,7 @@
 //
 // k_beam_part: 195 live rows of 151936 logits, 118 MB, in 36 us, 3.3 TB/s (a copy
 // reaches 5.1).  Its vector arithmetic alone is 24 us, most of it the exponentials
-// in 64 bits (18 instructions for each logit); the rest is waiting for loads and for
+// in 64 bits (19 instructions for each logit); the rest is waiting for loads and for
 // the part's other wavefronts.  Parts of 4096 columns came out the same (39 us), a
 // workgroup that loads its next part while it works on this one slower (58 us for
 // the whole call, 47 so): its registers leave fewer wavefronts.
@@ -63,25 +63,28 @@ __device__ __forceinline__ uint32_t key_high(double x)   // of the upper half: o
     return max(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u), 1u);
 }
 
-// exp(d) of d in [-700, 0], 64 bits, relative error below 1e-13: 2^(n + f) with n
-// the nearest whole number, 2^f by the polynomial of degree 9 that meets it at the
-// Chebyshev points of [-1/2, 1/2] (relative error 2e-14).  Adding 1.5 2^52 leaves
-// n in the low bits, so nothing but additions and multiplications is needed.
+// exp(d) of d in [-700, 0], 64 bits, relative error below 1e-15 down to -40 and 1.1e-14
+// down to -700, and exactly 1 at 0: 2^(n + f) with n the nearest whole number, 2^f by the
+// polynomial of degree 10 that meets it at the Chebyshev points of [-1/2, 1/2], of which
+// 0 is one (relative error 3.2e-16).  A row whose mask leaves one token so keeps its
+// score to the bit, and its ties with finished rows.  Adding 1.5 2^52 leaves n in the
+// low bits, so nothing but additions and multiplications is needed.
 __device__ __forceinline__ double exp_neg(double d)
 {
     const double magic = 6755399441055744.0, log2e = 1.4426950408889634074;
     const double z = __builtin_fma(d, log2e, magic);
     const double f = __builtin_fma(d, log2e, magic - z);
-    double p = 1.0205905366707709e-07;
-    p = __builtin_fma(p, f, 1.3259645242976312e-06);
-    p = __builtin_fma(p, f, 1.5252672925062890e-05);
-    p = __builtin_fma(p, f, 1.5403433751260721e-04);
-    p = __builtin_fma(p, f, 1.3333558200794317e-03);
-    p = __builtin_fma(p, f, 9.6181291939342940e-03);
-    p = __builtin_fma(p, f, 5.5504108664651670e-02);
-    p = __builtin_fma(p, f, 2.4022650695640340e-01);
-    p = __builtin_fma(p, f, 6.9314718055994620e-01);
-    p = __builtin_fma(p, f, 1.0000000000000135);
+    double p = 7.0725859492692234e-09;
+    p = __builtin_fma(p, f, 1.0208690299958306e-07);
+    p = __builtin_fma(p, f, 1.3215442587921689e-06);
+    p = __builtin_fma(p, f, 1.5252657260200837e-05);
+    p = __builtin_fma(p, f, 1.5403530441736050e-04);
+    p = __builtin_fma(p, f, 1.3333558230164974e-03);
+    p = __builtin_fma(p, f, 9.6181291076068882e-03);
+    p = __builtin_fma(p, f, 5.5504108664447722e-02);
+    p = __builtin_fma(p, f, 2.4022650695910097e-01);
+    p = __builtin_fma(p, f, 6.9314718055994995e-01);
+    p = __builtin_fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(z) << 20), __double2loint(p));
 }
 // exp(x - top), what is below exp(-700) as that
