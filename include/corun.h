@@ -510,9 +510,11 @@ int64_t corun_pages_workspace(const corun_kv *kv);
 /* Attention of a decode step whose rows share prefixes, over a bf16 or e4m3
  * cache.  The rows are n_groups groups of group_rows[g] rows each, back to back;
  * row r of group g sees tokens 0 .. prefix_lens[g] - 1 of slot prefix_slots[g],
- * which are read once for the group, and tokens prefix_lens[g] .. lens[r] - 1 of
- * slot r: out = softmax(q k / sqrt(head_dim)) v over all of them, sums in fp32.
- * A prefix of 0 tokens leaves the attention of an ordinary decode step.
+ * which are read once for up to 128 query heads to a kv head of the group (calls of
+ * few rows and at most 512 tokens, one launch, read them for each row), and tokens
+ * prefix_lens[g] .. lens[r] - 1 of slot r: out = softmax(q k / sqrt(head_dim)) v
+ * over all of them, sums in fp32.  A prefix of 0 tokens leaves the attention of an
+ * ordinary decode step.
  *  group_rows  host int32 [n_groups], each >= 1; their sum, the rows, at most
  *              n_slots and 65535 (CORUN_E_SHAPE also where rows, kv heads and
  *              splits make more than 2^24 - 1 workgroups)

@@ -649,8 +649,9 @@ def shared_attention(cache, layer, q, group_rows, lens, prefix_lens, out, ws, pr
     n_heads head_dim]) over a bf16 or e4m3 cache, where the rows are groups of
     group_rows[g] (a host sequence) that share the first prefix_lens[g] tokens
     of slot prefix_slots[g] (None: of each group's first row); row r's own
-    tokens prefix_lens[g] .. lens[r] - 1 are slot r's.  lens, prefix_lens,
-    prefix_slots: device int32; valid: device uint8 [rows].  ws: a device uint8
+    tokens prefix_lens[g] .. lens[r] - 1 are slot r's.  Softmax weights enter the
+    products in about 16 bits.  lens, prefix_lens, prefix_slots: device int32;
+    valid: device uint8 [rows].  ws: a device uint8
     tensor of shared_attention_workspace bytes, not shared by calls that may
     overlap.  Does not wait."""
     rows, nq, ldq, ldo = _attention_rows(cache, q, out)

@@ -14,8 +14,8 @@
 // its place by counting those before it.  Sums and places are in a fixed order,
 // whatever the order in which candidates were noted.
 //
-// k_beam_part: 195 live rows of 151936 logits, 118 MB, in 36 us, 3.3 TB/s (a copy
-// reaches 5.1).  Its vector arithmetic alone is 24 us, most of it the exponentials
+// k_beam_part: 195 live rows of 151936 logits, 118 MB, in 37 us, 3.2 TB/s (a copy
+// reaches 5.1).  Its vector arithmetic alone is some 25 us, most of it the exponentials
 // in 64 bits (19 instructions for each logit); the rest is waiting for loads and for
 // the part's other wavefronts.  Parts of 4096 columns came out the same (39 us), a
 // workgroup that loads its next part while it works on this one slower (58 us for

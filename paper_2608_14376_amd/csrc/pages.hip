@@ -17,9 +17,9 @@
 //
 // The plan is latency, barriers above all: 5 to 8 us in one workgroup (twice the
 // barriers took 1 to 2 us more), 11 to 13 in three launches.  The copies
-// are bound by memory: 148 pages of 1.57 MB (48 layers) moved in 85 us, 5.5 TB/s; 32
-// part-filled pages of 48 layers 18 us.  Pieces of 16 KB whose loads all go out before
-// the stores: one 4 KB head to a workgroup took 24 us there.
+// are bound by memory: 148 pages of 1.57 MB (48 layers) moved in 92 to 98 us, 4.8 to
+// 5.1 TB/s; 32 part-filled pages of 48 layers in 19 to 21.  Pieces of 16 KB whose loads
+// all go out before the stores: one 4 KB head to a workgroup took 24 us there.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
